@@ -468,6 +468,89 @@ int reft_get_tunable(const char *name, uint64_t *value);
 const char *reft_last_error(void);   /* thread-local, never NULL */
 const char *reft_version(void);
 
+/* ==== operators of a training step that repeats to the same bits ======================================
+ * After a restore the steps since the snapshot are run again.  These operators give the same bits each time
+ * they are called on the same values: sums are taken in an order that depends on the sizes alone, without atomics,
+ * and dropout's random bits come out of a counter that the training state holds (a seed and an offset, 16 bytes)
+ * instead of a stored mask or a generator's state.  Together they are the boundary of a residual sublayer in 8 bits:
+ * dropout of the sublayer's output, its addition to the residual stream, root-mean-square norm, 8-bit copies for the
+ * matrix cores, the products of the forward pass and of both gradients.
+ *
+ * Matrices are device pointers with a row length in elements ("ld", at least the number of columns); rows may begin at
+ * any element.  Sums, statistics and products are held in fp32; a result is rounded once, to nearest even, where it is
+ * stored in fewer bits.  The calls enqueue kernels on `stream`, allocate nothing, wait for nothing, keep nothing from call to
+ * call and may be captured in a graph; operands must stay as they are until the stream has passed the call.  They run on the
+ * current GPU.  Arguments are checked before anything is enqueued.  No outputs overlap an input or another output except as said.
+ *
+ * 8-bit matrices (REFT_E4M3: largest value 448; REFT_E5M2: 57344) carry a power of two for each block of 128 columns of a
+ * row, or of 128 x 128 values: the smallest one that makes the block fit the format, at least 2^-126.  Its exponent plus
+ * 127 is a byte, and the bytes of four consecutive blocks of a row lie together: byte j of word w of row r (of row of blocks r)
+ * is scales[(w * ld_s + r) * 4 + j] and belongs to block 4 w + j; bytes behind the last block hold 127 (one).  ld_s counts
+ * words.  There are ceil(columns / 512) words to a row.  Where a block holds an infinity or a NaN, its byte is 255 and all its values are NaN.
+ *
+ * Errors: REFT_EINVAL (null or misaligned pointers, unknown types, p or eps out of range), REFT_ESIZE (rows that
+ * overlap, sizes out of range, a workspace too small), REFT_EHIP.
+ */
+#define REFT_F32  0
+#define REFT_BF16 1
+#define REFT_F16  2
+#define REFT_E4M3 3
+#define REFT_E5M2 4
+
+/* y = dropout(x): element (r, c) is kept where its 16 random bits are at least t = round(65536 p), and multiplied by
+ * 65536 / (65536 - t); else it is 0, whatever x holds there.  The bits are number c % 8 (the low half of a word before the
+ * high one) of Philox4x32-10 with key seed and counter (c / 8, r, offset), low words first: they depend on
+ * neither strides nor launch.  The gradient of x is the same call on the gradient of y.  With p == 0 x is copied.  y may be x
+ * (with the same ld).  0 <= p <= 1; rows, cols < 2^31.
+ */
+int reft_dropout(const void *x, uint64_t ld_x, void *y, uint64_t ld_y, uint64_t rows, uint64_t cols, int dtype,
+                 double p, uint64_t seed, uint64_t offset, reft_stream stream);
+
+/* h = residual + dropout(x) (residual == NULL: h = dropout(x)), rstd[r] = 1 / sqrt(mean(h[r]^2) + eps), and h rstd weight,
+ * taken from h before it is rounded, as y in x's type and, or, as q in 8 bits with scales per 128 columns.  h, rstd, y and q
+ * are each left out where NULL.  h and residual have residual_dtype (dtype or fp32), the weight has weight_dtype (dtype or
+ * fp32).  h may be residual, or x where the types are the same, and y may be x (each with the same ld).  1 <= cols <= 65536.
+ */
+int reft_norm_forward(const void *x, uint64_t ld_x, const void *residual, uint64_t ld_r, const void *weight,
+                      uint64_t rows, uint64_t cols, int dtype, int residual_dtype, int weight_dtype, double eps,
+                      double p, uint64_t seed, uint64_t offset, void *h, uint64_t ld_h, float *rstd, void *y,
+                      uint64_t ld_y, void *q, uint64_t ld_q, int format, void *scales, uint64_t ld_s, reft_stream stream);
+
+/* The gradients of reft_norm_forward's residual, x and weight, from dy (the gradient of its output) and dh (that of h
+ * from elsewhere; NULL = 0), with its h and rstd and the same p, seed and offset:
+ *   dres = rstd (dy weight - h rstd mean(dy weight h rstd)) + dh,  dx = dropout(dres),  dweight[c] = sum over r of dy h rstd.
+ * dy and dx have dtype, dh, h and dres residual_dtype; dweight is fp32.  dres, dx and dweight are each left out where NULL.
+ * dres may be dh and dx may be dy (with the same ld).  rows == 0 gives dweight = 0.  workspace: on 16 bytes, of at least
+ * reft_norm_backward_workspace(rows, cols) bytes where dweight is wanted; scratch, not shared with a call in flight.
+ */
+uint64_t reft_norm_backward_workspace(uint64_t rows, uint64_t cols);
+int reft_norm_backward(const void *dy, uint64_t ld_dy, const void *dh, uint64_t ld_dh, const void *h, uint64_t ld_h,
+                       const float *rstd, const void *weight, uint64_t rows, uint64_t cols, int dtype,
+                       int residual_dtype, int weight_dtype, double p, uint64_t seed, uint64_t offset, void *dres,
+                       uint64_t ld_dres, void *dx, uint64_t ld_dx, float *dweight, void *workspace,
+                       uint64_t workspace_bytes, reft_stream stream);
+
+/* q = x in 8 bits, and q_t = the transpose of x in 8 bits ([cols][ld_qt]); either is left out where NULL.  blocks == 0:
+ * scales per 128 columns of a row of q, and per 128 columns of a row of q_t (which are rows of x).  blocks != 0: one
+ * per 128 x 128 values, the same ones for both, laid out for each with rows of blocks as rows.  rows < 2^31, cols <= 128 * 65535.
+ */
+int reft_quantize(const void *x, uint64_t ld_x, uint64_t rows, uint64_t cols, int dtype, int format, int blocks,
+                  void *q, uint64_t ld_q, void *scales, uint64_t ld_s, void *q_t, uint64_t ld_qt, void *scales_t,
+                  uint64_t ld_st, reft_stream stream);
+
+/* c[m][n] = sum over k of a[m][k] b[n][k], each with its scale.  a has scales per 128 columns of a row; b too, or, with b_blocks != 0,
+ * per 128 x 128 values.  A layer's output is a product of its inputs and weights; the gradient of its inputs one of the output's
+ * gradient and the transposed weights; that of its weights one of both transposes.  What lies between K and ld is not used.
+ * K == 0 gives zeros.  Fastest where both matrices begin at multiples of 16 bytes and their rows too.  workspace: on 16 bytes, of
+ * at least reft_product_workspace(M, N, K) bytes (0 for most sizes); scratch, not shared with a call in flight.
+ * M <= 128 * 65535; N, K < 2^31.
+ */
+uint64_t reft_product_workspace(uint64_t M, uint64_t N, uint64_t K);
+int reft_product(const void *a, uint64_t ld_a, int a_format, const void *a_scales, uint64_t ld_as, const void *b,
+                 uint64_t ld_b, int b_format, const void *b_scales, uint64_t ld_bs, int b_blocks, uint64_t M, uint64_t N,
+                 uint64_t K, void *c, uint64_t ld_c, int c_dtype, void *workspace, uint64_t workspace_bytes,
+                 reft_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,7 +9,8 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libreft.so")
-SOURCES = ["reft_api.hip", "reft_kernels.hip", "reft_stream.hip"]
+SOURCES = ["reft_api.hip", "reft_kernels.hip", "reft_stream.hip", "reft_step.hip",
+           "reft_product.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          # Packed-FP32 instruction selection off for every kernel in the library.  The feature
          # belongs to the gfx950 device pass, where it takes effect (a float2 multiply-add compiles

@@ -24,7 +24,7 @@ using namespace reft;
 // ------------------------------------------------------------------------------------------------
 static thread_local char g_err[512] = "";
 
-static int fail(int code, const char *fmt, ...)
+int reft::fail(int code, const char *fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);

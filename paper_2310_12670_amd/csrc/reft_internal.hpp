@@ -6,6 +6,9 @@
 
 namespace reft {
 
+// Sets the calling thread's message (see reft_last_error) and returns code.
+int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+
 constexpr int kThreads = 256;      // 4 wavefronts of 64 lanes per workgroup
 constexpr int kMaxSrc = 8;         // sources XORed by one launch of the burst and contiguous kernels
 constexpr int kMaxStreamSrc = 16;  // ... and of the stream kernel

@@ -1,0 +1,265 @@
+// Matrix product in 8-bit floating point with a power of two for each block of 128, on the matrix cores.
+#include "reft_step.hpp"
+
+#include <algorithm>
+
+namespace reft {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+struct ProductArgs {
+    const uint8_t *a, *b;          // [M][ld_a], [N][ld_b], K values of a row count
+    const uint32_t *sa, *sb;       // [ceil(K / 512)][ld_sa], [..][ld_sb]: words of four blocks' scales
+    uint64_t ld_a, ld_b, ld_sa, ld_sb, ld_c;
+    uint32_t M, N, K;
+    uint32_t b_shift;              // row n of b has scale n >> b_shift: 7 for blocks of 128 rows, else 0
+    void *c;
+    int c_type;
+};
+
+// ---- tiles in LDS -----------------------------------------------------------------------------------------
+// A row of a tile is 128 values of K: eight chunks of 16 bytes.  Chunk c of row r lies at place c ^ turn(r), so that
+// neither 8 nor 16 rows that are read at one chunk meet in a bank.
+__device__ __forceinline__ int turn(int r) { return (r ^ (r >> 3)) & 7; }
+__device__ __forceinline__ int place(int r, int c) { return r * 128 + ((c ^ turn(r)) << 4); }
+
+// A lane's operand of a product of 32 x 32 x 64: row lane % 32, 32 values of half s of the row's 128.  Which of a half's
+// 64 values a lane takes is the same for both operands, and the scale is the same for all.
+__device__ __forceinline__ i32x8 operand(const uint8_t *tile, int row, int s, int lane)
+{
+    const int c = s * 4 + (lane >> 5) * 2;
+    const w32x4 lo = *(const w32x4 *)(tile + place(row, c)), hi = *(const w32x4 *)(tile + place(row, c + 1));
+    i32x8 v;
+    v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w;
+    v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+    return v;
+}
+
+// What the matrix cores multiply.  Their 8-bit products apply the scales for nothing and run at 4.5 PFLOP/s (a loop of
+// independent ones), but align what they add to its largest part in fewer bits than fp32: measured, the
+// root-mean-square error is 1.5e-5 of the result's at every K from 16 to 8192.  That is lost in the rounding of a 16-bit
+// result (1.7e-3 in bf16, 2e-4 in f16).  Where the result is fp32 (EXACT), the values are turned into bf16, which
+// holds 8 bits times a power of two without error, and multiplied at 2.2 PFLOP/s, with an error of 8e-8.
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+template <int F, bool EXACT> struct Operand;
+template <int F> struct Operand<F, false> {
+    i32x8 v;
+    uint32_t scale;
+    __device__ __forceinline__ void take(i32x8 bytes, uint32_t e) { v = bytes, scale = e; }
+};
+template <int F> struct Operand<F, true> {
+    bf16x8 v[4];
+    __device__ __forceinline__ void take(i32x8 bytes, uint32_t e)
+    {
+        e &= 255;
+        const float f = __uint_as_float(e == 0 ? 0x00400000u : e == 255 ? 0x7fc00000u : e << 23);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bf16x2 lo = F ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(bytes[i], f, false)
+                                : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(bytes[i], f, false);
+            const bf16x2 hi = F ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(bytes[i], f, true)
+                                : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(bytes[i], f, true);
+            v[i / 2][i % 2 * 4] = lo.x, v[i / 2][i % 2 * 4 + 1] = lo.y;
+            v[i / 2][i % 2 * 4 + 2] = hi.x, v[i / 2][i % 2 * 4 + 3] = hi.y;
+        }
+    }
+};
+
+// acc[n][m] += scales * b[n][k] a[m][k]: the transposed product, so that a lane ends up with neighbouring columns of C.
+template <int FA, int FB>
+__device__ __forceinline__ f32x16 multiply(const Operand<FB, false> &b, const Operand<FA, false> &a, f32x16 acc)
+{
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b.v, a.v, acc, FB, FA, 0, (int)b.scale, 0, (int)a.scale);
+}
+template <int FA, int FB>
+__device__ __forceinline__ f32x16 multiply(const Operand<FB, true> &b, const Operand<FA, true> &a, f32x16 acc)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.v[i], a.v[i], acc, 0, 0, 0);
+    return acc;
+}
+
+// 16 bytes at p, of which the first n exist; the others are zero.
+__device__ __forceinline__ w32x4 load16(const uint8_t *p, int n)
+{
+    if (n >= 16) return *(const w32x4_any *)p;
+    w32x4 w = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (i < n) w[i / 4] |= (uint32_t)p[i] << (8 * (i & 3));
+    return w;
+}
+
+// Four neighbouring columns of a row of C, of which the first n exist.
+__device__ __forceinline__ void store4(const ProductArgs &p, uint64_t at, int n, const float v[4])
+{
+    if (n <= 0) return;
+    if (p.c_type == REFT_F32) {
+        float *c = (float *)p.c + at;
+        if (n >= 4) *(w32x4_any *)c = w32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        else for (int i = 0; i < n; ++i) c[i] = v[i];
+        return;
+    }
+    uint16_t t[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = p.c_type == REFT_BF16 ? narrow<bf16>(v[i]).bits : narrow<f16>(v[i]).bits;
+    uint16_t *c = (uint16_t *)p.c + at;
+    if (n >= 4) *(w32x2_any *)c = w32x2{t[0] | (uint32_t)t[1] << 16, t[2] | (uint32_t)t[3] << 16};
+    else for (int i = 0; i < n; ++i) c[i] = t[i];
+}
+
+// One row block of 32 x 32 results: lane holds column m = lane % 32 of the transposed tile and, of each eight rows n,
+// four neighbouring ones.
+__device__ __forceinline__ void store_tile(const ProductArgs &p, uint32_t m, uint32_t n0, int lane, f32x16 acc)
+{
+    if (m >= p.M) return;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const uint32_t n = n0 + 8 * g + 4 * (lane >> 5);
+        const float v[4] = {acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]};
+        store4(p, m * p.ld_c + n, n < p.N ? (int)min(p.N - n, 4u) : 0, v);
+    }
+}
+
+// ---- any sizes, any alignment: tiles of 128 x 128, four waves of 64 x 64 -----------------------------------------
+template <int FA, int FB, bool EXACT> __global__ __launch_bounds__(256) void k_product_any(ProductArgs p)
+{
+    __shared__ __align__(16) uint8_t tile[2][2][128 * 128];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint32_t m0 = blockIdx.y * 128, n0 = blockIdx.x * 128;
+    const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
+    const uint32_t steps = (p.K + 127) / 128;
+    w32x4 next[2][4];
+    auto load = [&](uint32_t step) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = (tid >> 3) + 32 * i;
+            const uint32_t k = step * 128 + (tid & 7) * 16;
+            const int n = k < p.K ? (int)min(p.K - k, 16u) : 0;
+            next[0][i] = load16(p.a + (m0 + r) * p.ld_a + k, m0 + r < p.M ? n : 0);
+            next[1][i] = load16(p.b + (n0 + r) * p.ld_b + k, n0 + r < p.N ? n : 0);
+        }
+    };
+    auto keep = [&](int half) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = (tid >> 3) + 32 * i;
+            *(w32x4 *)(tile[half][0] + place(r, tid & 7)) = next[0][i];
+            *(w32x4 *)(tile[half][1] + place(r, tid & 7)) = next[1][i];
+        }
+    };
+    f32x16 acc[2][2] = {};
+    uint32_t sa[2] = {}, sb[2] = {};
+    if (steps) {
+        load(0);
+        keep(0);
+    }
+    for (uint32_t step = 0; step < steps; ++step) {
+        __syncthreads();
+        const int half = step & 1;
+        if (step + 1 < steps) load(step + 1);
+        if (step % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                sa[i] = p.sa[step / 4 * p.ld_sa + min(m0 + wm + i * 32 + (lane & 31), p.M - 1)];
+                sb[i] = p.sb[step / 4 * p.ld_sb + (min(n0 + wn + i * 32 + (lane & 31), p.N - 1) >> p.b_shift)];
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            Operand<FA, EXACT> a[2];
+            Operand<FB, EXACT> b[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                a[i].take(operand(tile[half][0], wm + i * 32 + (lane & 31), s, lane), sa[i]);
+                b[i].take(operand(tile[half][1], wn + i * 32 + (lane & 31), s, lane), sb[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = multiply<FA, FB>(b[j], a[i], acc[i][j]);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            sa[i] >>= 8;
+            sb[i] >>= 8;
+        }
+        if (step + 1 < steps) keep(half ^ 1);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            store_tile(p, m0 + wm + i * 32 + (lane & 31), n0 + wn + j * 32, lane, acc[i][j]);
+}
+
+template <int FA, int FB> static hipError_t launch_product(const ProductArgs &p, hipStream_t s)
+{
+    const dim3 grid((p.N + 127) / 128, (p.M + 127) / 128);
+    if (p.c_type == REFT_F32) k_product_any<FA, FB, true><<<grid, 256, 0, s>>>(p);
+    else k_product_any<FA, FB, false><<<grid, 256, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+}  // namespace reft
+
+using namespace reft;
+
+extern "C" uint64_t reft_product_workspace(uint64_t M, uint64_t N, uint64_t K)
+{
+    (void)M;
+    (void)N;
+    (void)K;
+    return 0;
+}
+
+extern "C" int reft_product(const void *a, uint64_t ld_a, int a_format, const void *a_scales, uint64_t ld_as, const void *b,
+                            uint64_t ld_b, int b_format, const void *b_scales, uint64_t ld_bs, int b_blocks, uint64_t M, uint64_t N,
+                            uint64_t K, void *c, uint64_t ld_c, int c_dtype, void *workspace, uint64_t workspace_bytes,
+                            reft_stream stream)
+{
+#define NEED(cond, code, ...)                                                                     \
+    do {                                                                                          \
+        if (!(cond)) return fail(code, "reft_product: " __VA_ARGS__);                             \
+    } while (0)
+    NEED((a_format == REFT_E4M3 || a_format == REFT_E5M2) && (b_format == REFT_E4M3 || b_format == REFT_E5M2), REFT_EINVAL,
+         "unknown 8-bit format");
+    NEED(c_dtype == REFT_F32 || c_dtype == REFT_BF16 || c_dtype == REFT_F16, REFT_EINVAL, "unknown type %d", c_dtype);
+    // rows of tiles are counted by the grid's second dimension
+    NEED(M <= 128 * 65535 && N <= 0x7fffffff && K <= 0x7fffffff, REFT_ESIZE, "a matrix is too large");
+    NEED(!M || !N || (c && (!K || (a && b && a_scales && b_scales))), REFT_EINVAL, "null pointer");
+    NEED(ld_c >= N && ld_a >= K && ld_b >= K, REFT_ESIZE, "rows overlap");
+    NEED(ld_as >= M && ld_bs >= (b_blocks ? (N + 127) / 128 : N), REFT_ESIZE, "words of scales overlap");
+    if (!M || !N) return REFT_OK;
+    NEED((uintptr_t)c % (c_dtype == REFT_F32 ? 4 : 2) == 0 && (uintptr_t)a_scales % 4 == 0 && (uintptr_t)b_scales % 4 == 0, REFT_EINVAL,
+         "misaligned pointer");
+    const uint64_t need = reft_product_workspace(M, N, K);
+    NEED(!need || (workspace && (uintptr_t)workspace % 16 == 0), REFT_EINVAL, "no workspace, or not on 16 bytes");
+    NEED(workspace_bytes >= need, REFT_ESIZE, "workspace too small");
+#undef NEED
+    ProductArgs p;
+    p.a = (const uint8_t *)a;
+    p.b = (const uint8_t *)b;
+    p.sa = (const uint32_t *)a_scales;
+    p.sb = (const uint32_t *)b_scales;
+    p.ld_a = ld_a;
+    p.ld_b = ld_b;
+    p.ld_sa = ld_as;
+    p.ld_sb = ld_bs;
+    p.ld_c = ld_c;
+    p.M = (uint32_t)M;
+    p.N = (uint32_t)N;
+    p.K = (uint32_t)K;
+    p.b_shift = b_blocks ? 7 : 0;
+    p.c = c;
+    p.c_type = c_dtype;
+    hipStream_t s = (hipStream_t)stream;
+    hipError_t e;
+    if (a_format == REFT_E4M3) e = b_format == REFT_E4M3 ? launch_product<0, 0>(p, s) : launch_product<0, 1>(p, s);
+    else e = b_format == REFT_E4M3 ? launch_product<1, 0>(p, s) : launch_product<1, 1>(p, s);
+    if (e != hipSuccess) return fail(REFT_EHIP, "reft_product: %s", hipGetErrorString(e));
+    return REFT_OK;
+}

@@ -1,0 +1,645 @@
+// Operators of a training step that read and write each value once: dropout, root-mean-square norm with the
+// residual's addition (forward, backward), quantization to 8 bits.  Kernels and their entry points (see include/reft.h).
+#include "reft_step.hpp"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+namespace reft {
+
+// ------------------------------------------------------------------------------------------------
+// dropout
+// ------------------------------------------------------------------------------------------------
+struct DropoutArgs {
+    const void *x;
+    void *y;
+    uint64_t ld_x, ld_y;
+    uint64_t cols, groups, total;  // groups of eight columns in a row, and in the matrix
+    uint32_t inverse;              // floor(2^32 / groups)
+    Dropout d;
+};
+
+constexpr int kDropUnroll = 4;
+
+// A thread takes kDropUnroll groups.  Row and group of a block's first come of one division of whole numbers, those of
+// its threads of a multiplication.
+template <typename T> __global__ __launch_bounds__(256) void k_dropout(DropoutArgs a)
+{
+    const uint64_t first = (uint64_t)blockIdx.x * (256 * kDropUnroll);
+    const uint64_t row0 = first / a.groups;
+    const uint32_t rem = (uint32_t)(first - row0 * a.groups), groups = (uint32_t)a.groups;
+    float v[kDropUnroll][8];
+    uint32_t row[kDropUnroll], group[kDropUnroll];
+    int n[kDropUnroll];
+#pragma unroll
+    for (int u = 0; u < kDropUnroll; ++u) {
+        const uint32_t local = u * 256 + threadIdx.x, at = rem + local;
+        uint32_t r = __umulhi(at, a.inverse);
+        if (at - r * groups >= groups) ++r;                 // the rounded inverse may be one row short
+        row[u] = (uint32_t)row0 + r;
+        group[u] = at - r * groups;
+        const uint64_t left = a.cols - (uint64_t)group[u] * 8;
+        n[u] = first + local < a.total ? (int)(left < 8 ? left : 8) : 0;
+        load8((const T *)a.x + (uint64_t)row[u] * a.ld_x + (uint64_t)group[u] * 8, n[u], v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kDropUnroll; ++u) {
+        if (a.d.threshold) drop8(a.d, row[u], group[u], v[u]);
+        store8((T *)a.y + (uint64_t)row[u] * a.ld_y + (uint64_t)group[u] * 8, n[u], v[u]);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// norm
+// ------------------------------------------------------------------------------------------------
+struct NormForward {
+    const void *x, *residual, *weight;
+    uint64_t ld_x, ld_r;
+    uint32_t rows, cols;
+    float eps;
+    Dropout d;
+    void *h;
+    uint64_t ld_h;
+    float *rstd;
+    void *y;
+    uint64_t ld_y;
+    uint8_t *q;
+    uint64_t ld_q;
+    uint8_t *scales;
+    uint64_t ld_s;
+    uint8_t e5m2, weight_f32;
+};
+
+__device__ __forceinline__ float wave_sum(float v)
+{
+#pragma unroll
+    for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
+    return v;
+}
+
+// A row belongs to NW waves (four rows a block where that is one), each lane holds V times eight neighbouring columns
+// of it in registers, in fp32: one pass over the inputs whatever the row's length.  A wave's 512 columns are four
+// blocks of 128, 16 lanes each: one word of scales.
+template <typename T, typename R, int NW, int V>
+__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_forward(NormForward a)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t row = NW == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+    if (row >= a.rows) return;
+    const int first = (NW == 1 ? 0 : wave * 512) + lane * 8, cols = (int)a.cols;
+    float h[V][8], sum = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int c = first + v * NW * 512;
+        load8((const T *)a.x + row * a.ld_x + c, cols - c, h[v]);
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int c = first + v * NW * 512;
+        float r[8] = {};
+        if (a.residual) load8((const R *)a.residual + row * a.ld_r + c, cols - c, r);
+        if (a.d.threshold) drop8(a.d, row, (uint32_t)c / 8, h[v]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            h[v][i] += r[i];
+            sum += h[v][i] * h[v][i];
+        }
+        if (a.h) store8((R *)a.h + row * a.ld_h + c, cols - c, h[v]);
+    }
+    sum = wave_sum(sum);
+    if constexpr (NW > 1) {
+        __shared__ float part[NW];
+        if (lane == 0) part[wave] = sum;
+        __syncthreads();
+        sum = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) sum += part[i];
+    }
+    const float rstd = 1.f / sqrtf(sum / (float)cols + a.eps);
+    if (a.rstd && lane == 0 && (NW == 1 || wave == 0)) a.rstd[row] = rstd;
+    if (!a.y && !a.q) return;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int c = first + v * NW * 512;
+        float w[8];
+        load8_of<T>(a.weight, a.weight_f32, c, cols - c, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] *= h[v][i] * rstd;
+        if (a.y) store8((T *)a.y + row * a.ld_y + c, cols - c, w);
+        if (a.q) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most = max(most, magnitude(w[i]));
+#pragma unroll
+            for (int m = 8; m; m >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, m));
+            const uint32_t e = scale_of(most, top_of(a.e5m2));
+            store8_bytes(a.q + row * a.ld_q + c, cols - c, to_eight(w, inverse_of(e), a.e5m2));
+            const int word = c / 512;                       // the same in the whole wave
+            if ((lane & 15) == 0 && word * 512 < cols)
+                a.scales[(word * a.ld_s + row) * 4 + lane / 16] = c < cols ? (uint8_t)e : 127;
+        }
+    }
+}
+
+struct NormBackward {
+    const void *dy, *dh, *h, *weight;
+    const float *rstd;
+    uint64_t ld_dy, ld_dh, ld_h;
+    uint32_t rows, cols, workers;
+    Dropout d;
+    void *dres, *dx;
+    uint64_t ld_dres, ld_dx;
+    float *part;                   // [workers][cols]
+    uint8_t weight_f32;
+};
+
+// A worker (a block, or a wave where a row is a wave's) takes rows worker, worker + workers, ..., and keeps its part of
+// the weight's gradient in registers; k_sum_parts adds the workers' parts in their order.
+template <typename T, typename R, int NW, int V>
+__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_backward(NormBackward a)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t worker = NW == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+    if (worker >= a.workers) return;
+    const int first = (NW == 1 ? 0 : wave * 512) + lane * 8, cols = (int)a.cols;
+    __shared__ float part[2][NW];
+    float dw[V][8] = {};
+    int half = 0;
+    for (uint32_t row = worker; row < a.rows; row += a.workers, half ^= 1) {
+        float x[V][8], g[V][8], dot = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = first + v * NW * 512;
+            load8((const R *)a.h + row * a.ld_h + c, cols - c, x[v]);
+            load8((const T *)a.dy + row * a.ld_dy + c, cols - c, g[v]);
+        }
+        const float rstd = a.rstd[row];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = first + v * NW * 512;
+            float w[8];
+            load8_of<T>(a.weight, a.weight_f32, c, cols - c, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[v][i] *= rstd;
+                dw[v][i] += g[v][i] * x[v][i];
+                g[v][i] *= w[i];
+                dot += g[v][i] * x[v][i];
+            }
+        }
+        dot = wave_sum(dot);
+        if constexpr (NW > 1) {
+            if (lane == 0) part[half][wave] = dot;
+            __syncthreads();       // the other half is written before the next one, and read after it
+            dot = 0;
+#pragma unroll
+            for (int i = 0; i < NW; ++i) dot += part[half][i];
+        }
+        dot /= (float)cols;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = first + v * NW * 512;
+            float r[8] = {};
+            if (a.dh) load8((const R *)a.dh + row * a.ld_dh + c, cols - c, r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[i] += rstd * (g[v][i] - x[v][i] * dot);
+            if (a.dres) store8((R *)a.dres + row * a.ld_dres + c, cols - c, r);
+            if (a.dx) {
+                if (a.d.threshold) drop8(a.d, row, (uint32_t)c / 8, r);
+                store8((T *)a.dx + row * a.ld_dx + c, cols - c, r);
+            }
+        }
+    }
+    if (a.part) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = first + v * NW * 512;
+            store8(a.part + (uint64_t)worker * a.cols + c, cols - c, dw[v]);
+        }
+    }
+}
+
+// out[c] = sum of n rows of part, in an order that depends on n alone: 16 interleaved sums, then those one after the other.
+__global__ __launch_bounds__(1024) void k_sum_parts(const float *part, uint32_t n, uint32_t cols, float *out)
+{
+    __shared__ float sums[16][64];
+    const uint32_t x = threadIdx.x & 63, y = threadIdx.x >> 6, c = blockIdx.x * 64 + x;
+    float s = 0;
+    if (c < cols)
+        for (uint32_t i = y; i < n; i += 16) s += part[(uint64_t)i * cols + c];
+    sums[y][x] = s;
+    __syncthreads();
+    if (y == 0 && c < cols) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) s += sums[i][x];
+        out[c] = s;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// quantization
+// ------------------------------------------------------------------------------------------------
+struct QuantizeArgs {
+    const void *x;
+    uint64_t ld_x, rows, cols;
+    uint8_t *q, *scales, *q_t, *scales_t;
+    uint64_t ld_q, ld_s, ld_qt, ld_st;
+    uint8_t e5m2;
+};
+
+// A scale for each 128 columns of a row: a wave takes 512 columns of a row, 16 lanes each block.
+template <typename T> __global__ __launch_bounds__(256) void k_quantize_rows(QuantizeArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const uint64_t row = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6), c = (uint64_t)blockIdx.y * 512 + lane * 8;
+    if (row >= a.rows) return;
+    const int n = c >= a.cols ? 0 : (int)min(a.cols - c, (uint64_t)8);
+    float v[8];
+    load8((const T *)a.x + row * a.ld_x + c, n, v);
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[i]));
+#pragma unroll
+    for (int m = 8; m; m >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, m));
+    const uint32_t e = scale_of(most, top_of(a.e5m2));
+    store8_bytes(a.q + row * a.ld_q + c, n, to_eight(v, inverse_of(e), a.e5m2));
+    if ((lane & 15) == 0) a.scales[((uint64_t)blockIdx.y * a.ld_s + row) * 4 + lane / 16] = n ? (uint8_t)e : 127;
+}
+
+// The scale byte of block b of a row, and ones in the rest of its word behind the last of the `blocks` blocks.
+__device__ __forceinline__ void store_scale(uint8_t *scales, uint64_t ld, uint64_t row, uint64_t b, uint64_t blocks, uint32_t e)
+{
+    uint8_t *word = scales + ((b / 4) * ld + row) * 4;
+    word[b % 4] = (uint8_t)e;
+    if (b + 1 == blocks)
+        for (int i = (int)(b % 4) + 1; i < 4; ++i) word[i] = 127;
+}
+
+// A tile of 128 x 128 values, in registers: a thread holds 8 rows of 8 columns, so that each of its columns is 8 bytes of
+// the transpose, which leaves through LDS in whole rows.  BLOCKS: one scale for the tile, else one for each row and, in the
+// transpose, for each column.
+template <typename T, bool BLOCKS> __global__ __launch_bounds__(256) void k_quantize_tile(QuantizeArgs a)
+{
+    constexpr int kPitch = 1024 + 32;          // LDS bytes of eight columns of 128 rows: 16 lanes' writes meet no bank twice
+    __shared__ __align__(16) uint8_t tile[16 * kPitch];
+    __shared__ uint32_t most_of[4][128];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, tc = tid & 15, tr = tid >> 4;
+    const uint64_t row0 = (uint64_t)blockIdx.x * 128, col0 = (uint64_t)blockIdx.y * 128;
+    const int rows = (int)min(a.rows - row0, (uint64_t)128), cols = (int)min(a.cols - col0, (uint64_t)128);
+    float v[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        load8((const T *)a.x + (row0 + tr * 8 + i) * a.ld_x + col0 + tc * 8, tr * 8 + i < rows ? cols - tc * 8 : 0, v[i]);
+    const int top = top_of(a.e5m2);
+    uint32_t by_col[8] = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) by_col[j] = max(by_col[j], magnitude(v[i][j]));
+    uint32_t e_tile = 0;
+    if constexpr (BLOCKS) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, by_col[j]);
+#pragma unroll
+        for (int s = 32; s; s >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, s));
+        if (lane == 0) most_of[wave][0] = m;
+        __syncthreads();
+        e_tile = scale_of(max(max(most_of[0][0], most_of[1][0]), max(most_of[2][0], most_of[3][0])), top);
+        if (tid == 0) {
+            const uint64_t high = (a.rows + 127) / 128, wide = (a.cols + 127) / 128;
+            if (a.q) store_scale(a.scales, a.ld_s, blockIdx.x, blockIdx.y, wide, e_tile);
+            if (a.q_t) store_scale(a.scales_t, a.ld_st, blockIdx.y, blockIdx.x, high, e_tile);
+        }
+    }
+    if (a.q) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t e = e_tile;
+            const int r = tr * 8 + i;
+            if constexpr (!BLOCKS) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) m = max(m, magnitude(v[i][j]));
+#pragma unroll
+                for (int s = 8; s; s >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, s));
+                e = scale_of(m, top);
+                if (tc == 0 && r < rows) store_scale(a.scales, a.ld_s, row0 + r, blockIdx.y, (a.cols + 127) / 128, e);
+            }
+            if (r < rows) store8_bytes(a.q + (row0 + r) * a.ld_q + col0 + tc * 8, cols - tc * 8, to_eight(v[i], inverse_of(e), a.e5m2));
+        }
+    }
+    if (!a.q_t) return;
+    if constexpr (!BLOCKS) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            by_col[j] = max(by_col[j], (uint32_t)__shfl_xor((int)by_col[j], 16));
+            by_col[j] = max(by_col[j], (uint32_t)__shfl_xor((int)by_col[j], 32));
+            if (lane < 16) most_of[wave][tc * 8 + j] = by_col[j];
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        uint32_t e = e_tile;
+        const int c = tc * 8 + j;
+        if constexpr (!BLOCKS) {
+            e = scale_of(max(max(most_of[0][c], most_of[1][c]), max(most_of[2][c], most_of[3][c])), top);
+            if (tr == 0 && c < cols) store_scale(a.scales_t, a.ld_st, col0 + c, blockIdx.x, (a.rows + 127) / 128, e);
+        }
+        float t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = v[i][j];
+        *(w32x2 *)(tile + tc * kPitch + j * 128 + tr * 8) = to_eight(t, inverse_of(e), a.e5m2);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int c = (tid >> 3) + 32 * k, r = (tid & 7) * 16;
+        if (c >= cols || r >= rows) continue;
+        const w32x4 w = *(const w32x4 *)(tile + (c / 8) * kPitch + (c % 8) * 128 + r);
+        uint8_t *p = a.q_t + (col0 + c) * a.ld_qt + row0 + r;
+        if (r + 16 <= rows) {
+            *(w32x4_any *)p = w;
+        } else {
+            for (int i = 0; i < rows - r; ++i) p[i] = tile[(c / 8) * kPitch + (c % 8) * 128 + r + i];
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// which kernel
+// ------------------------------------------------------------------------------------------------
+// Waves that share a row and columns that a lane holds (times eight): NW * V * 512 >= cols.
+template <typename T, typename R, template <typename, typename, int, int> class Launch, typename A>
+static hipError_t by_width(const A &a, uint32_t rows, uint32_t cols, hipStream_t stream)
+{
+    if (cols <= 512) return Launch<T, R, 1, 1>::go(a, stream);
+    if (cols <= 1024) return Launch<T, R, 1, 2>::go(a, stream);
+    if (cols <= 2048) return Launch<T, R, 1, 4>::go(a, stream);
+    if (cols <= 4096) return Launch<T, R, 4, 2>::go(a, stream);
+    if (cols <= 8192) return Launch<T, R, 4, 4>::go(a, stream);
+    if (cols <= 16384) return Launch<T, R, 4, 8>::go(a, stream);
+    if (cols <= 32768) return Launch<T, R, 16, 4>::go(a, stream);
+    return Launch<T, R, 16, 8>::go(a, stream);
+}
+
+template <typename T, typename R, int NW, int V> struct Forward {
+    static hipError_t go(const NormForward &a, hipStream_t s)
+    {
+        k_norm_forward<T, R, NW, V><<<NW == 1 ? (a.rows + 3) / 4 : a.rows, NW == 1 ? 256 : 64 * NW, 0, s>>>(a);
+        return hipGetLastError();
+    }
+};
+template <typename T, typename R, int NW, int V> struct Backward {
+    static hipError_t go(const NormBackward &a, hipStream_t s)
+    {
+        k_norm_backward<T, R, NW, V><<<NW == 1 ? (a.workers + 3) / 4 : a.workers, NW == 1 ? 256 : 64 * NW, 0, s>>>(a);
+        return hipGetLastError();
+    }
+};
+
+template <template <typename, typename, int, int> class Launch, typename A>
+static hipError_t by_types(const A &a, int dtype, int residual, hipStream_t s)
+{
+    if (dtype == REFT_F32) return by_width<float, float, Launch>(a, a.rows, a.cols, s);
+    if (dtype == REFT_BF16)
+        return residual == REFT_F32 ? by_width<bf16, float, Launch>(a, a.rows, a.cols, s)
+                                    : by_width<bf16, bf16, Launch>(a, a.rows, a.cols, s);
+    return residual == REFT_F32 ? by_width<f16, float, Launch>(a, a.rows, a.cols, s)
+                                : by_width<f16, f16, Launch>(a, a.rows, a.cols, s);
+}
+
+constexpr uint64_t kMaxCols = 65536;       // of a norm: 16 waves, 8 times 8 columns a lane
+constexpr uint64_t kMaxWorkers = 1024;
+
+static uint32_t workers_of(uint64_t rows)
+{
+    return (uint32_t)std::min<uint64_t>(rows, kMaxWorkers);
+}
+
+static bool is_float_type(int t) { return t == REFT_F32 || t == REFT_BF16 || t == REFT_F16; }
+static bool is_eight(int t) { return t == REFT_E4M3 || t == REFT_E5M2; }
+static size_t size_of(int t) { return t == REFT_F32 ? 4 : 2; }
+// Arrays of elements lie on multiples of an element.
+static bool lies(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
+
+// p in [0, 1] as a threshold of 65536; false if it is none.
+static bool make_dropout(double p, uint64_t seed, uint64_t offset, Dropout *d)
+{
+    if (!(p >= 0 && p <= 1)) return false;
+    const long t = std::lround(p * 65536);
+    d->key0 = (uint32_t)seed;
+    d->key1 = (uint32_t)(seed >> 32);
+    d->off0 = (uint32_t)offset;
+    d->off1 = (uint32_t)(offset >> 32);
+    d->threshold = (uint32_t)t;
+    d->scale = t >= 65536 ? 0.f : (float)(65536.0 / (double)(65536 - t));
+    return true;
+}
+
+}  // namespace reft
+
+using namespace reft;
+
+#define NEED(cond, code, ...)                                                                     \
+    do {                                                                                          \
+        if (!(cond)) return fail(code, __VA_ARGS__);                                              \
+    } while (0)
+
+static int launched(const char *who, hipError_t e)
+{
+    if (e != hipSuccess) return fail(REFT_EHIP, "%s: %s", who, hipGetErrorString(e));
+    return REFT_OK;
+}
+
+extern "C" int reft_dropout(const void *x, uint64_t ld_x, void *y, uint64_t ld_y, uint64_t rows, uint64_t cols, int dtype,
+                            double p, uint64_t seed, uint64_t offset, reft_stream stream)
+{
+    DropoutArgs a;
+    NEED(is_float_type(dtype), REFT_EINVAL, "reft_dropout: unknown type %d", dtype);
+    NEED(make_dropout(p, seed, offset, &a.d), REFT_EINVAL, "reft_dropout: p is not within [0, 1]");
+    NEED(rows <= 0x7fffffff && cols <= 0x7fffffff, REFT_ESIZE, "reft_dropout: too many rows or columns");
+    NEED(ld_x >= cols && ld_y >= cols, REFT_ESIZE, "reft_dropout: rows overlap");
+    if (!rows || !cols) return REFT_OK;
+    NEED(x && y, REFT_EINVAL, "reft_dropout: null pointer");
+    NEED(lies(x, size_of(dtype)) && lies(y, size_of(dtype)), REFT_EINVAL, "reft_dropout: misaligned pointer");
+    a.x = x;
+    a.y = y;
+    a.ld_x = ld_x;
+    a.ld_y = ld_y;
+    a.cols = cols;
+    a.groups = (cols + 7) / 8;
+    a.total = a.groups * rows;
+    a.inverse = (uint32_t)std::min<uint64_t>((1ull << 32) / a.groups, 0xffffffffu);
+    const uint64_t blocks = (a.total + 256 * kDropUnroll - 1) / (256 * kDropUnroll);
+    NEED(blocks <= 0x7fffffff, REFT_ESIZE, "reft_dropout: too many values");
+    hipStream_t s = (hipStream_t)stream;
+    if (dtype == REFT_F32) k_dropout<float><<<(uint32_t)blocks, 256, 0, s>>>(a);
+    else if (dtype == REFT_BF16) k_dropout<bf16><<<(uint32_t)blocks, 256, 0, s>>>(a);
+    else k_dropout<f16><<<(uint32_t)blocks, 256, 0, s>>>(a);
+    return launched("reft_dropout", hipGetLastError());
+}
+
+extern "C" int reft_norm_forward(const void *x, uint64_t ld_x, const void *residual, uint64_t ld_r, const void *weight,
+                                 uint64_t rows, uint64_t cols, int dtype, int residual_dtype, int weight_dtype, double eps,
+                                 double p, uint64_t seed, uint64_t offset, void *h, uint64_t ld_h, float *rstd, void *y,
+                                 uint64_t ld_y, void *q, uint64_t ld_q, int format, void *scales, uint64_t ld_s,
+                                 reft_stream stream)
+{
+    NormForward a;
+    NEED(is_float_type(dtype), REFT_EINVAL, "reft_norm_forward: unknown type %d", dtype);
+    NEED(residual_dtype == dtype || residual_dtype == REFT_F32, REFT_EINVAL,
+         "reft_norm_forward: the residual has the type of x or fp32");
+    NEED(weight_dtype == dtype || weight_dtype == REFT_F32, REFT_EINVAL, "reft_norm_forward: the weight has the type of x or fp32");
+    NEED(eps >= 0 && eps <= 1e30, REFT_EINVAL, "reft_norm_forward: eps is negative or no number");
+    NEED(make_dropout(p, seed, offset, &a.d), REFT_EINVAL, "reft_norm_forward: p is not within [0, 1]");
+    NEED(cols >= 1 && cols <= kMaxCols, REFT_ESIZE, "reft_norm_forward: rows have 1 to %llu columns", (unsigned long long)kMaxCols);
+    NEED(rows <= 0x7fffffff, REFT_ESIZE, "reft_norm_forward: too many rows");
+    NEED(ld_x >= cols && (!residual || ld_r >= cols) && (!h || ld_h >= cols) && (!y || ld_y >= cols) && (!q || ld_q >= cols),
+         REFT_ESIZE, "reft_norm_forward: rows overlap");
+    NEED(h || rstd || y || q || !rows, REFT_EINVAL, "reft_norm_forward: no output");
+    if (q) {
+        NEED(is_eight(format), REFT_EINVAL, "reft_norm_forward: unknown 8-bit format %d", format);
+        NEED(scales || !rows, REFT_EINVAL, "reft_norm_forward: 8 bits without scales");
+        NEED(ld_s >= rows, REFT_ESIZE, "reft_norm_forward: words of scales overlap");
+    }
+    if (!rows) return REFT_OK;
+    NEED(x && (weight || (!y && !q)), REFT_EINVAL, "reft_norm_forward: null pointer");
+    NEED(lies(x, size_of(dtype)) && lies(y, size_of(dtype)) && lies(residual, size_of(residual_dtype)) &&
+             lies(h, size_of(residual_dtype)) && lies(weight, size_of(weight_dtype)) && lies(rstd, 4),
+         REFT_EINVAL, "reft_norm_forward: misaligned pointer");
+    a.x = x;
+    a.residual = residual;
+    a.weight = weight;
+    a.ld_x = ld_x;
+    a.ld_r = ld_r;
+    a.rows = (uint32_t)rows;
+    a.cols = (uint32_t)cols;
+    a.eps = (float)eps;
+    a.h = h;
+    a.ld_h = ld_h;
+    a.rstd = rstd;
+    a.y = y;
+    a.ld_y = ld_y;
+    a.q = (uint8_t *)q;
+    a.ld_q = ld_q;
+    a.scales = (uint8_t *)scales;
+    a.ld_s = ld_s;
+    a.e5m2 = format == REFT_E5M2;
+    a.weight_f32 = weight_dtype == REFT_F32;
+    return launched("reft_norm_forward", by_types<Forward>(a, dtype, residual_dtype, (hipStream_t)stream));
+}
+
+extern "C" uint64_t reft_norm_backward_workspace(uint64_t rows, uint64_t cols)
+{
+    const uint64_t workers = workers_of(rows);
+    return workers > 1 && cols <= kMaxCols ? workers * cols * sizeof(float) : 0;
+}
+
+extern "C" int reft_norm_backward(const void *dy, uint64_t ld_dy, const void *dh, uint64_t ld_dh, const void *h, uint64_t ld_h,
+                                  const float *rstd, const void *weight, uint64_t rows, uint64_t cols, int dtype,
+                                  int residual_dtype, int weight_dtype, double p, uint64_t seed, uint64_t offset, void *dres,
+                                  uint64_t ld_dres, void *dx, uint64_t ld_dx, float *dweight, void *workspace,
+                                  uint64_t workspace_bytes, reft_stream stream)
+{
+    NormBackward a;
+    NEED(is_float_type(dtype), REFT_EINVAL, "reft_norm_backward: unknown type %d", dtype);
+    NEED(residual_dtype == dtype || residual_dtype == REFT_F32, REFT_EINVAL,
+         "reft_norm_backward: the residual has the type of dy or fp32");
+    NEED(weight_dtype == dtype || weight_dtype == REFT_F32, REFT_EINVAL, "reft_norm_backward: the weight has the type of dy or fp32");
+    NEED(make_dropout(p, seed, offset, &a.d), REFT_EINVAL, "reft_norm_backward: p is not within [0, 1]");
+    NEED(cols >= 1 && cols <= kMaxCols, REFT_ESIZE, "reft_norm_backward: rows have 1 to %llu columns", (unsigned long long)kMaxCols);
+    NEED(rows <= 0x7fffffff, REFT_ESIZE, "reft_norm_backward: too many rows");
+    NEED((!rows || ld_dy >= cols) && (!dh || ld_dh >= cols) && (!rows || ld_h >= cols) && (!dres || ld_dres >= cols) && (!dx || ld_dx >= cols),
+         REFT_ESIZE, "reft_norm_backward: rows overlap");
+    NEED(dres || dx || dweight || !rows, REFT_EINVAL, "reft_norm_backward: no output");
+    hipStream_t s = (hipStream_t)stream;
+    a.workers = workers_of(rows);
+    if (dweight) {
+        NEED(lies(dweight, 4), REFT_EINVAL, "reft_norm_backward: misaligned pointer");
+        if (a.workers > 1) {
+            NEED(workspace && lies(workspace, 16), REFT_EINVAL, "reft_norm_backward: no workspace, or not on 16 bytes");
+            NEED(workspace_bytes >= reft_norm_backward_workspace(rows, cols), REFT_ESIZE, "reft_norm_backward: workspace too small");
+        }
+    }
+    if (!rows) {
+        if (dweight) k_sum_parts<<<(uint32_t)((cols + 63) / 64), 1024, 0, s>>>(nullptr, 0, (uint32_t)cols, dweight);
+        return launched("reft_norm_backward", hipGetLastError());
+    }
+    NEED(dy && h && rstd && weight, REFT_EINVAL, "reft_norm_backward: null pointer");
+    NEED(lies(dy, size_of(dtype)) && lies(dx, size_of(dtype)) && lies(dh, size_of(residual_dtype)) && lies(h, size_of(residual_dtype)) &&
+             lies(dres, size_of(residual_dtype)) && lies(weight, size_of(weight_dtype)) && lies(rstd, 4),
+         REFT_EINVAL, "reft_norm_backward: misaligned pointer");
+    a.dy = dy;
+    a.dh = dh;
+    a.h = h;
+    a.weight = weight;
+    a.rstd = rstd;
+    a.ld_dy = ld_dy;
+    a.ld_dh = ld_dh;
+    a.ld_h = ld_h;
+    a.rows = (uint32_t)rows;
+    a.cols = (uint32_t)cols;
+    a.dres = dres;
+    a.dx = dx;
+    a.ld_dres = ld_dres;
+    a.ld_dx = ld_dx;
+    a.part = !dweight ? nullptr : a.workers > 1 ? (float *)workspace : dweight;
+    a.weight_f32 = weight_dtype == REFT_F32;
+    hipError_t e = by_types<Backward>(a, dtype, residual_dtype, s);
+    if (e == hipSuccess && dweight && a.workers > 1) {
+        k_sum_parts<<<(uint32_t)((cols + 63) / 64), 1024, 0, s>>>((const float *)workspace, a.workers, a.cols, dweight);
+        e = hipGetLastError();
+    }
+    return launched("reft_norm_backward", e);
+}
+
+template <typename T> static hipError_t launch_quantize(const QuantizeArgs &a, bool blocks, hipStream_t s)
+{
+    if (!blocks && !a.q_t) {
+        k_quantize_rows<T><<<dim3((uint32_t)((a.rows + 3) / 4), (uint32_t)((a.cols + 511) / 512)), 256, 0, s>>>(a);
+    } else {
+        const dim3 grid((uint32_t)((a.rows + 127) / 128), (uint32_t)((a.cols + 127) / 128));
+        if (blocks) k_quantize_tile<T, true><<<grid, 256, 0, s>>>(a);
+        else k_quantize_tile<T, false><<<grid, 256, 0, s>>>(a);
+    }
+    return hipGetLastError();
+}
+
+extern "C" int reft_quantize(const void *x, uint64_t ld_x, uint64_t rows, uint64_t cols, int dtype, int format, int blocks, void *q,
+                             uint64_t ld_q, void *scales, uint64_t ld_s, void *q_t, uint64_t ld_qt, void *scales_t,
+                             uint64_t ld_st, reft_stream stream)
+{
+    QuantizeArgs a;
+    NEED(is_float_type(dtype), REFT_EINVAL, "reft_quantize: unknown type %d", dtype);
+    NEED(is_eight(format), REFT_EINVAL, "reft_quantize: unknown 8-bit format %d", format);
+    NEED(q || q_t || !rows || !cols, REFT_EINVAL, "reft_quantize: no output");
+    NEED((!q || scales || !rows || !cols) && (!q_t || scales_t || !rows || !cols), REFT_EINVAL, "reft_quantize: 8 bits without scales");
+    // the grid's second dimension counts blocks of columns
+    NEED(rows <= 0x7fffffff && cols <= 128 * 65535, REFT_ESIZE, "reft_quantize: too many rows or columns");
+    NEED(ld_x >= cols && (!q || ld_q >= cols) && (!q_t || ld_qt >= rows), REFT_ESIZE, "reft_quantize: rows overlap");
+    NEED((!q || ld_s >= (blocks ? (rows + 127) / 128 : rows)) && (!q_t || ld_st >= (blocks ? (cols + 127) / 128 : cols)),
+         REFT_ESIZE, "reft_quantize: words of scales overlap");
+    if (!rows || !cols) return REFT_OK;
+    NEED(x, REFT_EINVAL, "reft_quantize: null pointer");
+    NEED(lies(x, size_of(dtype)), REFT_EINVAL, "reft_quantize: misaligned pointer");
+    a.x = x;
+    a.ld_x = ld_x;
+    a.rows = rows;
+    a.cols = cols;
+    a.q = (uint8_t *)q;
+    a.scales = (uint8_t *)scales;
+    a.q_t = (uint8_t *)q_t;
+    a.scales_t = (uint8_t *)scales_t;
+    a.ld_q = ld_q;
+    a.ld_s = ld_s;
+    a.ld_qt = ld_qt;
+    a.ld_st = ld_st;
+    a.e5m2 = format == REFT_E5M2;
+    hipStream_t s = (hipStream_t)stream;
+    return launched("reft_quantize", dtype == REFT_F32    ? launch_quantize<float>(a, blocks, s)
+                                     : dtype == REFT_BF16 ? launch_quantize<bf16>(a, blocks, s)
+                                                          : launch_quantize<f16>(a, blocks, s));
+}

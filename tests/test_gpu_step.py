@@ -1,0 +1,547 @@
+"""GPU tests of the training step's operators: each against its definition in 64 bits, at the sizes, strides, types and
+values where it can go wrong.  Tolerances come from the formats: U is half a step of fp32 at one, and a sum of n
+terms errs by at most n U of the sum of their magnitudes."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2310_12670_amd as reft
+from oracle import step
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF = {"f32": U, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}          # rounding to the type, of the value
+F8 = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+# rounding to 8 bits: of the value, and half a step of the smallest normal numbers
+HALF8 = {"e4m3": (2.0 ** -4, 2.0 ** -10), "e5m2": (2.0 ** -3, 2.0 ** -17)}
+TINY = 2.0 ** -24                                                  # half a step of f16's smallest numbers, and more
+
+
+@pytest.fixture(scope="module")
+def dev():
+    assert torch.cuda.is_available(), "these tests need the GPU"
+    d = torch.device("cuda:0")
+    torch.cuda.set_device(d)
+    return d
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def padded(dev, rows, cols, dtype, pad=0, lead=0, fill=None):
+    """A [rows, cols] view whose rows lie cols + pad apart, lead elements into its memory; all of it holds `fill`."""
+    size = torch.empty((), dtype=dtype).element_size()
+    raw = torch.full(((lead + rows * (cols + pad) + 64) * size,), 0x5A, dtype=torch.uint8, device=dev)
+    view = raw.view(dtype)[lead:lead + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+    if fill is not None:
+        view.copy_(fill)
+    return raw, view
+
+
+def untouched(raw, view):
+    """Nothing but the view was written."""
+    size = view.element_size()
+    first = (view.data_ptr() - raw.data_ptr()) // size
+    flags = torch.zeros(raw.numel() // size, dtype=torch.bool, device=raw.device)
+    rows, cols, ld = view.shape[0], view.shape[1], view.stride(0)
+    at = first + torch.arange(rows, device=raw.device)[:, None] * ld + torch.arange(cols, device=raw.device)
+    flags[at.reshape(-1)] = True
+    outside = ~flags.repeat_interleave(size)
+    return bool((raw[:outside.numel()][outside] == 0x5A).all())
+
+
+def normal(dev, seed, *shape, std=1.0, dtype=torch.float32):
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(seed)
+    return (torch.randn(*shape, device=dev, generator=gen) * std).to(dtype)
+
+
+def scales_like(dev, rows, cols):
+    return torch.full((-(-cols // 512), rows, 4), 0x5A, dtype=torch.uint8, device=dev)
+
+
+# ------------------------------------------------------------------------------------------------
+# dropout
+# ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 8), (3, 7), (2, 9), (61, 1000), (257, 129), (5, 4099), (1, 70001), (2049, 3)])
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("pad,lead", [(0, 0), (5, 3)])
+def test_dropout(dev, rows, cols, dtype, pad, lead):
+    _, x = padded(dev, rows, cols, DT[dtype], pad, lead, normal(dev, rows + cols, rows, cols))
+    raw, y = padded(dev, rows, cols, DT[dtype], pad + 1, lead)
+    seed, offset = 2 ** 63 + 12345, 2 ** 33 + 7
+    reft.reft_dropout(x, y, 0.3, seed, offset)
+    keep, scale = step.keep_mask(rows, cols, 0.3, seed, offset)
+    kept = torch.from_numpy(keep).to(dev)
+    want = torch.where(kept, x.float() * np.float32(scale), torch.zeros((), device=dev)).to(DT[dtype])
+    assert torch.equal(y, want)
+    assert untouched(raw, y)
+    back = x.clone() if pad == 0 else x                  # in place, and backward on the gradient: the same mask
+    reft.reft_dropout(back, back, 0.3, seed, offset)
+    assert torch.equal(back, want)
+
+
+@pytest.mark.parametrize("p", [0.0, 1e-6, 0.5, 1.0])
+def test_dropout_shares(dev, p):
+    x = normal(dev, 3, 64, 777)
+    y = torch.empty_like(x)
+    reft.reft_dropout(x, y, p, 5, 0)
+    if p == 0 or p == 1e-6:                              # below half of 1 / 65536 nothing is dropped
+        assert torch.equal(y, x)
+    elif p == 1:
+        assert not y.any()
+    else:
+        assert abs(float((y == 0).float().mean()) - p) < 5 * 0.5 / np.sqrt(x.numel())
+
+
+def test_dropout_of_infinities_and_nan(dev):
+    x = normal(dev, 3, 33, 200)
+    x[::2, ::3], x[1::2, ::5] = float("nan"), float("inf")
+    y = torch.empty_like(x)
+    reft.reft_dropout(x, y, 0.4, 9, 1)
+    keep, _ = step.keep_mask(33, 200, 0.4, 9, 1)
+    kept = torch.from_numpy(keep).to(dev)
+    assert not y[~kept].any()
+    assert torch.equal(torch.isnan(y), torch.isnan(x) & kept) and torch.equal(torch.isinf(y), torch.isinf(x) & kept)
+
+
+def test_rows_further_apart_than_32_bits_count(dev):
+    """Three rows of 2^32 bytes and more between them, through every operator that takes strides."""
+    ld, cols = (1 << 31) + 24, 300
+    big = torch.empty(2 * ld + cols, dtype=torch.bfloat16, device=dev)
+    x = torch.as_strided(big, (3, cols), (ld, 1))
+    x.copy_(normal(dev, 8, 3, cols))
+    small = x.contiguous()
+    a, b = torch.empty_like(small), torch.empty_like(small)
+    reft.reft_dropout(x, a, 0.2, 4, 4)
+    reft.reft_dropout(small, b, 0.2, 4, 4)
+    assert torch.equal(a, b)
+    w = normal(dev, 9, cols, dtype=torch.bfloat16)
+    rstd = torch.empty(2, 3, device=dev)
+    reft.reft_norm_forward(x, x, w, 1e-5, y=a, rstd=rstd[0])
+    reft.reft_norm_forward(small, small, w, 1e-5, y=b, rstd=rstd[1])
+    assert torch.equal(a, b)
+    dw = torch.empty(2, cols, device=dev)
+    ws = torch.empty(reft.reft_norm_backward_workspace(3, cols), dtype=torch.uint8, device=dev)
+    reft.reft_norm_backward(x, x, x, rstd[0], w, dres=a, dweight=dw[0], workspace=ws)
+    reft.reft_norm_backward(small, small, small, rstd[0], w, dres=b, dweight=dw[1], workspace=ws)
+    assert torch.equal(a, b) and torch.equal(dw[0], dw[1])
+    q = torch.empty(2, 3, cols, dtype=torch.uint8, device=dev).view(F8["e4m3"])
+    s = torch.empty(2, 1, 3, 4, dtype=torch.uint8, device=dev)
+    far = torch.as_strided(big.view(torch.uint8).view(F8["e4m3"]), (3, cols), (2 * ld, 1))
+    reft.reft_quantize(x, q[0], s[0])
+    reft.reft_quantize(small, q[1], s[1])
+    assert torch.equal(q[0].view(torch.uint8), q[1].view(torch.uint8)) and torch.equal(s[0], s[1])
+    far.view(torch.uint8).copy_(q[0].view(torch.uint8))
+    c = torch.empty(2, 3, 3, device=dev)
+    reft.reft_product(far, s[0], far, s[0], c[0])
+    reft.reft_product(q[0], s[0], q[0], s[0], c[1])
+    assert torch.equal(c[0], c[1]) and c[0].abs().sum() > 0
+
+
+# ------------------------------------------------------------------------------------------------
+# norm
+# ------------------------------------------------------------------------------------------------
+WIDTHS = [1, 7, 128, 513, 1000, 1024, 2047, 2056, 4096, 5120, 8191, 8200, 16384, 16385, 32776, 65536]
+
+
+def near_eight(q, scales, y, y_err, fmt, cols):
+    """q with its scales stands for y: each block's power of two is the smallest that fits (to the error of y), and each value
+    the nearest of the format."""
+    blocks = -(-cols // 128)
+    rows = y.shape[0]
+    e = scales.cpu().numpy().astype(np.int64).transpose(1, 0, 2).reshape(rows, -1)
+    assert (e[:, blocks:] == 127).all()
+    e = e[:, :blocks]
+    for b in range(blocks):
+        at = slice(b * 128, min((b + 1) * 128, cols))
+        most, err = np.abs(y[:, at]).max(1), y_err[:, at].max(1)
+        f = np.exp2(e[:, b] - 127.0)
+        assert (most - err <= step.LARGEST[fmt] * f).all()
+        assert ((most + err > step.LARGEST[fmt] * f / 2) | (e[:, b] == 1)).all()
+        rel, low = HALF8[fmt]
+        t = np.abs(y[:, at]) / f[:, None]
+        assert (np.abs(f64(q)[:, at] - y[:, at] / f[:, None]) <= np.maximum(rel * t, low) + 2 * y_err[:, at] / f[:, None]).all()
+
+
+def check_forward(dev, rows, cols, dtype, residual, weight, p, out, pad=0, lead=0, in_place=False):
+    T, R, W = DT[dtype], DT[residual] if residual else None, DT[weight]
+    _, x = padded(dev, rows, cols, T, pad, lead, normal(dev, cols, rows, cols))
+    res = padded(dev, rows, cols, R, pad, lead, normal(dev, cols + 1, rows, cols, std=2.0))[1] if residual else None
+    w = (1 + normal(dev, cols + 2, cols, std=0.3)).to(W)
+    seed, offset, eps = 2 ** 64 - 3, 2 ** 32 - 1, 1e-5
+    x64, r64 = f64(x), f64(res) if residual else None
+    h64, rstd64, y64 = step.norm_forward(x64, r64, f64(w), eps, p, seed, offset)
+    raw_h, h = (None, res) if in_place else padded(dev, rows, cols, R or T, pad + 2, lead)
+    rstd = torch.empty(rows, device=dev)
+    raw_y, y = padded(dev, rows, cols, T, pad + 1, lead)
+    raw_q, q = padded(dev, rows, cols, F8[out], pad + 3, lead)
+    scales = scales_like(dev, rows, cols)
+    reft.reft_norm_forward(x, res, w, eps, p, seed, offset, h=h, rstd=rstd, y=y, q=q, scales=scales)
+    # h: the factor is rounded to fp32, the product and the sum once each
+    drop = np.abs(step.dropout(x64, p, seed, offset))
+    h_err = U * (3 * drop + 2 * np.abs(h64))
+    kind = residual or dtype
+    assert (np.abs(f64(h) - h64) <= h_err + HALF[kind] * 1.01 * np.abs(h64) + (TINY if kind == "f16" else 0)).all()
+    # the statistics: up to 64 squares a lane, six steps in the wave and 16 waves, half of it through the root; then
+    # mean, addition, root, quotient; and what h brings in
+    n = 64 + 6 + 16
+    rel = (n / 2 + 4) * U + np.sqrt((h_err ** 2).mean(1)) * rstd64
+    assert (np.abs(f64(rstd) - rstd64) <= rel * rstd64).all()
+    y_err = np.abs(y64) * (rel + 3 * U)[:, None] + h_err * np.abs(rstd64[:, None] * f64(w))
+    assert (np.abs(f64(y) - y64) <= y_err + HALF[dtype] * 1.01 * np.abs(y64) + (TINY if dtype == "f16" else 0)).all()
+    near_eight(q, scales, y64, y_err, out, cols)
+    assert untouched(raw_y, y) and untouched(raw_q, q) and (in_place or untouched(raw_h, h))
+    # outputs left out change nothing
+    y2, q2, s2 = torch.empty_like(y), torch.empty(rows, cols, dtype=torch.uint8, device=dev).view(F8[out]), torch.empty_like(scales)
+    if not in_place:
+        reft.reft_norm_forward(x, res, w, eps, p, seed, offset, y=y2)
+        reft.reft_norm_forward(x, res, w, eps, p, seed, offset, q=q2, scales=s2, **({} if residual else dict(rstd=rstd)))
+        assert torch.equal(y2, y) and torch.equal(s2, scales) and torch.equal(q2.view(torch.uint8), q.view(torch.uint8))
+
+
+@pytest.mark.parametrize("cols", WIDTHS)
+@pytest.mark.parametrize("rows", [1, 5])
+def test_norm_forward_widths(dev, rows, cols):
+    check_forward(dev, rows, cols, "bf16", "f32", "bf16", 0.1, "e4m3")
+
+
+@pytest.mark.parametrize("dtype,residual,weight", [("f32", "f32", "f32"), ("bf16", "bf16", "bf16"), ("bf16", "f32", "f32"),
+                                                   ("f16", "f16", "f16"), ("f16", "f32", "f32"), ("bf16", None, "bf16"),
+                                                   ("f32", None, "f32"), ("f16", None, "f32")])
+@pytest.mark.parametrize("rows,cols", [(3, 130), (130, 1100), (2, 4104), (700, 640)])
+@pytest.mark.parametrize("p,out", [(0.0, "e5m2"), (0.25, "e4m3")])
+def test_norm_forward_types(dev, dtype, residual, weight, rows, cols, p, out):
+    check_forward(dev, rows, cols, dtype, residual, weight, p, out, pad=3, lead=1)
+
+
+@pytest.mark.parametrize("cols", [100, 3000, 9000, 20000])
+def test_norm_forward_in_place(dev, cols):
+    check_forward(dev, 7, cols, "bf16", "bf16", "bf16", 0.2, "e4m3", in_place=True)
+    x = normal(dev, 5, 7, cols, dtype=torch.bfloat16)
+    w = normal(dev, 6, cols, dtype=torch.bfloat16)
+    y = torch.empty_like(x)
+    reft.reft_norm_forward(x, None, w, 1e-5, 0.2, 1, 1, y=y)
+    reft.reft_norm_forward(x, None, w, 1e-5, 0.2, 1, 1, y=x)
+    assert torch.equal(x, y)
+
+
+def test_norm_forward_of_zeros_infinities_and_nan(dev):
+    x = normal(dev, 5, 6, 700)
+    x[0] = 0
+    x[1, 300], x[2, 300] = float("inf"), float("nan")
+    x[3], x[4] = 1e30, 1e-30                             # squares beyond fp32's range, and below it
+    w = torch.ones(700, device=dev)
+    y, rstd = torch.empty_like(x), torch.empty(6, device=dev)
+    q, s = torch.empty(6, 700, dtype=torch.uint8, device=dev).view(F8["e4m3"]), scales_like(dev, 6, 700)
+    reft.reft_norm_forward(x, None, w, 1e-6, y=y, rstd=rstd, q=q, scales=s)
+    assert not y[0].any() and (s[0, 0] == 1).all() and not q.float()[0].any()
+    assert torch.isnan(y[1, 300]) and not y[1, :300].any() and torch.isnan(y[2]).all()
+    assert torch.isnan(q.float()[2]).all() and (s[0, 2] == 255).all() and s[1, 2].tolist() == [255, 255, 127, 127]
+    # one value of a block is no number: all of that block, and no other
+    assert torch.isnan(q.float()[1, 256:384]).all() and not torch.isnan(q.float()[1, :256]).any()
+    assert s[0, 1].tolist() == [1, 1, 255, 1]
+    assert rstd[3] == 0 and not y[3].any()
+    assert torch.allclose(y[4], x[4] * 1e3, rtol=1e-6) and torch.isfinite(y[5]).all()
+
+
+def check_backward(dev, rows, cols, dtype, residual, weight, p, pad=0, lead=0, with_dh=True):
+    T, R, W = DT[dtype], DT[residual], DT[weight]
+    _, dy = padded(dev, rows, cols, T, pad, lead, normal(dev, cols, rows, cols))
+    dh = padded(dev, rows, cols, R, pad, lead, normal(dev, cols + 1, rows, cols))[1] if with_dh else None
+    _, h = padded(dev, rows, cols, R, pad + 1, lead, normal(dev, cols + 2, rows, cols, std=2.0))
+    w = (1 + normal(dev, cols + 3, cols, std=0.3)).to(W)
+    rstd = torch.rsqrt(h.float().square().mean(1) + 1e-5)
+    seed, offset = 99, 2 ** 63 + 1
+    want = step.norm_backward(f64(dy), f64(dh) if with_dh else None, f64(h), f64(rstd), f64(w), p, seed, offset)
+    raw_r, dres = padded(dev, rows, cols, R, pad + 2, lead)
+    raw_x, dx = padded(dev, rows, cols, T, pad, lead)
+    dw = torch.empty(cols, device=dev)
+    ws = torch.empty(reft.reft_norm_backward_workspace(rows, cols), dtype=torch.uint8, device=dev)
+    reft.reft_norm_backward(dy, dh, h, rstd, w, p, seed, offset, dres=dres, dx=dx, dweight=dw, workspace=ws)
+    xhat, g = f64(h) * f64(rstd)[:, None], f64(dy) * f64(w)
+    # the mean: products of three rounded factors, up to 64 a lane, then wave and waves
+    dot_err = (64 + 6 + 16 + 6) * U * np.abs(g * xhat).mean(1, keepdims=True)
+    dot = (g * xhat).mean(1, keepdims=True)
+    err = f64(rstd)[:, None] * (4 * U * np.abs(g) + np.abs(xhat) * (dot_err + 4 * U * np.abs(dot))) + 2 * U * np.abs(want[0])
+    if with_dh:
+        err = err + U * np.abs(f64(dh))
+    assert (np.abs(f64(dres) - want[0]) <= err + HALF[residual] * 1.01 * np.abs(want[0]) + (TINY if residual == "f16" else 0)).all()
+    factor = 65536 / (65536 - round(p * 65536))
+    assert (np.abs(f64(dx) - want[1]) <= err * factor + (HALF[dtype] * 1.01 + 2 * U) * np.abs(want[1]) + (TINY if dtype == "f16" else 0)).all()
+    assert ((f64(dx) == 0) >= (want[1] == 0)).all()
+    assert (np.abs(f64(dw) - want[2]) <= (rows + 4) * U * np.abs(f64(dy) * xhat).sum(0)).all()
+    assert untouched(raw_r, dres) and untouched(raw_x, dx)
+    # each output alone, and in the place of what it is the gradient of
+    alone = torch.empty(cols, device=dev)
+    reft.reft_norm_backward(dy, dh, h, rstd, w, p, seed, offset, dweight=alone, workspace=ws)
+    assert torch.equal(alone, dw)
+    kept_dres, kept_dx = dres.clone(), dx.clone()
+    dx.zero_()
+    reft.reft_norm_backward(dy, dh, h, rstd, w, p, seed, offset, dx=dx)
+    assert torch.equal(dx, kept_dx)
+    reft.reft_norm_backward(dy, dh, h, rstd, w, p, seed, offset, dres=dh if with_dh else dres, dx=dy, dweight=alone, workspace=ws)
+    assert torch.equal(dy, kept_dx) and torch.equal(alone, dw) and torch.equal(dh if with_dh else dres, kept_dres)
+
+
+@pytest.mark.parametrize("cols", WIDTHS)
+@pytest.mark.parametrize("rows", [1, 6])
+def test_norm_backward_widths(dev, rows, cols):
+    check_backward(dev, rows, cols, "bf16", "bf16", "bf16", 0.1)
+
+
+@pytest.mark.parametrize("dtype,residual,weight", [("f32", "f32", "f32"), ("bf16", "bf16", "f32"), ("bf16", "f32", "bf16"),
+                                                   ("f16", "f16", "f16"), ("f16", "f32", "f32")])
+@pytest.mark.parametrize("rows,cols", [(3, 130), (130, 1100), (1500, 264), (2, 4104), (2111, 40)])
+@pytest.mark.parametrize("p,with_dh", [(0.0, True), (0.25, False)])
+def test_norm_backward_types(dev, dtype, residual, weight, rows, cols, p, with_dh):
+    check_backward(dev, rows, cols, dtype, residual, weight, p, pad=3, lead=1, with_dh=with_dh)
+
+
+def test_norm_gradient_against_differences(dev):
+    """The slope of sum(y g) along random directions, from the forward kernel itself, in fp32."""
+    rows, cols, eps, p = 4, 96, 1e-5, 0.25
+    x, res = normal(dev, 1, rows, cols), normal(dev, 2, rows, cols)
+    w, g = 1 + normal(dev, 3, cols, std=0.2), normal(dev, 4, rows, cols)
+
+    def y_of(x, res, w):
+        y = torch.empty_like(x)
+        reft.reft_norm_forward(x, res, w, eps, p, 7, 8, y=y)
+        return f64(y)
+
+    h, rstd = torch.empty_like(x), torch.empty(rows, device=dev)
+    reft.reft_norm_forward(x, res, w, eps, p, 7, 8, h=h, rstd=rstd)
+    dres, dx, dw = torch.empty_like(x), torch.empty_like(x), torch.empty(cols, device=dev)
+    ws = torch.empty(reft.reft_norm_backward_workspace(rows, cols), dtype=torch.uint8, device=dev)
+    reft.reft_norm_backward(g, None, h, rstd, w, p, 7, 8, dres=dres, dx=dx, dweight=dw, workspace=ws)
+    t = 2.0 ** -7
+    for at, grad in enumerate((dx, dres, dw)):
+        for k in range(4):
+            to = normal(dev, 50 + 10 * at + k, *grad.shape)
+            to /= to.norm()
+            ends = []
+            for sign in (t, -t):
+                args = [x, res, w]
+                args[at] = args[at] + sign * to
+                ends.append((y_of(*args) * f64(g)).sum())
+            slope, want = (ends[0] - ends[1]) / (2 * t), (f64(grad) * f64(to)).sum()
+            # the forward's rounding over 2 t: 384 values of order one, sqrt(384) * 4 U / (2 t) < 4e-4, three times that; the
+            # cubic term, t^2 times a third derivative of order |g| = 20, over 6: 2e-4
+            assert abs(slope - want) <= 1.5e-3
+
+
+def test_norm_backward_without_rows(dev):
+    empty = torch.empty(0, 40, device=dev)
+    dw = torch.full((40,), 3.0, device=dev)
+    reft.reft_norm_backward(empty, None, empty, torch.empty(0, device=dev), torch.ones(40, device=dev), dweight=dw)
+    assert not dw.any()
+
+
+# ------------------------------------------------------------------------------------------------
+# quantization
+# ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 512), (5, 127), (3, 130), (128, 128), (129, 257), (300, 1000), (17, 1537), (1000, 24)])
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("blocks", [False, True])
+@pytest.mark.parametrize("fmt,which", [("e4m3", "both"), ("e5m2", "q"), ("e4m3", "t"), ("e4m3", "q")])
+def test_quantize(dev, rows, cols, dtype, blocks, fmt, which):
+    value = normal(dev, rows * cols, rows, cols) * torch.exp2(normal(dev, 2, rows, 1) * 4)
+    if rows * cols > 200:
+        value[:, :60] = 0
+        value[rows // 2, cols - 1] = 2.0 ** -120 if dtype != "f16" else 2.0 ** -24
+    _, x = padded(dev, rows, cols, DT[dtype], 3, 1, value)
+    raw_q, q = padded(dev, rows, cols, F8[fmt], 5, 1)
+    raw_t, q_t = padded(dev, cols, rows, F8[fmt], 2, 3)
+    s = scales_like(dev, -(-rows // 128) if blocks else rows, cols)
+    s_t = scales_like(dev, -(-cols // 128) if blocks else cols, rows)
+    kw = {}
+    if which != "t":
+        kw.update(q=q, scales=s)
+    if which != "q":
+        kw.update(q_t=q_t, scales_t=s_t)
+    reft.reft_quantize(x, **kw, blocks=blocks)
+    for got, scales, value in ((q, s, f64(x)), (q_t, s_t, f64(x).T)):
+        if (got is q) == (which == "t") and which != "both":
+            continue
+        want, e = step.quantize(np.ascontiguousarray(value), fmt, blocks)
+        assert np.array_equal(scales.cpu().numpy(), step.words_of(e))
+        assert np.array_equal(f64(got.float()), want)
+    assert untouched(raw_q, q) and untouched(raw_t, q_t)
+
+
+@pytest.mark.parametrize("blocks", [False, True])
+@pytest.mark.parametrize("both", [False, True])
+def test_quantize_infinities_and_nan(dev, blocks, both):
+    x = normal(dev, 1, 260, 700)
+    x[3, 5], x[130, 300], x[259, 699] = float("inf"), float("nan"), float("-inf")
+    x[128:256, 512:640] = 0
+    x[200, 0] = 3.0e38
+    q = torch.empty(260, 700, dtype=torch.uint8, device=dev).view(F8["e4m3"])
+    s = scales_like(dev, 3 if blocks else 260, 700)
+    kw = {}
+    if both:
+        kw = dict(q_t=torch.empty(700, 260, dtype=torch.uint8, device=dev).view(F8["e4m3"]), scales_t=scales_like(dev, 6 if blocks else 700, 260))
+    reft.reft_quantize(x, q, s, **kw, blocks=blocks)
+    pairs = [(q, s, f64(x))] + ([(kw["q_t"], kw["scales_t"], f64(x).T)] if both else [])
+    for got, scales, value in pairs:
+        want, e = step.quantize(np.ascontiguousarray(value), "e4m3", blocks)
+        assert np.array_equal(scales.cpu().numpy(), step.words_of(e))
+        assert np.array_equal(f64(got.float()), want, equal_nan=True)
+
+
+# ------------------------------------------------------------------------------------------------
+# product
+# ------------------------------------------------------------------------------------------------
+SIZES = [(1, 1, 1), (1, 16, 128), (1, 300, 4096), (2, 33, 1000), (7, 129, 513), (16, 256, 384), (17, 1000, 640), (33, 48, 72),
+         (64, 512, 2048), (65, 130, 1537), (100, 260, 31), (128, 128, 128), (129, 255, 257), (256, 256, 512), (300, 700, 896),
+         (511, 513, 1025), (1024, 512, 768), (2000, 40, 160), (40, 2000, 160), (512, 1024, 3200)]
+
+
+def whole_numbers(dev, seed, rows, cols, fmt, pad, lead):
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(seed)
+    v = torch.randint(-2, 3, (rows, cols), device=dev, generator=gen).float()
+    raw, q = padded(dev, rows, cols, F8[fmt], pad, lead)
+    raw.fill_(0x7F)                                      # what lies between the rows is no number
+    q.copy_(v.to(F8[fmt]))
+    return q, v
+
+
+def powers(dev, seed, rows, cols, low, high):
+    """Scales whose bytes behind the last block are no numbers: they are not used."""
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(seed)
+    s = torch.randint(low + 127, high + 128, (-(-cols // 512), rows, 4), device=dev, generator=gen, dtype=torch.uint8)
+    flat = s.transpose(0, 1).reshape(rows, -1).clone()
+    flat[:, -(-cols // 128):] = 255
+    return flat.view(rows, -1, 4).transpose(0, 1).contiguous()
+
+
+@pytest.mark.parametrize("M,N,K", SIZES)
+@pytest.mark.parametrize("blocks", [False, True])
+@pytest.mark.parametrize("out", list(DT))
+@pytest.mark.parametrize("fa,fb,pad,lead", [("e4m3", "e4m3", None, 0), ("e5m2", "e4m3", 1, 3), ("e4m3", "e5m2", None, 0), ("e5m2", "e5m2", None, 16)])
+def test_product_of_whole_numbers(dev, M, N, K, blocks, out, fa, fb, pad, lead):
+    """Values of -2 .. 2 with scales of 1/2, 1 and 2 for each side: every partial sum is a multiple of 1/4 below 2^24, so the
+    result is exact, whatever the order.  pad None: rows begin at multiples of 16 bytes."""
+    pad = -K % 16 if pad is None else pad
+    a, va = whole_numbers(dev, M + K, M, K, fa, pad, lead)
+    b, vb = whole_numbers(dev, N + 2 * K, N, K, fb, pad, lead)
+    tall = -(-N // 128) if blocks else N
+    sa, sb = powers(dev, 1, M, K, -1, 1), powers(dev, 2, tall, K, -1, 1)
+    raw, c = padded(dev, M, N, DT[out], 3, 1)
+    ws = torch.empty(reft.reft_product_workspace(M, N, K), dtype=torch.uint8, device=dev)
+    reft.reft_product(a, sa, b, sb, c, ws, b_blocks=blocks)
+    want = step.product(f64(va), sa.cpu().numpy(), f64(vb), sb.cpu().numpy(), blocks)
+    assert torch.equal(c, torch.from_numpy(want).to(dev).float().to(DT[out]))
+    assert untouched(raw, c)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 272, 4096), (5, 700, 1000), (60, 520, 2000), (130, 300, 4097), (700, 520, 1600)])
+@pytest.mark.parametrize("blocks", [False, True])
+@pytest.mark.parametrize("out,limit", [("f32", 1e-6), ("bf16", 2.0 ** -9), ("f16", 2.0 ** -11)])
+def test_product_of_random_numbers(dev, M, N, K, blocks, out, limit):
+    """The norm of the result's error: a step of 2^-7 (bf16) or 2^-10 (f16), of values from 1 to 2 times a power of two, errs by
+    its twelfth part's root over about 1.5, 1.5e-3 and 1.9e-4; a sum in fp32 by U times the root of its 16 to 256 steps."""
+    a32, b32 = normal(dev, 1, M, K) * torch.exp2(normal(dev, 2, M, 1) * 2), normal(dev, 3, N, K, std=0.02)
+    a, b = (torch.empty(n, K + (-K % 16), dtype=torch.uint8, device=dev).view(F8["e4m3"])[:, :K] for n in (M, N))
+    sa, sb = scales_like(dev, M, K), scales_like(dev, -(-N // 128) if blocks else N, K)
+    reft.reft_quantize(a32, a, sa)
+    reft.reft_quantize(b32, b, sb, blocks=blocks)
+    c = torch.empty(M, N, dtype=DT[out], device=dev)
+    ws = torch.empty(reft.reft_product_workspace(M, N, K), dtype=torch.uint8, device=dev)
+    reft.reft_product(a, sa, b, sb, c, ws, b_blocks=blocks)
+    want = step.product(f64(a.float()), sa.cpu().numpy(), f64(b.float()), sb.cpu().numpy(), blocks)
+    assert np.linalg.norm(f64(c) - want) <= limit * np.linalg.norm(want)
+    again = torch.empty_like(c)
+    for _ in range(3):                                   # the same bits each time
+        reft.reft_product(a, sa, b, sb, again, ws, b_blocks=blocks)
+        assert torch.equal(again, c)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [3, 40, 200])
+def test_product_with_scales_that_are_no_numbers(dev, M, out):
+    a, va = whole_numbers(dev, 1, M, 300, "e4m3", 4, 0)
+    b, vb = whole_numbers(dev, 2, 200, 300, "e4m3", 4, 0)
+    sa, sb = torch.full((1, M, 4), 127, dtype=torch.uint8, device=dev), torch.full((1, 2, 4), 127, dtype=torch.uint8, device=dev)
+    sa[0, 1, 2], sb[0, 1, 0] = 255, 255
+    sa[0, 2, 0] = 0                                      # 2^-127: nothing beside the other blocks' values, but no error
+    c = torch.empty(M, 200, dtype=DT[out], device=dev)
+    reft.reft_product(a, sa, b, sb, c, torch.empty(reft.reft_product_workspace(M, 200, 300), dtype=torch.uint8, device=dev), b_blocks=True)
+    bad = torch.zeros(M, 200, dtype=torch.bool, device=dev)
+    bad[1], bad[:, 128:] = True, True
+    assert torch.equal(torch.isnan(c), bad)
+    want = (va[2, 128:].double() @ vb[:128, 128:].double().t()).to(DT[out])
+    assert torch.equal(c[2, :128], want)
+
+
+def test_product_of_nothing(dev):
+    e = lambda *s: torch.empty(*s, dtype=torch.uint8, device=dev)                        # noqa: E731
+    c = torch.full((5, 7), 3.0, device=dev)
+    reft.reft_product(e(5, 0).view(F8["e4m3"]), e(0, 5, 4), e(7, 0).view(F8["e4m3"]), e(0, 7, 4), c)
+    assert not c.any()
+    reft.reft_product(e(0, 16).view(F8["e4m3"]), e(1, 0, 4), e(7, 16).view(F8["e4m3"]), e(1, 7, 4), torch.empty(0, 7, device=dev))
+    reft.reft_quantize(torch.empty(0, 5, device=dev), e(0, 5).view(F8["e4m3"]), e(1, 0, 4))
+    reft.reft_dropout(torch.empty(0, 5, device=dev), torch.empty(0, 5, device=dev), 0.5, 1)
+    torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------------------------------------
+# streams and graphs
+# ------------------------------------------------------------------------------------------------
+def chain(dev, s, stream=None):
+    reft.reft_norm_forward(s["x"], s["res"], s["w"], 1e-5, 0.1, 3, 4, h=s["h"], rstd=s["rstd"], q=s["q"], scales=s["s"], stream=stream)
+    reft.reft_product(s["q"], s["s"], s["wq"], s["ws"], s["c"], s["scratch"], b_blocks=True, stream=stream)
+    reft.reft_dropout(s["c"], s["c2"], 0.1, 3, 5, stream=stream)
+    reft.reft_norm_backward(s["c3"], None, s["h"], s["rstd"], s["w"], 0.1, 3, 4, dres=s["dres"], dweight=s["dw"], workspace=s["scratch2"],
+                            stream=stream)
+    return [s[k] for k in ("h", "rstd", "c", "c2", "dres", "dw")]
+
+
+def chain_state(dev, rows=200, cols=1000, wide=600):
+    s = dict(x=normal(dev, 1, rows, cols, dtype=torch.bfloat16), res=normal(dev, 2, rows, cols, dtype=torch.bfloat16),
+             w=1 + normal(dev, 3, cols, std=0.1, dtype=torch.bfloat16), c3=normal(dev, 4, rows, cols, dtype=torch.bfloat16))
+    s.update(h=torch.empty_like(s["x"]), rstd=torch.empty(rows, device=dev), dres=torch.empty_like(s["x"]), dw=torch.empty(cols, device=dev),
+             q=torch.empty(rows, 1008, dtype=torch.uint8, device=dev).view(F8["e4m3"])[:, :cols], s=scales_like(dev, rows, cols),
+             wq=torch.empty(wide, 1008, dtype=torch.uint8, device=dev).view(F8["e4m3"])[:, :cols], ws=scales_like(dev, 5, cols),
+             c=torch.empty(rows, wide, dtype=torch.bfloat16, device=dev), c2=torch.empty(rows, wide, dtype=torch.bfloat16, device=dev),
+             scratch=torch.empty(reft.reft_product_workspace(rows, wide, cols), dtype=torch.uint8, device=dev),
+             scratch2=torch.empty(reft.reft_norm_backward_workspace(rows, cols), dtype=torch.uint8, device=dev))
+    reft.reft_quantize(normal(dev, 5, wide, cols, std=0.03, dtype=torch.bfloat16), s["wq"], s["ws"], blocks=True)
+    torch.cuda.synchronize()
+    return s
+
+
+def test_on_another_stream(dev):
+    s = chain_state(dev)
+    want = [t.clone() for t in chain(dev, s)]
+    torch.cuda.synchronize()
+    for t in ("h", "rstd", "c", "c2", "dres", "dw"):
+        s[t].zero_()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = chain(dev, s, side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_in_a_graph(dev):
+    s = chain_state(dev)
+    want = [t.clone() for t in chain(dev, s)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        got = chain(dev, s, side)
+    for _ in range(4):
+        for t in got:
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        normal(dev, 1, 1000, 1000).sum().item()          # the program's own work between the replays
