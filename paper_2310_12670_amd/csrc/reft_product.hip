@@ -20,16 +20,18 @@ struct ProductArgs {
 
 // ---- tiles in LDS -----------------------------------------------------------------------------------------
 // A row of a tile is 128 values of K: eight chunks of 16 bytes.  Chunk c of row r lies at place c ^ turn(r), so that
-// neither 8 nor 16 rows that are read at one chunk meet in a bank.
-__device__ __forceinline__ int turn(int r) { return (r ^ (r >> 3)) & 7; }
+// neither 8 nor 16 rows that are read at one chunk meet in a bank.  Rows 16 apart are turned alike: their addresses differ by a
+// constant.
+__device__ __forceinline__ int turn(int r) { return (r ^ (r >> 3 & 1)) & 7; }
 __device__ __forceinline__ int place(int r, int c) { return r * 128 + ((c ^ turn(r)) << 4); }
 
-// A lane's operand of a product of 32 x 32 x 64: row lane % 32, 32 values of half s of the row's 128.  Which of a half's
-// 64 values a lane takes is the same for both operands, and the scale is the same for all.
+// A lane's operand of a product of 32 x 32 x 64: row lane % 32 of those from `row` (a multiple of 32) on, 32 values of
+// half s of the row's 128.  Which of a half's 64 values a lane takes is the same for both operands, and the scale is the same for all.
 __device__ __forceinline__ i32x8 operand(const uint8_t *tile, int row, int s, int lane)
 {
     const int c = s * 4 + (lane >> 5) * 2;
-    const w32x4 lo = *(const w32x4 *)(tile + place(row, c)), hi = *(const w32x4 *)(tile + place(row, c + 1));
+    tile += row * 128;
+    const w32x4 lo = *(const w32x4 *)(tile + place(lane & 31, c)), hi = *(const w32x4 *)(tile + place(lane & 31, c + 1));
     i32x8 v;
     v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w;
     v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
@@ -174,8 +176,8 @@ template <int FA, int FB, bool EXACT> __global__ __launch_bounds__(256) void k_p
             Operand<FB, EXACT> b[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                a[i].take(operand(tile[half][0], wm + i * 32 + (lane & 31), s, lane), sa[i]);
-                b[i].take(operand(tile[half][1], wn + i * 32 + (lane & 31), s, lane), sb[i]);
+                a[i].take(operand(tile[half][0], wm + i * 32, s, lane), sa[i]);
+                b[i].take(operand(tile[half][1], wn + i * 32, s, lane), sb[i]);
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -196,8 +198,226 @@ template <int FA, int FB, bool EXACT> __global__ __launch_bounds__(256) void k_p
             store_tile(p, m0 + wm + i * 32 + (lane & 31), n0 + wn + j * 32, lane, acc[i][j]);
 }
 
+// ---- rows on 16 bytes: two tiles of each operand in LDS, filled by the memory system ------------------------------
+// Four waves of MT x NT products of 32 x 32, two by two.
+constexpr int kGroup = 8;              // rows of tiles that are walked together, so that what runs at once shares operands
+
+// 16 bytes a lane from base + offset to LDS, those of a wave one after the other.  An offset of 32 bits from a base that the
+// wave shares takes half the registers of addresses.
+struct Base {
+    __amdgpu_buffer_rsrc_t r;
+    __device__ __forceinline__ Base(const uint8_t *p) : r(__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, -1, 0x00027000)) {}
+};
+__device__ __forceinline__ void copy_to_lds(const Base &from, uint32_t offset, uint8_t *to)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from.r, (__attribute__((address_space(3))) void *)to, 16, (int)offset, 0, 0, 0);
+}
+
+// All waves' copies so far have arrived and all have read what they asked for.
+__device__ __forceinline__ void meet()
+{
+    __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0)
+    __syncthreads();
+}
+
+// Which tile a workgroup takes.  Workgroups are dealt to the eight dies in turn, and each die has an L2 of its own: a die gets
+// tiles that follow each other.
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t &m, uint32_t &n)
+{
+    const uint32_t total = tiles_m * tiles_n, each = total / 8, more = total % 8, die = id % 8;
+    const uint32_t t = die * each + min(die, more) + id / 8;
+    const uint32_t band = kGroup * tiles_n, first = t / band * kGroup, high = min(tiles_m - first, (uint32_t)kGroup);
+    m = first + t % band % high;
+    n = t % band / high;
+}
+
+// The order of half a step's instructions: a product, then a few reads and copies that do not depend on it, and so on; the
+// reads are done early, so that the wait for them at the half's end is none.
+template <int PRODUCTS, int READS, int COPIES> __device__ __forceinline__ void interleave()
+{
+    constexpr int kReads = (READS * 4 + PRODUCTS * 3 - 1) / (PRODUCTS * 3), kCopies = (COPIES + PRODUCTS - 1) / PRODUCTS;
+#pragma unroll
+    for (int i = 0; i < PRODUCTS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (i * kReads < READS) __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+        if (i * kCopies < COPIES) __builtin_amdgcn_sched_group_barrier(0x010, kCopies, 0);
+    }
+}
+
+template <int FA, int FB, bool EXACT, int MT, int NT>
+__global__ __launch_bounds__(256, MT * NT >= 16 ? 1 : 2) void k_product(ProductArgs p)
+{
+    constexpr int kRowsA = 64 * MT, kRowsB = 64 * NT, kCopiesA = 2 * MT, kCopiesB = 2 * NT;
+    // variables of their own, so that the compiler knows which copies a read has to wait for
+    __shared__ __align__(16) uint8_t ta0[kRowsA * 128], ta1[kRowsA * 128], tb0[kRowsB * 128], tb1[kRowsB * 128];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    uint32_t tm, tn;
+    tile_of(blockIdx.x, (p.M + kRowsA - 1) / kRowsA, (p.N + kRowsB - 1) / kRowsB, tm, tn);
+    const uint32_t m0 = tm * kRowsA, n0 = tn * kRowsB;
+    const int wm = (wave & 1) * 32 * MT, wn = (wave >> 1) * 32 * NT;
+    const uint32_t steps = (p.K + 127) / 128;
+    // A wave's copy fills eight rows of a tile: lane i the place i % 8 of row i / 8.  Rows behind the matrix's last repeat that.
+    const uint8_t *base_a = p.a + (uint64_t)m0 * p.ld_a, *base_b = p.b + (uint64_t)n0 * p.ld_b;
+    uint32_t from_a[kCopiesA], from_b[kCopiesB];
+    auto chunk = [&](int i) { return ((lane & 7) ^ turn(i * 8 + (lane >> 3))) * 16; };
+#pragma unroll
+    for (int i = 0; i < kCopiesA; ++i)
+        from_a[i] = min((uint32_t)((wave * kCopiesA + i) * 8 + (lane >> 3)), p.M - 1 - m0) * (uint32_t)p.ld_a + chunk(i);
+#pragma unroll
+    for (int i = 0; i < kCopiesB; ++i)
+        from_b[i] = min((uint32_t)((wave * kCopiesB + i) * 8 + (lane >> 3)), p.N - 1 - n0) * (uint32_t)p.ld_b + chunk(i);
+    auto fill = [&](uint32_t step, uint8_t *ta, uint8_t *tb) {
+        const Base a(base_a + (uint64_t)step * 128), b(base_b + (uint64_t)step * 128);
+#pragma unroll
+        for (int i = 0; i < kCopiesA; ++i) copy_to_lds(a, from_a[i], ta + (wave * kCopiesA + i) * 1024);
+#pragma unroll
+        for (int i = 0; i < kCopiesB; ++i) copy_to_lds(b, from_b[i], tb + (wave * kCopiesB + i) * 1024);
+    };
+    // The last step may end inside the tile: chunks that begin behind K are read from the row's first one instead (a chunk
+    // lies on 16 bytes, so one that holds a value of the row is memory of the row's), and clear() zeroes all behind K.
+    const uint32_t tail = p.K - (steps - 1) * 128;
+    auto fill_last = [&](uint32_t step, uint8_t *ta, uint8_t *tb) {
+        const Base a(base_a + (uint64_t)step * 128), b(base_b + (uint64_t)step * 128);
+#pragma unroll
+        for (int i = 0; i < kCopiesA; ++i)
+            copy_to_lds(a, from_a[i] - ((uint32_t)chunk(i) < tail ? 0 : chunk(i)), ta + (wave * kCopiesA + i) * 1024);
+#pragma unroll
+        for (int i = 0; i < kCopiesB; ++i)
+            copy_to_lds(b, from_b[i] - ((uint32_t)chunk(i) < tail ? 0 : chunk(i)), tb + (wave * kCopiesB + i) * 1024);
+    };
+    auto clear = [&](uint8_t *ta, uint8_t *tb) {
+        for (int r = tid; r < kRowsA + kRowsB; r += 256) {
+            uint8_t *t = r < kRowsA ? ta : tb;
+            const int row = r < kRowsA ? r : r - kRowsA;
+            int k = (int)tail;
+            for (; k % 16; ++k) t[place(row, k / 16) + k % 16] = 0;
+            for (; k < 128; k += 16) *(w32x4 *)(t + place(row, k / 16)) = w32x4{0, 0, 0, 0};
+        }
+    };
+    auto read = [&](i32x8 (&a)[MT], i32x8 (&b)[NT], const uint8_t *ta, const uint8_t *tb, int s) {
+        a[0] = operand(ta, wm, s, lane);                     // in the order of their use
+#pragma unroll
+        for (int i = 0; i < NT; ++i) b[i] = operand(tb, wn + i * 32, s, lane);
+#pragma unroll
+        for (int i = 1; i < MT; ++i) a[i] = operand(ta, wm + i * 32, s, lane);
+    };
+    f32x16 acc[MT][NT] = {};
+    auto multiply_all = [&](const i32x8 (&ra)[MT], const i32x8 (&rb)[NT], const uint32_t (&sa)[MT], const uint32_t (&sb)[NT]) {
+        Operand<FA, EXACT> a[MT];
+        Operand<FB, EXACT> b[NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) a[i].take(ra[i], sa[i]);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) b[i].take(rb[i], sb[i]);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = multiply<FA, FB>(b[j], a[i], acc[i][j]);
+    };
+    const uint32_t last_word = (steps - 1) / 4;
+    auto words = [&](uint32_t w, uint32_t (&sa)[MT], uint32_t (&sb)[NT]) {
+        w = min(w, last_word);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) sa[i] = (p.sa + w * p.ld_sa)[min(m0 + wm + i * 32 + (lane & 31), p.M - 1)];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) sb[i] = (p.sb + w * p.ld_sb)[min(n0 + wn + i * 32 + (lane & 31), p.N - 1) >> p.b_shift];
+    };
+    auto shifted = [&](uint32_t (&sa)[MT], uint32_t (&sb)[NT]) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) sa[i] >>= 8;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) sb[i] >>= 8;
+    };
+    auto any_fill = [&](uint32_t step, uint8_t *ta, uint8_t *tb) {
+        if (step + 1 < steps) fill(step, ta, tb);
+        else if (step + 1 == steps) fill_last(step, ta, tb);
+    };
+
+    i32x8 a0[MT], b0[NT], a1[MT], b1[NT];
+    uint32_t sa[MT], sb[NT], next_sa[MT], next_sb[NT];
+    words(0, sa, sb);
+    any_fill(0, ta0, tb0);
+    any_fill(1, ta1, tb1);
+    meet();
+    if (steps == 1 && tail < 128) {
+        clear(ta0, tb0);
+        meet();
+    }
+    read(a0, b0, ta0, tb0, 0);
+    uint32_t step = 0;
+    // Half a step multiplies what half a step ago was read from LDS, while the next half is read; between a step's halves its tile
+    // has been read by all and the next one's has arrived, so that the one after next may be fetched into its place: it has
+    // a whole step's time.
+    for (; step + 6 < steps; step += 4) {
+        words(step / 4 + 1, next_sa, next_sb);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint8_t *ta = j % 2 ? ta1 : ta0, *tb = j % 2 ? tb1 : tb0, *oa = j % 2 ? ta0 : ta1, *ob = j % 2 ? tb0 : tb1;
+            read(a1, b1, ta, tb, 1);
+            multiply_all(a0, b0, sa, sb);
+            interleave<MT * NT * (EXACT ? 4 : 1), 2 * (MT + NT), 0>();
+            __builtin_amdgcn_sched_barrier(0);
+            meet();
+            __builtin_amdgcn_sched_barrier(0);
+            fill(step + j + 2, ta, tb);
+            read(a0, b0, oa, ob, 0);
+            multiply_all(a1, b1, sa, sb);
+            interleave<MT * NT * (EXACT ? 4 : 1), 2 * (MT + NT), 2 * (MT + NT)>();
+            __builtin_amdgcn_sched_barrier(0);
+            shifted(sa, sb);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) sa[i] = next_sa[i];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) sb[i] = next_sb[i];
+    }
+    words(step / 4 + 1, next_sa, next_sb);
+#pragma unroll
+    for (int j = 0; j < 6; ++j) {
+        if (step + j >= steps) break;
+        uint8_t *ta = j % 2 ? ta1 : ta0, *tb = j % 2 ? tb1 : tb0, *oa = j % 2 ? ta0 : ta1, *ob = j % 2 ? tb0 : tb1;
+        read(a1, b1, ta, tb, 1);
+        multiply_all(a0, b0, sa, sb);
+        meet();
+        any_fill(step + j + 2, ta, tb);
+        if (step + j + 2 == steps && tail < 128) {
+            clear(oa, ob);
+            meet();
+        }
+        if (step + j + 1 < steps) read(a0, b0, oa, ob, 0);
+        multiply_all(a1, b1, sa, sb);
+        shifted(sa, sb);
+        if (j == 3) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i) sa[i] = next_sa[i];
+#pragma unroll
+            for (int i = 0; i < NT; ++i) sb[i] = next_sb[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            store_tile(p, m0 + wm + i * 32 + (lane & 31), n0 + wn + j * 32, lane, acc[i][j]);
+}
+
+template <int FA, int FB, int MT, int NT> static hipError_t launch_tiles(const ProductArgs &p, hipStream_t s)
+{
+    const uint64_t tiles = (uint64_t)((p.M + 64 * MT - 1) / (64 * MT)) * ((p.N + 64 * NT - 1) / (64 * NT));
+    if (p.c_type == REFT_F32) k_product<FA, FB, true, MT, NT><<<(uint32_t)tiles, 256, 0, s>>>(p);
+    else k_product<FA, FB, false, MT, NT><<<(uint32_t)tiles, 256, 0, s>>>(p);
+    return hipGetLastError();
+}
+
 template <int FA, int FB> static hipError_t launch_product(const ProductArgs &p, hipStream_t s)
 {
+    const bool on16 = ((uintptr_t)p.a | (uintptr_t)p.b | p.ld_a | p.ld_b) % 16 == 0;
+    // offsets inside a tile are held in 32 bits
+    if (on16 && p.K && p.ld_a < (1u << 23) && p.ld_b < (1u << 23)) {
+        const uint64_t big = (uint64_t)((p.M + 255) / 256) * ((p.N + 255) / 256);
+        if (big >= 192) return launch_tiles<FA, FB, 4, 4>(p, s);
+        return launch_tiles<FA, FB, 2, 2>(p, s);
+    }
     const dim3 grid((p.N + 127) / 128, (p.M + 127) / 128);
     if (p.c_type == REFT_F32) k_product_any<FA, FB, true><<<grid, 256, 0, s>>>(p);
     else k_product_any<FA, FB, false><<<grid, 256, 0, s>>>(p);
