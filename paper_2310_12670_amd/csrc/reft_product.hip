@@ -198,26 +198,34 @@ template <int FA, int FB, bool EXACT> __global__ __launch_bounds__(256) void k_p
             store_tile(p, m0 + wm + i * 32 + (lane & 31), n0 + wn + j * 32, lane, acc[i][j]);
 }
 
-// ---- rows on 16 bytes: two tiles of each operand in LDS, filled by the memory system ------------------------------
-// Four waves of MT x NT products of 32 x 32, two by two.
+// ---- rows on 16 bytes: tiles in LDS that the memory system fills -------------------------------------------------
+// Four waves, two by two, of MT x NT products of 32 x 32 each.  K is walked in steps of 128, with two tiles of each operand in LDS.
 constexpr int kGroup = 8;              // rows of tiles that are walked together, so that what runs at once shares operands
 
 // 16 bytes a lane from base + offset to LDS, those of a wave one after the other.  An offset of 32 bits from a base that the
 // wave shares takes half the registers of addresses.
+// A base that is not `there` has no bytes: the buffer's own bounds check keeps its copies from memory, but they count.
+constexpr uint32_t kOutside = 0xffffffe0u;
 struct Base {
     __amdgpu_buffer_rsrc_t r;
-    __device__ __forceinline__ Base(const uint8_t *p) : r(__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, -1, 0x00027000)) {}
+    __device__ __forceinline__ Base(const uint8_t *p, bool there)
+        : r(__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, __builtin_amdgcn_readfirstlane(there ? kOutside : 0), 0x00027000)) {}
 };
 __device__ __forceinline__ void copy_to_lds(const Base &from, uint32_t offset, uint8_t *to)
 {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from.r, (__attribute__((address_space(3))) void *)to, 16, (int)offset, 0, 0, 0);
 }
 
-// All waves' copies so far have arrived and all have read what they asked for.
-__device__ __forceinline__ void meet()
+// For every wave: all but its last COPIES copies have arrived, what it asked LDS for is read, what it wrote is there.
+template <int COPIES> __device__ __forceinline__ void meet()
 {
-    __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0)
-    __syncthreads();
+    static_assert(COPIES < 64, "vmcnt has six bits");
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((COPIES & 15) | (COPIES >> 4) << 14 | 0x0070);      // vmcnt(COPIES) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // Which tile a workgroup takes.  Workgroups are dealt to the eight dies in turn, and each die has an L2 of its own: a die gets
@@ -227,15 +235,15 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t 
     const uint32_t total = tiles_m * tiles_n, each = total / 8, more = total % 8, die = id % 8;
     const uint32_t t = die * each + min(die, more) + id / 8;
     const uint32_t band = kGroup * tiles_n, first = t / band * kGroup, high = min(tiles_m - first, (uint32_t)kGroup);
-    m = first + t % band % high;
-    n = t % band / high;
+    m = __builtin_amdgcn_readfirstlane(first + t % band % high);
+    n = __builtin_amdgcn_readfirstlane(t % band / high);
 }
 
-// The order of half a step's instructions: a product, then a few reads and copies that do not depend on it, and so on; the
-// reads are done early, so that the wait for them at the half's end is none.
+// The order of a step's instructions: a product, then a few reads and copies that do not depend on it, and so on; the
+// reads are done early, so that the wait for them at the step's end is none.
 template <int PRODUCTS, int READS, int COPIES> __device__ __forceinline__ void interleave()
 {
-    constexpr int kReads = (READS * 4 + PRODUCTS * 3 - 1) / (PRODUCTS * 3), kCopies = (COPIES + PRODUCTS - 1) / PRODUCTS;
+    constexpr int kReads = (READS * 4 + PRODUCTS * 3 - 1) / (PRODUCTS * 3), kCopies = (COPIES * 2 + PRODUCTS - 1) / PRODUCTS;
 #pragma unroll
     for (int i = 0; i < PRODUCTS; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -244,168 +252,185 @@ template <int PRODUCTS, int READS, int COPIES> __device__ __forceinline__ void i
     }
 }
 
-template <int FA, int FB, bool EXACT, int MT, int NT>
+// A wave's results leave in whole rows of 128 bytes, by way of 4 KB of LDS that are its own: 32 rows m of one product's columns n
+// (fp32) or two products' (16 bits).
+// WHOLE: all of them are C's.
+template <typename T, int PARTS, bool WHOLE>
+__device__ __forceinline__ void store_rows(const ProductArgs &p, uint8_t *room, uint32_t m, uint32_t n, int lane, const f32x16 *acc)
+{
+    constexpr uint32_t kEach = 16 / sizeof(T);
+    static_assert(PARTS * 32 * sizeof(T) == 128, "a row of 128 bytes");
+#pragma unroll
+    for (int j = 0; j < PARTS; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const uint32_t at = (j * 32 + 8 * g + 4 * (lane >> 5)) * sizeof(T);          // of four neighbouring columns
+            union { T t[4]; w32x2 w2; w32x4 w4; } u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u.t[i] = narrow<T>(acc[j][4 * g + i]);
+            uint8_t *to = room + place(lane & 31, at / 16) + at % 16;
+            if constexpr (sizeof(T) == 4) *(w32x4 *)to = u.w4;
+            else *(w32x2 *)to = u.w2;
+        }
+    const uint32_t col = n + (lane & 7) * kEach;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = k * 8 + (lane >> 3);
+        union { T t[kEach]; w32x4 w; } u;
+        u.w = *(const w32x4 *)(room + place(r, lane & 7));
+        if (!WHOLE && m + r >= p.M) continue;
+        T *c = (T *)p.c + (m + r) * p.ld_c + col;
+        if (WHOLE || col + kEach <= p.N) {
+            *(w32x4_any *)c = u.w;
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < kEach; ++i)
+                if (col + i < p.N) c[i] = u.t[i];
+        }
+    }
+}
+
+template <int FA, int FB, typename T, int MT, int NT>
 __global__ __launch_bounds__(256, MT * NT >= 16 ? 1 : 2) void k_product(ProductArgs p)
 {
-    constexpr int kRowsA = 64 * MT, kRowsB = 64 * NT, kCopiesA = 2 * MT, kCopiesB = 2 * NT;
+    constexpr bool EXACT = sizeof(T) == 4;
+    constexpr int kRowsA = 64 * MT, kRowsB = 64 * NT, kCopiesA = 2 * MT, kCopiesB = 2 * NT, kCopies = kCopiesA + kCopiesB;
+    constexpr int kProducts = MT * NT * (EXACT ? 4 : 1);
     // variables of their own, so that the compiler knows which copies a read has to wait for
     __shared__ __align__(16) uint8_t ta0[kRowsA * 128], ta1[kRowsA * 128], tb0[kRowsB * 128], tb1[kRowsB * 128];
+    uint8_t *const ta[2] = {ta0, ta1}, *const tb[2] = {tb0, tb1};
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     uint32_t tm, tn;
     tile_of(blockIdx.x, (p.M + kRowsA - 1) / kRowsA, (p.N + kRowsB - 1) / kRowsB, tm, tn);
     const uint32_t m0 = tm * kRowsA, n0 = tn * kRowsB;
     const int wm = (wave & 1) * 32 * MT, wn = (wave >> 1) * 32 * NT;
-    const uint32_t steps = (p.K + 127) / 128;
+    // steps of whole chunks; where K ends in one, the last may be a part of a step, else that part is left to the end
+    const uint32_t steps = p.K % 16 ? p.K / 128 : (p.K + 127) / 128;
     // A wave's copy fills eight rows of a tile: lane i the place i % 8 of row i / 8.  Rows behind the matrix's last repeat that.
     const uint8_t *base_a = p.a + (uint64_t)m0 * p.ld_a, *base_b = p.b + (uint64_t)n0 * p.ld_b;
     uint32_t from_a[kCopiesA], from_b[kCopiesB];
-    auto chunk = [&](int i) { return ((lane & 7) ^ turn(i * 8 + (lane >> 3))) * 16; };
+    auto chunk = [&](int i) { return (uint32_t)((lane & 7) ^ turn(i * 8 + (lane >> 3))) * 16; };
 #pragma unroll
     for (int i = 0; i < kCopiesA; ++i)
         from_a[i] = min((uint32_t)((wave * kCopiesA + i) * 8 + (lane >> 3)), p.M - 1 - m0) * (uint32_t)p.ld_a + chunk(i);
 #pragma unroll
     for (int i = 0; i < kCopiesB; ++i)
         from_b[i] = min((uint32_t)((wave * kCopiesB + i) * 8 + (lane >> 3)), p.N - 1 - n0) * (uint32_t)p.ld_b + chunk(i);
-    auto fill = [&](uint32_t step, uint8_t *ta, uint8_t *tb) {
-        const Base a(base_a + (uint64_t)step * 128), b(base_b + (uint64_t)step * 128);
+    auto fill = [&](uint32_t step, uint8_t *a, uint8_t *b) {
+        const Base from(base_a + (uint64_t)step * 128, step < steps), from2(base_b + (uint64_t)step * 128, step < steps);
+        // chunks behind K lie outside the buffer, and arrive as zeroes
+        const uint32_t left = p.K - step * 128, out0 = chunk(0) < left ? 0 : kOutside, out1 = chunk(1) < left ? 0 : kOutside;
 #pragma unroll
-        for (int i = 0; i < kCopiesA; ++i) copy_to_lds(a, from_a[i], ta + (wave * kCopiesA + i) * 1024);
+        for (int i = 0; i < kCopiesA; ++i) copy_to_lds(from, from_a[i] | (i % 2 ? out1 : out0), a + (wave * kCopiesA + i) * 1024);
 #pragma unroll
-        for (int i = 0; i < kCopiesB; ++i) copy_to_lds(b, from_b[i], tb + (wave * kCopiesB + i) * 1024);
+        for (int i = 0; i < kCopiesB; ++i) copy_to_lds(from2, from_b[i] | (i % 2 ? out1 : out0), b + (wave * kCopiesB + i) * 1024);
     };
-    // The last step may end inside the tile: chunks that begin behind K are read from the row's first one instead (a chunk
-    // lies on 16 bytes, so one that holds a value of the row is memory of the row's), and clear() zeroes all behind K.
-    const uint32_t tail = p.K - (steps - 1) * 128;
-    auto fill_last = [&](uint32_t step, uint8_t *ta, uint8_t *tb) {
-        const Base a(base_a + (uint64_t)step * 128), b(base_b + (uint64_t)step * 128);
+    auto read = [&](i32x8 (&a)[MT], i32x8 (&b)[NT], const uint8_t *from_a, const uint8_t *from_b, int s) {
+        a[0] = operand(from_a, wm, s, lane);                 // in the order of their use
 #pragma unroll
-        for (int i = 0; i < kCopiesA; ++i)
-            copy_to_lds(a, from_a[i] - ((uint32_t)chunk(i) < tail ? 0 : chunk(i)), ta + (wave * kCopiesA + i) * 1024);
+        for (int i = 0; i < NT; ++i) b[i] = operand(from_b, wn + i * 32, s, lane);
 #pragma unroll
-        for (int i = 0; i < kCopiesB; ++i)
-            copy_to_lds(b, from_b[i] - ((uint32_t)chunk(i) < tail ? 0 : chunk(i)), tb + (wave * kCopiesB + i) * 1024);
-    };
-    auto clear = [&](uint8_t *ta, uint8_t *tb) {
-        for (int r = tid; r < kRowsA + kRowsB; r += 256) {
-            uint8_t *t = r < kRowsA ? ta : tb;
-            const int row = r < kRowsA ? r : r - kRowsA;
-            int k = (int)tail;
-            for (; k % 16; ++k) t[place(row, k / 16) + k % 16] = 0;
-            for (; k < 128; k += 16) *(w32x4 *)(t + place(row, k / 16)) = w32x4{0, 0, 0, 0};
-        }
-    };
-    auto read = [&](i32x8 (&a)[MT], i32x8 (&b)[NT], const uint8_t *ta, const uint8_t *tb, int s) {
-        a[0] = operand(ta, wm, s, lane);                     // in the order of their use
-#pragma unroll
-        for (int i = 0; i < NT; ++i) b[i] = operand(tb, wn + i * 32, s, lane);
-#pragma unroll
-        for (int i = 1; i < MT; ++i) a[i] = operand(ta, wm + i * 32, s, lane);
+        for (int i = 1; i < MT; ++i) a[i] = operand(from_a, wm + i * 32, s, lane);
     };
     f32x16 acc[MT][NT] = {};
-    auto multiply_all = [&](const i32x8 (&ra)[MT], const i32x8 (&rb)[NT], const uint32_t (&sa)[MT], const uint32_t (&sb)[NT]) {
+    uint32_t sa[MT], sb[NT], next_sa[MT], next_sb[NT];
+    const uint32_t last_word = (p.K - 1) / 512;
+    auto words = [&](uint32_t w) {
+        w = min(w, last_word);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) next_sa[i] = (p.sa + w * p.ld_sa)[min(m0 + wm + i * 32 + (lane & 31), p.M - 1)];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) next_sb[i] = (p.sb + w * p.ld_sb)[min(n0 + wn + i * 32 + (lane & 31), p.N - 1) >> p.b_shift];
+    };
+    auto take_words = [&]() {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) sa[i] = next_sa[i];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) sb[i] = next_sb[i];
+    };
+    auto multiply_all = [&](const i32x8 (&ra)[MT], const i32x8 (&rb)[NT], int shift) {
         Operand<FA, EXACT> a[MT];
         Operand<FB, EXACT> b[NT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) a[i].take(ra[i], sa[i]);
+        for (int i = 0; i < MT; ++i) a[i].take(ra[i], sa[i] >> shift);
 #pragma unroll
-        for (int i = 0; i < NT; ++i) b[i].take(rb[i], sb[i]);
+        for (int i = 0; i < NT; ++i) b[i].take(rb[i], sb[i] >> shift);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j) acc[i][j] = multiply<FA, FB>(b[j], a[i], acc[i][j]);
     };
-    const uint32_t last_word = (steps - 1) / 4;
-    auto words = [&](uint32_t w, uint32_t (&sa)[MT], uint32_t (&sb)[NT]) {
-        w = min(w, last_word);
-#pragma unroll
-        for (int i = 0; i < MT; ++i) sa[i] = (p.sa + w * p.ld_sa)[min(m0 + wm + i * 32 + (lane & 31), p.M - 1)];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) sb[i] = (p.sb + w * p.ld_sb)[min(n0 + wn + i * 32 + (lane & 31), p.N - 1) >> p.b_shift];
-    };
-    auto shifted = [&](uint32_t (&sa)[MT], uint32_t (&sb)[NT]) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i) sa[i] >>= 8;
-#pragma unroll
-        for (int i = 0; i < NT; ++i) sb[i] >>= 8;
-    };
-    auto any_fill = [&](uint32_t step, uint8_t *ta, uint8_t *tb) {
-        if (step + 1 < steps) fill(step, ta, tb);
-        else if (step + 1 == steps) fill_last(step, ta, tb);
-    };
 
+    fill(0, ta0, tb0);
+    fill(1, ta1, tb1);
+    words(0);
+    take_words();
+    meet<0>();
     i32x8 a0[MT], b0[NT], a1[MT], b1[NT];
-    uint32_t sa[MT], sb[NT], next_sa[MT], next_sb[NT];
-    words(0, sa, sb);
-    any_fill(0, ta0, tb0);
-    any_fill(1, ta1, tb1);
-    meet();
-    if (steps == 1 && tail < 128) {
-        clear(ta0, tb0);
-        meet();
-    }
     read(a0, b0, ta0, tb0, 0);
-    uint32_t step = 0;
     // Half a step multiplies what half a step ago was read from LDS, while the next half is read; between a step's halves its tile
-    // has been read by all and the next one's has arrived, so that the one after next may be fetched into its place: it has
-    // a whole step's time.
-    for (; step + 6 < steps; step += 4) {
-        words(step / 4 + 1, next_sa, next_sb);
+    // has been read by all and the next one's has arrived, so that the one after next is fetched into its place.  A word
+    // of scales serves four steps.
+    for (uint32_t step = 0; step < steps; step += 4) {
+        words(step / 4 + 1);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            uint8_t *ta = j % 2 ? ta1 : ta0, *tb = j % 2 ? tb1 : tb0, *oa = j % 2 ? ta0 : ta1, *ob = j % 2 ? tb0 : tb1;
-            read(a1, b1, ta, tb, 1);
-            multiply_all(a0, b0, sa, sb);
-            interleave<MT * NT * (EXACT ? 4 : 1), 2 * (MT + NT), 0>();
+            if (step + j >= steps) break;
+            read(a1, b1, ta[j % 2], tb[j % 2], 1);
+            multiply_all(a0, b0, j * 8);
+            interleave<kProducts, 2 * (MT + NT), 0>();
+            meet<0>();
+            fill(step + j + 2, ta[j % 2], tb[j % 2]);
+            read(a0, b0, ta[(j + 1) % 2], tb[(j + 1) % 2], 0);
+            multiply_all(a1, b1, j * 8);
+            interleave<kProducts, 2 * (MT + NT), kCopies>();
             __builtin_amdgcn_sched_barrier(0);
-            meet();
-            __builtin_amdgcn_sched_barrier(0);
-            fill(step + j + 2, ta, tb);
-            read(a0, b0, oa, ob, 0);
-            multiply_all(a1, b1, sa, sb);
-            interleave<MT * NT * (EXACT ? 4 : 1), 2 * (MT + NT), 2 * (MT + NT)>();
-            __builtin_amdgcn_sched_barrier(0);
-            shifted(sa, sb);
         }
-#pragma unroll
-        for (int i = 0; i < MT; ++i) sa[i] = next_sa[i];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) sb[i] = next_sb[i];
+        take_words();
     }
-    words(step / 4 + 1, next_sa, next_sb);
-#pragma unroll
-    for (int j = 0; j < 6; ++j) {
-        if (step + j >= steps) break;
-        uint8_t *ta = j % 2 ? ta1 : ta0, *tb = j % 2 ? tb1 : tb0, *oa = j % 2 ? ta0 : ta1, *ob = j % 2 ? tb0 : tb1;
-        read(a1, b1, ta, tb, 1);
-        multiply_all(a0, b0, sa, sb);
-        meet();
-        any_fill(step + j + 2, ta, tb);
-        if (step + j + 2 == steps && tail < 128) {
-            clear(oa, ob);
-            meet();
+    if (p.K % 16) {                                          // the rest of K, with zeroes behind it: through registers
+        const uint32_t left = p.K - steps * 128;
+        meet<0>();
+#pragma unroll 1
+        for (int r = tid >> 3; r < kRowsA + kRowsB; r += 32) {
+            const int row = r < kRowsA ? r : r - kRowsA, k = (tid & 7) * 16;
+            const uint32_t at = r < kRowsA ? min((uint32_t)row, p.M - 1 - m0) : min((uint32_t)row, p.N - 1 - n0);
+            const uint8_t *from = (r < kRowsA ? base_a + at * p.ld_a : base_b + at * p.ld_b) + (uint64_t)steps * 128 + k;
+            *(w32x4 *)((r < kRowsA ? ta0 : tb0) + place(row, k / 16)) = load16(from, (int)left - k);
         }
-        if (step + j + 1 < steps) read(a0, b0, oa, ob, 0);
-        multiply_all(a1, b1, sa, sb);
-        shifted(sa, sb);
-        if (j == 3) {
-#pragma unroll
-            for (int i = 0; i < MT; ++i) sa[i] = next_sa[i];
-#pragma unroll
-            for (int i = 0; i < NT; ++i) sb[i] = next_sb[i];
+        words(last_word);
+        take_words();
+        meet<0>();
+#pragma unroll 1
+        for (int s = 0; s < 2; ++s) {
+            read(a0, b0, ta0, tb0, s);
+            multiply_all(a0, b0, steps % 4 * 8);
         }
     }
+    constexpr int kParts = 4 / sizeof(T);
+    uint8_t *const room = (wave & 2 ? ta1 : ta0) + (wave & 1) * 4096;
+    meet<0>();
+    if (m0 + kRowsA <= p.M && n0 + kRowsB <= p.N) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-            store_tile(p, m0 + wm + i * 32 + (lane & 31), n0 + wn + j * 32, lane, acc[i][j]);
+            for (int j = 0; j < NT; j += kParts)
+                store_rows<T, kParts, true>(p, room, m0 + wm + i * 32, n0 + wn + j * 32, lane, &acc[i][j]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; j += kParts)
+                store_rows<T, kParts, false>(p, room, m0 + wm + i * 32, n0 + wn + j * 32, lane, &acc[i][j]);
+    }
 }
 
 template <int FA, int FB, int MT, int NT> static hipError_t launch_tiles(const ProductArgs &p, hipStream_t s)
 {
     const uint64_t tiles = (uint64_t)((p.M + 64 * MT - 1) / (64 * MT)) * ((p.N + 64 * NT - 1) / (64 * NT));
-    if (p.c_type == REFT_F32) k_product<FA, FB, true, MT, NT><<<(uint32_t)tiles, 256, 0, s>>>(p);
-    else k_product<FA, FB, false, MT, NT><<<(uint32_t)tiles, 256, 0, s>>>(p);
+    if (p.c_type == REFT_F32) k_product<FA, FB, float, MT, NT><<<(uint32_t)tiles, 256, 0, s>>>(p);
+    else if (p.c_type == REFT_BF16) k_product<FA, FB, bf16, MT, NT><<<(uint32_t)tiles, 256, 0, s>>>(p);
+    else k_product<FA, FB, f16, MT, NT><<<(uint32_t)tiles, 256, 0, s>>>(p);
     return hipGetLastError();
 }
 
