@@ -426,109 +426,119 @@ def reft_restore_wait(plan) -> None:
 _TYPES = {"torch.float32": REFT_F32, "torch.bfloat16": REFT_BF16, "torch.float16": REFT_F16,
           "torch.float8_e4m3fn": REFT_E4M3, "torch.float8_e5m2": REFT_E5M2}
 _TYPE_OF: dict = {}                       # the same by torch.dtype, filled as they are met
-
-
-def _type(t) -> int:
-    code = _TYPE_OF.get(t.dtype)
-    if code is None:
-        code = _TYPES.get(str(t.dtype))
-        if code is None:
-            raise ReftError(REFT_EINVAL, f"no operator takes {t.dtype}")
-        _TYPE_OF[t.dtype] = code
-    return code
+_FLOATS, _EIGHTS = (REFT_F32, REFT_BF16, REFT_F16), (REFT_E4M3, REFT_E5M2)
+_OR_F32 = {REFT_F32: (REFT_F32,), REFT_BF16: (REFT_BF16, REFT_F32), REFT_F16: (REFT_F16, REFT_F32)}
+_ONLY = {c: (c,) for c in _FLOATS + _EIGHTS}
+_JUST_F32 = (REFT_F32,)
+_NONE = (None, 0, 0)
 
 
 def _refuse(who: str, what: str):
     raise ReftError(REFT_EINVAL, f"{who}: {what}")
 
 
-def _matrix(who: str, name: str, t, shape=None, types=None):
-    """(address, row length, type) of a 2-D tensor whose rows are contiguous."""
-    if t is None:
-        return None, 0, 0
-    size = t.shape
-    if len(size) != 2 or (shape is not None and (size[0] != shape[0] or size[1] != shape[1])):
-        _refuse(who, f"{name} has the shape {tuple(size)}, not {shape or 'of a matrix'}")
-    down, along = t.stride()
-    if along != 1 and size[1] > 1:
-        _refuse(who, f"{name}'s rows are not contiguous")
-    if size[0] <= 1:
-        down = size[1]
-    code = _type(t)
-    if types is not None and code not in types:
+# A call's time on the host is mostly spent here: the usual case first, everything else in the functions behind.
+def _matrix(who: str, name: str, t, shape, types):
+    """(address, row length, type) of a 2-D tensor of that shape whose rows are contiguous."""
+    if t.shape == shape:
+        code = _TYPE_OF.get(t.dtype)
+        down, along = t.stride()
+        if along == 1 and down >= shape[1] and code in types:
+            return t.data_ptr(), down, code
+    return _other_matrix(who, name, t, shape, types)
+
+
+def _other_matrix(who, name, t, shape, types):
+    if len(shape) != 2 or tuple(t.shape) != tuple(shape):
+        _refuse(who, f"{name} has the shape {tuple(t.shape)}" + (f", not {tuple(shape)}" if len(shape) == 2 else ""))
+    if str(t.dtype) in _TYPES:
+        _TYPE_OF[t.dtype] = _TYPES[str(t.dtype)]
+    code = _TYPE_OF.get(t.dtype)
+    if code not in types:
         _refuse(who, f"{name} is {t.dtype}")
-    return t.data_ptr() or None, down, code
+    down, along = t.stride()
+    if along != 1 and shape[1] > 1:
+        _refuse(who, f"{name}'s rows are not contiguous")
+    return t.data_ptr(), down if shape[0] > 1 else shape[1], code
+
+
+def _first(who: str, name: str, t, types):
+    """The same of a call's first matrix, whose shape the others go by."""
+    code = _TYPE_OF.get(t.dtype)
+    if code in types and t.dim() == 2:
+        down, along = t.stride()
+        if along == 1 and down >= t.shape[1]:
+            return t.data_ptr(), down, code
+    return _other_matrix(who, name, t, t.shape, types)
 
 
 def _vector(who: str, name: str, t, n: int, types):
     """(address, type) of a contiguous vector of n values."""
-    if t is None:
-        return None, 0
-    code = _type(t)
-    if t.shape != (n,) or code not in types or (n > 1 and t.stride(0) != 1):
-        _refuse(who, f"{name} is no contiguous vector of {n} values of a type that it may have")
-    return t.data_ptr() or None, code
+    code = _TYPE_OF.get(t.dtype)
+    if code in types and t.shape == (n,) and t.is_contiguous():
+        return t.data_ptr(), code
+    if code is None and str(t.dtype) in _TYPES:
+        _TYPE_OF[t.dtype] = _TYPES[str(t.dtype)]
+        return _vector(who, name, t, n, types)
+    _refuse(who, f"{name} is no contiguous vector of {n} values of a type that it may have")
 
 
 def _scales(who: str, name: str, t, rows: int, cols: int):
     """(address, words from one word of a row to its next) of bytes [ceil(cols / 512)][rows][4]."""
-    if t is None:
-        return None, 0
-    words = (cols + 511) // 512
+    words = (cols + 511) >> 9
     if t.shape != (words, rows, 4) or t.element_size() != 1:
         _refuse(who, f"{name} are not bytes [{words}][{rows}][4]")
     wide, row, one = t.stride()
+    if one == 1 and row == 4 and wide == 4 * rows:
+        return t.data_ptr(), rows
     if (one != 1 or (rows > 1 and row != 4) or (words > 1 and wide % 4)) and t.numel():
         _refuse(who, f"{name}: the words of a row's scales are not contiguous")
-    return t.data_ptr() or None, wide // 4 if words > 1 else rows
+    return t.data_ptr(), wide // 4 if words > 1 else rows
 
 
 def _scratch(t):
-    return (None, 0) if t is None else (t.data_ptr() or None, t.numel() * t.element_size())
-
-
-_FLOATS, _EIGHTS = (REFT_F32, REFT_BF16, REFT_F16), (REFT_E4M3, REFT_E5M2)
+    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
 
 
 def reft_dropout(x, y, p: float, seed: int, offset: int = 0, stream=None) -> None:
     """``y`` (may be ``x``) gets ``x`` with elements dropped by the counter (seed, offset)."""
-    who = "reft_dropout"
-    ax, ld_x, code = _matrix(who, "x", x, None, _FLOATS)
-    ay, ld_y, _ = _matrix(who, "y", y, x.shape, (code,))
-    _check(_load().reft_dropout(ax, ld_x, ay, ld_y, x.shape[0], x.shape[1], code, p, seed, offset, _stream(stream)))
+    ax, ld_x, code = _first("reft_dropout", "x", x, _FLOATS)
+    rows, cols = shape = x.shape
+    ay, ld_y, _ = _matrix("reft_dropout", "y", y, shape, _ONLY[code])
+    _check(_load().reft_dropout(ax, ld_x, ay, ld_y, rows, cols, code, p, seed, offset, _stream(stream)))
 
 
 def reft_norm_forward(x, residual, weight, eps: float, p: float = 0.0, seed: int = 0, offset: int = 0, *, h=None,
                       rstd=None, y=None, q=None, scales=None, stream=None) -> None:
-    who, shape = "reft_norm_forward", x.shape
-    ax, ld_x, code = _matrix(who, "x", x, None, _FLOATS)
-    rows, cols = shape
-    wide = (code, REFT_F32)
-    ar, ld_r, r_code = _matrix(who, "residual", residual, shape, wide)
-    ah, ld_h, h_code = _matrix(who, "h", h, shape, wide if residual is None else (r_code,))
-    aw, w_code = _vector(who, "weight", weight, cols, wide)
-    arstd, _ = _vector(who, "rstd", rstd, rows, (REFT_F32,))
-    ay, ld_y, _ = _matrix(who, "y", y, shape, (code,))
-    aq, ld_q, fmt = _matrix(who, "q", q, shape, _EIGHTS)
-    asc, ld_s = _scales(who, "scales", scales, rows, cols)
+    who = "reft_norm_forward"
+    ax, ld_x, code = _first(who, "x", x, _FLOATS)
+    rows, cols = shape = x.shape
+    wide = _OR_F32[code]
+    ar, ld_r, r_code = (None, 0, None) if residual is None else _matrix(who, "residual", residual, shape, wide)
+    ah, ld_h, h_code = (None, 0, code) if h is None else _matrix(who, "h", h, shape, wide if r_code is None else _ONLY[r_code])
+    aw, w_code = (None, code) if weight is None else _vector(who, "weight", weight, cols, wide)
+    arstd = None if rstd is None else _vector(who, "rstd", rstd, rows, _JUST_F32)[0]
+    ay, ld_y, _ = _NONE if y is None else _matrix(who, "y", y, shape, _ONLY[code])
+    aq, ld_q, fmt = _NONE if q is None else _matrix(who, "q", q, shape, _EIGHTS)
+    asc, ld_s = (None, 0) if scales is None else _scales(who, "scales", scales, rows, cols)
     _check(_load().reft_norm_forward(
-        ax, ld_x, ar, ld_r, aw, rows, cols, code, r_code if residual is not None else h_code if h is not None else code,
-        w_code if weight is not None else code, eps, p, seed, offset, ah, ld_h, arstd, ay, ld_y, aq, ld_q, fmt, asc, ld_s,
-        _stream(stream)))
+        ax, ld_x, ar, ld_r, aw, rows, cols, code, h_code if r_code is None else r_code, w_code, eps, p,
+        seed, offset, ah, ld_h, arstd, ay, ld_y, aq, ld_q, fmt, asc, ld_s, _stream(stream)))
 
 
 def reft_norm_backward(dy, dh, h, rstd, weight, p: float = 0.0, seed: int = 0, offset: int = 0, *, dres=None, dx=None,
                        dweight=None, workspace=None, stream=None) -> None:
-    who, shape = "reft_norm_backward", dy.shape
-    ady, ld_dy, code = _matrix(who, "dy", dy, None, _FLOATS)
-    rows, cols = shape
-    ah, ld_h, r_code = _matrix(who, "h", h, shape, (code, REFT_F32))
-    adh, ld_dh, _ = _matrix(who, "dh", dh, shape, (r_code,))
-    arstd, _ = _vector(who, "rstd", rstd, rows, (REFT_F32,))
-    aw, w_code = _vector(who, "weight", weight, cols, (code, REFT_F32))
-    adres, ld_dres, _ = _matrix(who, "dres", dres, shape, (r_code,))
-    adx, ld_dx, _ = _matrix(who, "dx", dx, shape, (code,))
-    adw, _ = _vector(who, "dweight", dweight, cols, (REFT_F32,))
+    who = "reft_norm_backward"
+    ady, ld_dy, code = _first(who, "dy", dy, _FLOATS)
+    rows, cols = shape = dy.shape
+    wide = _OR_F32[code]
+    ah, ld_h, r_code = _matrix(who, "h", h, shape, wide)
+    adh, ld_dh, _ = _NONE if dh is None else _matrix(who, "dh", dh, shape, _ONLY[r_code])
+    arstd = None if rstd is None else _vector(who, "rstd", rstd, rows, _JUST_F32)[0]
+    aw, w_code = (None, code) if weight is None else _vector(who, "weight", weight, cols, wide)
+    adres, ld_dres, _ = _NONE if dres is None else _matrix(who, "dres", dres, shape, _ONLY[r_code])
+    adx, ld_dx, _ = _NONE if dx is None else _matrix(who, "dx", dx, shape, _ONLY[code])
+    adw = None if dweight is None else _vector(who, "dweight", dweight, cols, _JUST_F32)[0]
     ws, ws_bytes = _scratch(workspace)
     _check(_load().reft_norm_backward(
         ady, ld_dy, adh, ld_dh, ah, ld_h, arstd, aw, rows, cols, code, r_code, w_code, p, seed, offset, adres, ld_dres, adx,
@@ -542,27 +552,28 @@ def reft_norm_backward_workspace(rows: int, cols: int) -> int:
 def reft_quantize(x, q=None, scales=None, q_t=None, scales_t=None, *, blocks: bool = False, stream=None) -> None:
     """``q`` and ``q_t`` are float8 tensors of the shape of ``x`` and of its transpose."""
     who = "reft_quantize"
-    ax, ld_x, code = _matrix(who, "x", x, None, _FLOATS)
-    rows, cols = x.shape
-    aq, ld_q, fmt = _matrix(who, "q", q, (rows, cols), _EIGHTS)
-    at, ld_t, fmt_t = _matrix(who, "q_t", q_t, (cols, rows), _EIGHTS)
-    if q is not None and q_t is not None and fmt != fmt_t:
-        _refuse(who, "q and q_t have different types")
-    asc, ld_s = _scales(who, "scales", scales, (rows + 127) // 128 if blocks else rows, cols)
-    ast, ld_st = _scales(who, "scales_t", scales_t, (cols + 127) // 128 if blocks else cols, rows)
-    _check(_load().reft_quantize(ax, ld_x, rows, cols, code, fmt if q is not None else fmt_t, 1 if blocks else 0, aq, ld_q,
-                                 asc, ld_s, at, ld_t, ast, ld_st, _stream(stream)))
+    ax, ld_x, code = _first(who, "x", x, _FLOATS)
+    rows, cols = shape = x.shape
+    aq, ld_q, fmt = (None, 0, None) if q is None else _matrix(who, "q", q, shape, _EIGHTS)
+    at, ld_t, fmt_t = _NONE if q_t is None else _matrix(who, "q_t", q_t, (cols, rows), _EIGHTS if fmt is None else _ONLY[fmt])
+    tall, wide = ((rows + 127) >> 7, (cols + 127) >> 7) if blocks else (rows, cols)
+    asc, ld_s = (None, 0) if scales is None else _scales(who, "scales", scales, tall, cols)
+    ast, ld_st = (None, 0) if scales_t is None else _scales(who, "scales_t", scales_t, wide, rows)
+    _check(_load().reft_quantize(ax, ld_x, rows, cols, code, fmt_t if fmt is None else fmt, 1 if blocks else 0, aq, ld_q, asc,
+                                 ld_s, at, ld_t, ast, ld_st, _stream(stream)))
 
 
 def reft_product(a, a_scales, b, b_scales, c, workspace=None, *, b_blocks: bool = False, stream=None) -> None:
     """``c`` [M, N] = ``a`` [M, K] times the transpose of ``b`` [N, K], both float8 with their scales."""
     who = "reft_product"
-    aa, ld_a, fa = _matrix(who, "a", a, None, _EIGHTS)
+    aa, ld_a, fa = _first(who, "a", a, _EIGHTS)
+    ab, ld_b, fb = _first(who, "b", b, _EIGHTS)
     M, K = a.shape
-    N = b.shape[0]
-    ab, ld_b, fb = _matrix(who, "b", b, (N, K), _EIGHTS)
-    asa, ld_as = _scales(who, "a_scales", a_scales, M, K)
-    asb, ld_bs = _scales(who, "b_scales", b_scales, (N + 127) // 128 if b_blocks else N, K)
+    N, K2 = b.shape
+    if K != K2:
+        _refuse(who, f"a has {K} columns and b {K2}")
+    asa, ld_as = (None, 0) if a_scales is None else _scales(who, "a_scales", a_scales, M, K)
+    asb, ld_bs = (None, 0) if b_scales is None else _scales(who, "b_scales", b_scales, (N + 127) >> 7 if b_blocks else N, K)
     ac, ld_c, fc = _matrix(who, "c", c, (M, N), _FLOATS)
     ws, ws_bytes = _scratch(workspace)
     _check(_load().reft_product(aa, ld_a, fa, asa, ld_as, ab, ld_b, fb, asb, ld_bs, 1 if b_blocks else 0, M, N, K, ac, ld_c,

@@ -16,6 +16,8 @@ struct ProductArgs {
     uint32_t b_shift;              // row n of b has scale n >> b_shift: 7 for blocks of 128 rows, else 0
     void *c;
     int c_type;
+    uint32_t splits, split_steps;  // parts that K is cut into, and steps of 128 to a part (a multiple of 4)
+    float *parts;                  // [splits][M][N] where there are several
 };
 
 // ---- tiles in LDS -----------------------------------------------------------------------------------------
@@ -93,6 +95,13 @@ __device__ __forceinline__ w32x4 load16(const uint8_t *p, int n)
     for (int i = 0; i < 16; ++i)
         if (i < n) w[i / 4] |= (uint32_t)p[i] << (8 * (i & 3));
     return w;
+}
+
+__device__ __forceinline__ void store1(const ProductArgs &p, uint64_t at, float v)
+{
+    if (p.c_type == REFT_F32) ((float *)p.c)[at] = v;
+    else if (p.c_type == REFT_BF16) ((bf16 *)p.c)[at] = narrow<bf16>(v);
+    else ((f16 *)p.c)[at] = narrow<f16>(v);
 }
 
 // Four neighbouring columns of a row of C, of which the first n exist.
@@ -198,9 +207,85 @@ template <int FA, int FB, bool EXACT> __global__ __launch_bounds__(256) void k_p
             store_tile(p, m0 + wm + i * 32 + (lane & 31), n0 + wn + j * 32, lane, acc[i][j]);
 }
 
+// ---- few rows of A: the weights' bytes are the bound ------------------------------------------------------------------
+// A workgroup takes 16 rows of B, its waves blocks of 128 of K in turn; each lane loads its part of a product of 16 x 16 x 128 from
+// memory itself (any alignment), four blocks ahead, and multiplies it with up to MT times 16 rows of A.  The waves' sums meet in
+// LDS and are added in the waves' order.
+template <int FA, int FB, bool EXACT>
+__device__ __forceinline__ f32x4 multiply16(i32x8 b, i32x8 a, f32x4 acc, uint32_t eb, uint32_t ea)
+{
+    if constexpr (!EXACT) {
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc, FB, FA, 0, (int)eb, 0, (int)ea);
+    } else {
+        Operand<FB, true> wb;
+        Operand<FA, true> wa;
+        wb.take(b, eb);
+        wa.take(a, ea);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb.v[i], wa.v[i], acc, 0, 0, 0);
+        return acc;
+    }
+}
+
+template <int FA, int FB, bool EXACT, int MT, int WAVES> __global__ __launch_bounds__(64 * WAVES) void k_product_few(ProductArgs p)
+{
+    constexpr int kAhead = MT == 1 ? 4 : 2;
+    __shared__ f32x4 sums[WAVES][MT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t n0 = blockIdx.x * 16, r = lane & 15, blocks = (p.K + 127) / 128;
+    const uint32_t n = min(n0 + r, p.N - 1);                 // rows behind the last repeat it, and are not stored
+    const uint8_t *b = p.b + n * p.ld_b, *sb = (const uint8_t *)(p.sb + (n >> p.b_shift));
+    f32x4 acc[MT] = {};
+    for (uint32_t first = wave; first < blocks; first += WAVES * kAhead) {
+        w32x4 vb[kAhead][2], va[kAhead][MT][2];
+        uint32_t eb[kAhead], ea[kAhead][MT];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const uint32_t block = first + u * WAVES, k = block * 128 + (lane >> 4) * 32;
+            const bool there = block < blocks;
+            const int left = !there || k >= p.K ? 0 : (int)min(p.K - k, 32u);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) vb[u][h] = load16(b + k + h * 16, left - h * 16);
+            eb[u] = there ? sb[block / 4 * p.ld_sb * 4 + block % 4] : 127;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const uint32_t m = i * 16 + r;
+                const bool row = there && m < p.M;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) va[u][i][h] = load16(p.a + m * p.ld_a + k + h * 16, row ? left - h * 16 : 0);
+                ea[u][i] = row ? ((const uint8_t *)p.sa)[(block / 4 * p.ld_sa + m) * 4 + block % 4] : 127;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            i32x8 ob, oa;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ob[e] = (int)vb[u][e / 4][e % 4];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) oa[e] = (int)va[u][i][e / 4][e % 4];
+                acc[i] = multiply16<FA, FB, EXACT>(ob, oa, acc[i], eb[u], ea[u][i]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+    __syncthreads();
+    for (int t = threadIdx.x; t < MT * 256; t += 64 * WAVES) {
+        // column t % 16 of row t / 16: lane (column / 4) * 16 + row % 16 holds it, in place column % 4
+        const uint32_t col = t % 16, row = t / 16;
+        float v = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) v += sums[w][row / 16][col / 4 * 16 + row % 16][col % 4];
+        if (row < p.M && n0 + col < p.N) store1(p, row * p.ld_c + n0 + col, v);
+    }
+}
+
 // ---- rows on 16 bytes: tiles in LDS that the memory system fills -------------------------------------------------
-// Four waves, two by two, of MT x NT products of 32 x 32 each.  K is walked in steps of 128, with two tiles of each operand in LDS.
-constexpr int kGroup = 8;              // rows of tiles that are walked together, so that what runs at once shares operands
+// Four waves, two by two, of MT x NT products of 32 x 32 each.  K is walked in steps of 128, with three tiles of A and two of B in LDS.
+// Rows of tiles that are walked together, so that what runs at once on a die shares operands (8192 x 28672 x 8192: 4 1456 us, 8 1490, 16 1590).
+constexpr int kGroup = 4;
 
 // 16 bytes a lane from base + offset to LDS, those of a wave one after the other.  An offset of 32 bits from a base that the
 // wave shares takes half the registers of addresses.
@@ -243,7 +328,7 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t 
 // reads are done early, so that the wait for them at the step's end is none.
 template <int PRODUCTS, int READS, int COPIES> __device__ __forceinline__ void interleave()
 {
-    constexpr int kReads = (READS * 4 + PRODUCTS * 3 - 1) / (PRODUCTS * 3), kCopies = (COPIES * 2 + PRODUCTS - 1) / PRODUCTS;
+    constexpr int kReads = (READS * 4 + PRODUCTS * 3 - 1) / (PRODUCTS * 3), kCopies = (COPIES + PRODUCTS - 1) / PRODUCTS;
 #pragma unroll
     for (int i = 0; i < PRODUCTS; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -256,7 +341,8 @@ template <int PRODUCTS, int READS, int COPIES> __device__ __forceinline__ void i
 // (fp32) or two products' (16 bits).
 // WHOLE: all of them are C's.
 template <typename T, int PARTS, bool WHOLE>
-__device__ __forceinline__ void store_rows(const ProductArgs &p, uint8_t *room, uint32_t m, uint32_t n, int lane, const f32x16 *acc)
+__device__ __forceinline__ void store_rows(T *to_c, uint64_t ld_c, const ProductArgs &p, uint8_t *room, uint32_t m, uint32_t n, int lane,
+                                           const f32x16 *acc)
 {
     constexpr uint32_t kEach = 16 / sizeof(T);
     static_assert(PARTS * 32 * sizeof(T) == 128, "a row of 128 bytes");
@@ -279,7 +365,7 @@ __device__ __forceinline__ void store_rows(const ProductArgs &p, uint8_t *room, 
         union { T t[kEach]; w32x4 w; } u;
         u.w = *(const w32x4 *)(room + place(r, lane & 7));
         if (!WHOLE && m + r >= p.M) continue;
-        T *c = (T *)p.c + (m + r) * p.ld_c + col;
+        T *c = to_c + (m + r) * ld_c + col;
         if (WHOLE || col + kEach <= p.N) {
             *(w32x4_any *)c = u.w;
         } else {
@@ -290,24 +376,44 @@ __device__ __forceinline__ void store_rows(const ProductArgs &p, uint8_t *room, 
     }
 }
 
-template <int FA, int FB, typename T, int MT, int NT>
+template <typename T, int MT, int NT>
+__device__ __forceinline__ void store_all(T *c, uint64_t ld_c, const ProductArgs &p, uint8_t *room, uint32_t m, uint32_t n, int lane,
+                                          const f32x16 (&acc)[MT][NT])
+{
+    constexpr int kParts = 4 / sizeof(T);
+    if (m + 32 * MT <= p.M && n + 32 * NT <= p.N) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; j += kParts) store_rows<T, kParts, true>(c, ld_c, p, room, m + i * 32, n + j * 32, lane, &acc[i][j]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; j += kParts) store_rows<T, kParts, false>(c, ld_c, p, room, m + i * 32, n + j * 32, lane, &acc[i][j]);
+    }
+}
+
+// T: what is stored, into C or, of several parts of K, into a part's place.
+template <int FA, int FB, bool EXACT, typename T, int MT, int NT>
 __global__ __launch_bounds__(256, MT * NT >= 16 ? 1 : 2) void k_product(ProductArgs p)
 {
-    constexpr bool EXACT = sizeof(T) == 4;
     constexpr int kRowsA = 64 * MT, kRowsB = 64 * NT, kCopiesA = 2 * MT, kCopiesB = 2 * NT, kCopies = kCopiesA + kCopiesB;
     constexpr int kProducts = MT * NT * (EXACT ? 4 : 1);
     // variables of their own, so that the compiler knows which copies a read has to wait for
-    __shared__ __align__(16) uint8_t ta0[kRowsA * 128], ta1[kRowsA * 128], tb0[kRowsB * 128], tb1[kRowsB * 128];
-    uint8_t *const ta[2] = {ta0, ta1}, *const tb[2] = {tb0, tb1};
+    __shared__ __align__(16) uint8_t ta0[kRowsA * 128], ta1[kRowsA * 128], ta2[kRowsA * 128], tb0[kRowsB * 128], tb1[kRowsB * 128];
+    uint8_t *const ta[3] = {ta0, ta1, ta2}, *const tb[2] = {tb0, tb1};
+    constexpr bool kWhole = MT * NT >= 16;                   // K is never cut
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     uint32_t tm, tn;
     tile_of(blockIdx.x, (p.M + kRowsA - 1) / kRowsA, (p.N + kRowsB - 1) / kRowsB, tm, tn);
     const uint32_t m0 = tm * kRowsA, n0 = tn * kRowsB;
     const int wm = (wave & 1) * 32 * MT, wn = (wave >> 1) * 32 * NT;
     // steps of whole chunks; where K ends in one, the last may be a part of a step, else that part is left to the end
-    const uint32_t steps = p.K % 16 ? p.K / 128 : (p.K + 127) / 128;
+    const uint32_t all = p.K % 16 ? p.K / 128 : (p.K + 127) / 128, start = kWhole ? 0 : blockIdx.y * p.split_steps;
+    const uint32_t steps = kWhole ? all : start < all ? min(all - start, p.split_steps) : 0, K = p.K - start * 128;
     // A wave's copy fills eight rows of a tile: lane i the place i % 8 of row i / 8.  Rows behind the matrix's last repeat that.
-    const uint8_t *base_a = p.a + (uint64_t)m0 * p.ld_a, *base_b = p.b + (uint64_t)n0 * p.ld_b;
+    const uint8_t *base_a = p.a + (uint64_t)m0 * p.ld_a + (uint64_t)start * 128, *base_b = p.b + (uint64_t)n0 * p.ld_b + (uint64_t)start * 128;
     uint32_t from_a[kCopiesA], from_b[kCopiesB];
     auto chunk = [&](int i) { return (uint32_t)((lane & 7) ^ turn(i * 8 + (lane >> 3))) * 16; };
 #pragma unroll
@@ -316,14 +422,18 @@ __global__ __launch_bounds__(256, MT * NT >= 16 ? 1 : 2) void k_product(ProductA
 #pragma unroll
     for (int i = 0; i < kCopiesB; ++i)
         from_b[i] = min((uint32_t)((wave * kCopiesB + i) * 8 + (lane >> 3)), p.N - 1 - n0) * (uint32_t)p.ld_b + chunk(i);
-    auto fill = [&](uint32_t step, uint8_t *a, uint8_t *b) {
-        const Base from(base_a + (uint64_t)step * 128, step < steps), from2(base_b + (uint64_t)step * 128, step < steps);
-        // chunks behind K lie outside the buffer, and arrive as zeroes
-        const uint32_t left = p.K - step * 128, out0 = chunk(0) < left ? 0 : kOutside, out1 = chunk(1) < left ? 0 : kOutside;
+    // chunks behind K lie outside the buffer, and arrive as zeroes
+    auto fill_a = [&](uint32_t step, uint8_t *a) {
+        const Base from(base_a + (uint64_t)step * 128, step < steps);
+        const uint32_t left = K - step * 128, out0 = chunk(0) < left ? 0 : kOutside, out1 = chunk(1) < left ? 0 : kOutside;
 #pragma unroll
         for (int i = 0; i < kCopiesA; ++i) copy_to_lds(from, from_a[i] | (i % 2 ? out1 : out0), a + (wave * kCopiesA + i) * 1024);
+    };
+    auto fill_b = [&](uint32_t step, uint8_t *b) {
+        const Base from(base_b + (uint64_t)step * 128, step < steps);
+        const uint32_t left = K - step * 128, out0 = chunk(0) < left ? 0 : kOutside, out1 = chunk(1) < left ? 0 : kOutside;
 #pragma unroll
-        for (int i = 0; i < kCopiesB; ++i) copy_to_lds(from2, from_b[i] | (i % 2 ? out1 : out0), b + (wave * kCopiesB + i) * 1024);
+        for (int i = 0; i < kCopiesB; ++i) copy_to_lds(from, from_b[i] | (i % 2 ? out1 : out0), b + (wave * kCopiesB + i) * 1024);
     };
     auto read = [&](i32x8 (&a)[MT], i32x8 (&b)[NT], const uint8_t *from_a, const uint8_t *from_b, int s) {
         a[0] = operand(from_a, wm, s, lane);                 // in the order of their use
@@ -336,7 +446,7 @@ __global__ __launch_bounds__(256, MT * NT >= 16 ? 1 : 2) void k_product(ProductA
     uint32_t sa[MT], sb[NT], next_sa[MT], next_sb[NT];
     const uint32_t last_word = (p.K - 1) / 512;
     auto words = [&](uint32_t w) {
-        w = min(w, last_word);
+        w = min(start / 4 + w, last_word);
 #pragma unroll
         for (int i = 0; i < MT; ++i) next_sa[i] = (p.sa + w * p.ld_sa)[min(m0 + wm + i * 32 + (lane & 31), p.M - 1)];
 #pragma unroll
@@ -348,48 +458,67 @@ __global__ __launch_bounds__(256, MT * NT >= 16 ? 1 : 2) void k_product(ProductA
 #pragma unroll
         for (int i = 0; i < NT; ++i) sb[i] = next_sb[i];
     };
-    auto multiply_all = [&](const i32x8 (&ra)[MT], const i32x8 (&rb)[NT], int shift) {
+    auto multiply_all = [&](const i32x8 (&ra)[MT], const i32x8 (&rb)[NT]) {
         Operand<FA, EXACT> a[MT];
         Operand<FB, EXACT> b[NT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) a[i].take(ra[i], sa[i] >> shift);
+        for (int i = 0; i < MT; ++i) a[i].take(ra[i], sa[i]);
 #pragma unroll
-        for (int i = 0; i < NT; ++i) b[i].take(rb[i], sb[i] >> shift);
+        for (int i = 0; i < NT; ++i) b[i].take(rb[i], sb[i]);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j) acc[i][j] = multiply<FA, FB>(b[j], a[i], acc[i][j]);
+        // The products stay on this side of what follows: nothing else holds them, and behind it they would keep their operands'
+        // registers.
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                if constexpr (kWhole) asm volatile("" : "+a"(acc[i][j]));
+                else asm volatile("" : "+v"(acc[i][j]));
     };
 
-    fill(0, ta0, tb0);
-    fill(1, ta1, tb1);
+    fill_a(0, ta0);
+    fill_b(0, tb0);
+    fill_a(1, ta1);
+    fill_b(1, tb1);
     words(0);
-    take_words();
     meet<0>();
     i32x8 a0[MT], b0[NT], a1[MT], b1[NT];
     read(a0, b0, ta0, tb0, 0);
-    // Half a step multiplies what half a step ago was read from LDS, while the next half is read; between a step's halves its tile
-    // has been read by all and the next one's has arrived, so that the one after next is fetched into its place.  A word
-    // of scales serves four steps.
-    for (uint32_t step = 0; step < steps; step += 4) {
-        words(step / 4 + 1);
+    // Half a step multiplies what half a step ago was read from LDS, while the next half is read.  Between a step's halves its
+    // tiles have been read by all and the next step's have arrived; the ones after those are fetched all the time, A's in a step's
+    // first half (into a third place), B's in the second: a half's copies more in flight than with two places each, and no more
+    // at once than the way from the L2 takes (8192 x 28672 x 8192: 1460 -> 1360 us).  A word of scales serves four steps.
+    for (uint32_t step = 0; step < steps; step += 6) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (step + j >= steps) break;
-            read(a1, b1, ta[j % 2], tb[j % 2], 1);
-            multiply_all(a0, b0, j * 8);
-            interleave<kProducts, 2 * (MT + NT), 0>();
-            meet<0>();
-            fill(step + j + 2, ta[j % 2], tb[j % 2]);
-            read(a0, b0, ta[(j + 1) % 2], tb[(j + 1) % 2], 0);
-            multiply_all(a1, b1, j * 8);
-            interleave<kProducts, 2 * (MT + NT), kCopies>();
+        for (int j = 0; j < 6; ++j) {
+            const uint32_t at = step + j;
+            if (at >= steps) break;
+            if (at % 4 == 0) {
+                take_words();
+                words(at / 4 + 1);
+            }
             __builtin_amdgcn_sched_barrier(0);
+            fill_a(at + 2, ta[(j + 2) % 3]);
+            read(a1, b1, ta[j % 3], tb[j % 2], 1);
+            multiply_all(a0, b0);
+            interleave<kProducts, 2 * (MT + NT), kCopiesA>();
+            meet<kCopiesA>();
+            fill_b(at + 2, tb[j % 2]);
+            read(a0, b0, ta[(j + 1) % 3], tb[(j + 1) % 2], 0);
+            multiply_all(a1, b1);
+            interleave<kProducts, 2 * (MT + NT), kCopiesB>();
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) sa[i] >>= 8;
+#pragma unroll
+            for (int i = 0; i < NT; ++i) sb[i] >>= 8;
         }
-        take_words();
     }
-    if (p.K % 16) {                                          // the rest of K, with zeroes behind it: through registers
-        const uint32_t left = p.K - steps * 128;
+    if (p.K % 16 && (kWhole || blockIdx.y + 1 == p.splits)) {        // the rest of K, with zeroes behind it: through registers
+        const uint32_t left = K - steps * 128;
         meet<0>();
 #pragma unroll 1
         for (int r = tid >> 3; r < kRowsA + kRowsB; r += 32) {
@@ -400,48 +529,135 @@ __global__ __launch_bounds__(256, MT * NT >= 16 ? 1 : 2) void k_product(ProductA
         }
         words(last_word);
         take_words();
+#pragma unroll
+        for (int i = 0; i < MT; ++i) sa[i] >>= steps % 4 * 8;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) sb[i] >>= steps % 4 * 8;
         meet<0>();
 #pragma unroll 1
         for (int s = 0; s < 2; ++s) {
             read(a0, b0, ta0, tb0, s);
-            multiply_all(a0, b0, steps % 4 * 8);
+            multiply_all(a0, b0);
         }
     }
-    constexpr int kParts = 4 / sizeof(T);
     uint8_t *const room = (wave & 2 ? ta1 : ta0) + (wave & 1) * 4096;
+    const uint32_t m = m0 + wm, n = n0 + wn;
     meet<0>();
-    if (m0 + kRowsA <= p.M && n0 + kRowsB <= p.N) {
+    if (!kWhole && sizeof(T) == 4 && p.splits > 1) store_all((T *)p.parts + (uint64_t)blockIdx.y * p.M * p.N, p.N, p, room, m, n, lane, acc);
+    else store_all((T *)p.c, p.ld_c, p, room, m, n, lane, acc);
+}
+
+// C from the parts of K, added in their order; four neighbouring columns a thread.
+template <typename T> __global__ __launch_bounds__(256) void k_add_parts(ProductArgs p)
+{
+    const uint32_t wide = (p.N + 3) / 4;
+    const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x, m = id / wide, n = id % wide * 4;
+    if (m >= p.M) return;
+    const int count = (int)min((uint64_t)4, p.N - n);
+    float v[4] = {};
+#pragma unroll 4
+    for (uint32_t s = 0; s < p.splits; ++s) {
+        const float *from = p.parts + ((uint64_t)s * p.M + m) * p.N + n;
+        if (count == 4) {
+            const w32x4 w = *(const w32x4_any *)from;
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+            for (int i = 0; i < 4; ++i) v[i] += __uint_as_float(w[i]);
+        } else {
 #pragma unroll
-            for (int j = 0; j < NT; j += kParts)
-                store_rows<T, kParts, true>(p, room, m0 + wm + i * 32, n0 + wn + j * 32, lane, &acc[i][j]);
+            for (int i = 0; i < 4; ++i)
+                if (i < count) v[i] += from[i];
+        }
+    }
+    T *c = (T *)p.c + m * p.ld_c + n;
+    union { T t[4]; w32x2 w2; w32x4 w4; } u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u.t[i] = narrow<T>(v[i]);
+    if (count == 4) {
+        if constexpr (sizeof(T) == 4) *(w32x4_any *)c = u.w4;
+        else *(w32x2_any *)c = u.w2;
     } else {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; j += kParts)
-                store_rows<T, kParts, false>(p, room, m0 + wm + i * 32, n0 + wn + j * 32, lane, &acc[i][j]);
+        for (int i = 0; i < 4; ++i)
+            if (i < count) c[i] = u.t[i];
     }
+}
+
+// Which tiles, and into how many parts K is cut where they are too few for the 256 compute units.
+struct Shape {
+    int tile;                      // 0: 64 x 128, 1: 128 x 128, 2: 256 x 256
+    uint32_t splits, split_steps;
+};
+constexpr uint64_t kMaxParts = 64ull << 20;            // bytes of the workspace
+
+// Time goes by the tiles that fall to a compute unit, which runs two of 128 x 128 at once or one of 256 x 256; one of these takes
+// three of those (measured at N x K = 11008 x 4096, us for 128 and 256: M = 512 29 and 41, 768 47 and 42, 1280 61 and 50, 1536 76
+// and 88, 2560 113 and 101; 5120 x 13824: M = 1536 112 and 136, 2048 185 and 139, 3200 218 and 269).  K is cut where there are
+// at most half as many tiles as units (M = 128 and 512 of 4096 x 11008: 46 -> 21, 46 -> 33; one in two of 512 places: 46 -> 44).
+static Shape shape_of(uint64_t M, uint64_t N, uint64_t K)
+{
+    Shape t;
+    const uint64_t big = (M + 255) / 256 * ((N + 255) / 256), small = (M + 127) / 128 * ((N + 127) / 128), steps = (K + 127) / 128;
+    t.tile = M <= 64 ? 0 : 3 * ((big + 255) / 256) <= (small + 255) / 256 ? 2 : 1;
+    t.splits = 1;
+    t.split_steps = (uint32_t)((steps + 3) / 4 * 4);
+    if (M <= 16 || t.tile == 2) return t;
+    const uint64_t tiles = t.tile == 0 ? (N + 127) / 128 : small;
+    const uint64_t want = std::min((t.tile == 0 ? 512 : 256) / tiles, std::min(steps / 8, kMaxParts / (M * N * 4)));
+    if (want < 2) return t;
+    t.split_steps = (uint32_t)(((steps + want - 1) / want + 3) / 4 * 4);
+    t.splits = (uint32_t)((steps + t.split_steps - 1) / t.split_steps);
+    return t;
+}
+
+// Rows on 16 bytes, so that chunks are; offsets inside a tile are held in 32 bits.
+static bool on_16_bytes(const ProductArgs &p)
+{
+    return p.K && ((uintptr_t)p.a | (uintptr_t)p.b | p.ld_a | p.ld_b) % 16 == 0 && p.ld_a < (1u << 23) && p.ld_b < (1u << 23);
 }
 
 template <int FA, int FB, int MT, int NT> static hipError_t launch_tiles(const ProductArgs &p, hipStream_t s)
 {
-    const uint64_t tiles = (uint64_t)((p.M + 64 * MT - 1) / (64 * MT)) * ((p.N + 64 * NT - 1) / (64 * NT));
-    if (p.c_type == REFT_F32) k_product<FA, FB, float, MT, NT><<<(uint32_t)tiles, 256, 0, s>>>(p);
-    else if (p.c_type == REFT_BF16) k_product<FA, FB, bf16, MT, NT><<<(uint32_t)tiles, 256, 0, s>>>(p);
-    else k_product<FA, FB, f16, MT, NT><<<(uint32_t)tiles, 256, 0, s>>>(p);
+    const dim3 grid((p.M + 64 * MT - 1) / (64 * MT) * ((p.N + 64 * NT - 1) / (64 * NT)), p.splits);
+    if (p.c_type == REFT_F32) {
+        k_product<FA, FB, true, float, MT, NT><<<grid, 256, 0, s>>>(p);
+    } else if (p.splits > 1) {
+        if constexpr (MT * NT < 16) k_product<FA, FB, false, float, MT, NT><<<grid, 256, 0, s>>>(p);
+        else return hipErrorInvalidValue;                    // shape_of cuts K for the smaller tiles only
+    } else if (p.c_type == REFT_BF16) {
+        k_product<FA, FB, false, bf16, MT, NT><<<grid, 256, 0, s>>>(p);
+    } else {
+        k_product<FA, FB, false, f16, MT, NT><<<grid, 256, 0, s>>>(p);
+    }
+    if (p.splits > 1) {
+        const uint32_t blocks = (uint32_t)(((uint64_t)p.M * ((p.N + 3) / 4) + 255) / 256);
+        if (p.c_type == REFT_F32) k_add_parts<float><<<blocks, 256, 0, s>>>(p);
+        else if (p.c_type == REFT_BF16) k_add_parts<bf16><<<blocks, 256, 0, s>>>(p);
+        else k_add_parts<f16><<<blocks, 256, 0, s>>>(p);
+    }
+    return hipGetLastError();
+}
+
+template <int FA, int FB, int MT> static hipError_t launch_few(const ProductArgs &p, hipStream_t s)
+{
+    const uint32_t grid = (p.N + 15) / 16;
+    if (p.c_type == REFT_F32) k_product_few<FA, FB, true, MT, 8><<<grid, 512, 0, s>>>(p);
+    else k_product_few<FA, FB, false, MT, 8><<<grid, 512, 0, s>>>(p);
     return hipGetLastError();
 }
 
 template <int FA, int FB> static hipError_t launch_product(const ProductArgs &p, hipStream_t s)
 {
-    const bool on16 = ((uintptr_t)p.a | (uintptr_t)p.b | p.ld_a | p.ld_b) % 16 == 0;
-    // offsets inside a tile are held in 32 bits
-    if (on16 && p.K && p.ld_a < (1u << 23) && p.ld_b < (1u << 23)) {
-        const uint64_t big = (uint64_t)((p.M + 255) / 256) * ((p.N + 255) / 256);
-        if (big >= 192) return launch_tiles<FA, FB, 4, 4>(p, s);
-        return launch_tiles<FA, FB, 2, 2>(p, s);
+    if (p.M <= 16) return launch_few<FA, FB, 1>(p, s);
+    if (on_16_bytes(p)) {
+        const Shape t = shape_of(p.M, p.N, p.K);
+        ProductArgs q = p;
+        q.splits = t.splits;
+        q.split_steps = t.split_steps;
+        switch (t.tile) {
+        case 2: return launch_tiles<FA, FB, 4, 4>(q, s);
+        case 1: return launch_tiles<FA, FB, 2, 2>(q, s);
+        default: return launch_tiles<FA, FB, 1, 2>(q, s);
+        }
     }
     const dim3 grid((p.N + 127) / 128, (p.M + 127) / 128);
     if (p.c_type == REFT_F32) k_product_any<FA, FB, true><<<grid, 256, 0, s>>>(p);
@@ -455,10 +671,9 @@ using namespace reft;
 
 extern "C" uint64_t reft_product_workspace(uint64_t M, uint64_t N, uint64_t K)
 {
-    (void)M;
-    (void)N;
-    (void)K;
-    return 0;
+    if (!M || !N || !K || M > 128 * 65535 || N > 0x7fffffff || K > 0x7fffffff) return 0;
+    const Shape t = shape_of(M, N, K);
+    return t.splits > 1 ? t.splits * M * N * sizeof(float) : 0;
 }
 
 extern "C" int reft_product(const void *a, uint64_t ld_a, int a_format, const void *a_scales, uint64_t ld_as, const void *b,
@@ -501,6 +716,9 @@ extern "C" int reft_product(const void *a, uint64_t ld_a, int a_format, const vo
     p.b_shift = b_blocks ? 7 : 0;
     p.c = c;
     p.c_type = c_dtype;
+    p.splits = 1;
+    p.split_steps = 0;
+    p.parts = (float *)workspace;
     hipStream_t s = (hipStream_t)stream;
     hipError_t e;
     if (a_format == REFT_E4M3) e = b_format == REFT_E4M3 ? launch_product<0, 0>(p, s) : launch_product<0, 1>(p, s);
