@@ -41,7 +41,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_dropout(DropoutAr
         group[u] = at - r * groups;
         const uint64_t left = a.cols - (uint64_t)group[u] * 8;
         n[u] = first + local < a.total ? (int)(left < 8 ? left : 8) : 0;
-        load8((const T *)a.x + (uint64_t)row[u] * a.ld_x + (uint64_t)group[u] * 8, n[u], v[u]);
+        load8<true>((const T *)a.x + (uint64_t)row[u] * a.ld_x + (uint64_t)group[u] * 8, n[u], v[u]);
     }
 #pragma unroll
     for (int u = 0; u < kDropUnroll; ++u) {
@@ -73,68 +73,77 @@ struct NormForward {
 
 __device__ __forceinline__ float wave_sum(float v)
 {
-#pragma unroll
-    for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
+    v = sum_of_16(v);
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+// The sum over a row's waves, added in their order.  room: a place for each wave of the block; all of the block calls.
+__device__ __forceinline__ float row_sum(float v, float *room)
+{
+    const int waves = blockDim.x / 64;
+    v = wave_sum(v);
+    if (waves == 1) return v;
+    float *mine = room + threadIdx.y * waves;
+    if ((threadIdx.x & 63) == 0) mine[threadIdx.x / 64] = v;
+    __syncthreads();
+    v = 0;
+    for (int i = 0; i < waves; ++i) v += mine[i];
     return v;
 }
 
-// A row belongs to NW waves (four rows a block where that is one), each lane holds V times eight neighbouring columns
-// of it in registers, in fp32: one pass over the inputs whatever the row's length.  A wave's 512 columns are four
-// blocks of 128, 16 lanes each: one word of scales.
-template <typename T, typename R, int NW, int V>
-__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_forward(NormForward a)
+// A row belongs to the threads of one y (64 to 1024 of them); each holds V times eight neighbouring columns of it in registers: one
+// pass over the inputs whatever the row's length.  A wave's 512 columns are four blocks of 128, 16 lanes each: one word of scales.
+template <typename T, typename R, int V> __global__ __launch_bounds__(1024) void k_norm_forward(NormForward a)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t row = NW == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
-    if (row >= a.rows) return;
-    const int first = (NW == 1 ? 0 : wave * 512) + lane * 8, cols = (int)a.cols;
-    float h[V][8], sum = 0;
+    __shared__ float room[16];
+    const int lane = threadIdx.x & 63, first = threadIdx.x * 8, wide = blockDim.x * 8, cols = (int)a.cols;
+    const uint32_t row = blockIdx.x * blockDim.y + threadIdx.y;
+    const bool there = row < a.rows;
+    constexpr bool kAhead = V <= 2;                          // all is asked for at once, as far as registers go
+    Eight<T> x[V];
+    Eight<R> r[V];
+    float h[V][8], w[V][8], sum = 0;
+    auto fetch = [&](int v) {
+        const int c = first + v * wide, n = there ? cols - c : 0;
+        x[v].template load<false>((const T *)a.x + row * a.ld_x + c, n);
+        r[v].template load<false>((const R *)a.residual + row * a.ld_r + c, a.residual ? n : 0);
+        if (kAhead) load8_of<T>(a.weight, a.weight_f32, c, a.weight ? n : 0, w[v]);
+    };
+    if (kAhead)
+#pragma unroll
+        for (int v = 0; v < V; ++v) fetch(v);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int c = first + v * NW * 512;
-        load8((const T *)a.x + row * a.ld_x + c, cols - c, h[v]);
-    }
+        if (!kAhead) fetch(v);
+        const int c = first + v * wide, n = there ? cols - c : 0;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int c = first + v * NW * 512;
-        float r[8] = {};
-        if (a.residual) load8((const R *)a.residual + row * a.ld_r + c, cols - c, r);
+        for (int i = 0; i < 8; ++i) h[v][i] = x[v][i];
         if (a.d.threshold) drop8(a.d, row, (uint32_t)c / 8, h[v]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            h[v][i] += r[i];
+            h[v][i] += r[v][i];
             sum += h[v][i] * h[v][i];
         }
-        if (a.h) store8((R *)a.h + row * a.ld_h + c, cols - c, h[v]);
+        if (a.h) store8((R *)a.h + row * a.ld_h + c, n, h[v]);
     }
-    sum = wave_sum(sum);
-    if constexpr (NW > 1) {
-        __shared__ float part[NW];
-        if (lane == 0) part[wave] = sum;
-        __syncthreads();
-        sum = 0;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) sum += part[i];
-    }
-    const float rstd = 1.f / sqrtf(sum / (float)cols + a.eps);
-    if (a.rstd && lane == 0 && (NW == 1 || wave == 0)) a.rstd[row] = rstd;
+    const float rstd = 1.f / sqrtf(row_sum(sum, room) / (float)cols + a.eps);
+    if (!there) return;
+    if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
     if (!a.y && !a.q) return;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int c = first + v * NW * 512;
-        float w[8];
-        load8_of<T>(a.weight, a.weight_f32, c, cols - c, w);
+        const int c = first + v * wide;
+        if (!kAhead) load8_of<T>(a.weight, a.weight_f32, c, cols - c, w[v]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] *= h[v][i] * rstd;
-        if (a.y) store8((T *)a.y + row * a.ld_y + c, cols - c, w);
+        for (int i = 0; i < 8; ++i) w[v][i] *= h[v][i] * rstd;
+        if (a.y) store8((T *)a.y + row * a.ld_y + c, cols - c, w[v]);
         if (a.q) {
             uint32_t most = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) most = max(most, magnitude(w[i]));
-#pragma unroll
-            for (int m = 8; m; m >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, m));
-            const uint32_t e = scale_of(most, top_of(a.e5m2));
-            store8_bytes(a.q + row * a.ld_q + c, cols - c, to_eight(w, inverse_of(e), a.e5m2));
+            for (int i = 0; i < 8; ++i) most = max(most, magnitude(w[v][i]));
+            const uint32_t e = scale_of(max_of_16(most), top_of(a.e5m2));
+            store8_bytes(a.q + row * a.ld_q + c, cols - c, to_eight(w[v], inverse_of(e), a.e5m2));
             const int word = c / 512;                       // the same in the whole wave
             if ((lane & 15) == 0 && word * 512 < cols)
                 a.scales[(word * a.ld_s + row) * 4 + lane / 16] = c < cols ? (uint8_t)e : 127;
@@ -146,93 +155,126 @@ struct NormBackward {
     const void *dy, *dh, *h, *weight;
     const float *rstd;
     uint64_t ld_dy, ld_dh, ld_h;
-    uint32_t rows, cols, workers;
+    uint32_t rows, cols;
     Dropout d;
     void *dres, *dx;
     uint64_t ld_dres, ld_dx;
-    float *part;                   // [workers][cols]
+    float *part;                   // [blocks][cols]
     uint8_t weight_f32;
 };
 
-// A worker (a block, or a wave where a row is a wave's) takes rows worker, worker + workers, ..., and keeps its part of
-// the weight's gradient in registers; k_sum_parts adds the workers' parts in their order.
-template <typename T, typename R, int NW, int V>
-__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_backward(NormBackward a)
+// Rows as above.  A block takes every so manyth row (or, of short rows, blockDim.y of them) and keeps its part of the weight's
+// gradient in registers; k_sum_parts adds the blocks' parts in their order.  Of rows with more than eight columns a lane the operands
+// are read again for the second half of the work (from the L2) rather than held.
+template <typename T, typename R, int V> __global__ __launch_bounds__(1024) void k_norm_backward(NormBackward a)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t worker = NW == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
-    if (worker >= a.workers) return;
-    const int first = (NW == 1 ? 0 : wave * 512) + lane * 8, cols = (int)a.cols;
-    __shared__ float part[2][NW];
-    float dw[V][8] = {};
+    __shared__ float room[2][16];
+    __shared__ float fold[V == 1 ? 3 * 512 : 1];
+    const int first = threadIdx.x * 8, wide = blockDim.x * 8, cols = (int)a.cols;
+    const uint32_t step = gridDim.x * blockDim.y;
+    constexpr bool kHeld = V <= 2;                           // the weights
+    float dw[V][8] = {}, w[V][8];
+    auto fetch_w = [&](int v) {
+        load8_of<T>(a.weight, a.weight_f32, first + v * wide, cols - first - v * wide, w[v]);
+    };
+    if (kHeld)
+#pragma unroll
+        for (int v = 0; v < V; ++v) fetch_w(v);
+    Eight<T> dy[V], next_dy;
+    Eight<R> h[V], dh[V], next_h, next_dh;
+    float rstd, next_rstd;
+    auto fetch = [&](int v, uint32_t row) {
+        const int c = first + v * wide, n = row < a.rows ? cols - c : 0;
+        h[v].template load<false>((const R *)a.h + row * a.ld_h + c, n);
+        dy[v].template load<false>((const T *)a.dy + row * a.ld_dy + c, n);
+    };
+    auto fetch_dh = [&](int v, uint32_t row) {
+        const int c = first + v * wide, n = row < a.rows ? cols - c : 0;
+        dh[v].template load<false>((const R *)a.dh + row * a.ld_dh + c, a.dh ? n : 0);
+    };
+    auto fetch_next = [&](uint32_t row) {
+        const int n = row < a.rows ? cols - first : 0;
+        next_h.template load<true>((const R *)a.h + row * a.ld_h + first, n);
+        next_dy.template load<true>((const T *)a.dy + row * a.ld_dy + first, n);
+        next_dh.template load<true>((const R *)a.dh + row * a.ld_dh + first, a.dh ? n : 0);
+        next_rstd = row < a.rows ? a.rstd[row] : 0.f;
+    };
+    if (V == 1) fetch_next(blockIdx.x * blockDim.y + threadIdx.y);
     int half = 0;
-    for (uint32_t row = worker; row < a.rows; row += a.workers, half ^= 1) {
-        float x[V][8], g[V][8], dot = 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = first + v * NW * 512;
-            load8((const R *)a.h + row * a.ld_h + c, cols - c, x[v]);
-            load8((const T *)a.dy + row * a.ld_dy + c, cols - c, g[v]);
+    for (uint32_t base = blockIdx.x * blockDim.y; base < a.rows; base += step, half ^= 1) {
+        const uint32_t row = base + threadIdx.y;
+        const bool there = row < a.rows;
+        float dot = 0;
+        if (V == 1) {
+            h[0] = next_h;
+            dy[0] = next_dy;
+            dh[0] = next_dh;
+            rstd = next_rstd;
+            if (base + step < a.rows) fetch_next(row + step);
+        } else {
+            rstd = there ? a.rstd[row] : 0.f;
         }
-        const float rstd = a.rstd[row];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int c = first + v * NW * 512;
-            float w[8];
-            load8_of<T>(a.weight, a.weight_f32, c, cols - c, w);
+            if (V > 1) fetch(v, row);
+            if (!kHeld) fetch_w(v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                x[v][i] *= rstd;
-                dw[v][i] += g[v][i] * x[v][i];
-                g[v][i] *= w[i];
-                dot += g[v][i] * x[v][i];
+                const float part = dy[v][i] * (h[v][i] * rstd);
+                dw[v][i] += part;
+                dot += part * w[v][i];
             }
+            if (!kHeld) asm volatile("" ::: "memory");       // eight columns at a time: registers
         }
-        dot = wave_sum(dot);
-        if constexpr (NW > 1) {
-            if (lane == 0) part[half][wave] = dot;
-            __syncthreads();       // the other half is written before the next one, and read after it
-            dot = 0;
-#pragma unroll
-            for (int i = 0; i < NW; ++i) dot += part[half][i];
-        }
-        dot /= (float)cols;
+        dot = row_sum(dot, room[half]) / (float)cols;        // this half is written again two rows on, behind another barrier
+        if (!there) continue;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int c = first + v * NW * 512;
-            float r[8] = {};
-            if (a.dh) load8((const R *)a.dh + row * a.ld_dh + c, cols - c, r);
+            const int c = first + v * wide;
+            float o[8];
+            if (V > 1) fetch(v, row), fetch_dh(v, row);
+            if (!kHeld) fetch_w(v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[i] += rstd * (g[v][i] - x[v][i] * dot);
-            if (a.dres) store8((R *)a.dres + row * a.ld_dres + c, cols - c, r);
+            for (int i = 0; i < 8; ++i) o[i] = dh[v][i] + rstd * (dy[v][i] * w[v][i] - h[v][i] * rstd * dot);
+            if (a.dres) store8((R *)a.dres + row * a.ld_dres + c, cols - c, o);
             if (a.dx) {
-                if (a.d.threshold) drop8(a.d, row, (uint32_t)c / 8, r);
-                store8((T *)a.dx + row * a.ld_dx + c, cols - c, r);
+                if (a.d.threshold) drop8(a.d, row, (uint32_t)c / 8, o);
+                store8((T *)a.dx + row * a.ld_dx + c, cols - c, o);
             }
+            if (!kHeld) asm volatile("" ::: "memory");
         }
     }
-    if (a.part) {
+    if (!a.part) return;
+    if (V == 1 && blockDim.y > 1) {                          // (64, 4) or (128, 2) threads: at most 3 times 512 sums to fold
+        if (threadIdx.y > 0)
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = first + v * NW * 512;
-            store8(a.part + (uint64_t)worker * a.cols + c, cols - c, dw[v]);
-        }
+            for (int i = 0; i < 8; ++i) fold[(threadIdx.y - 1) * wide + first + i] = dw[0][i];
+        __syncthreads();
+        if (threadIdx.y > 0) return;
+        for (uint32_t y = 1; y < blockDim.y; ++y)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dw[0][i] += fold[(y - 1) * wide + first + i];
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int c = first + v * wide;
+        store8(a.part + (uint64_t)blockIdx.x * a.cols + c, cols - c, dw[v]);
     }
 }
 
-// out[c] = sum of n rows of part, in an order that depends on n alone: 16 interleaved sums, then those one after the other.
+// out[c] = sum of n rows of part, in an order that depends on n alone: 64 interleaved sums, then those one after the other.
 __global__ __launch_bounds__(1024) void k_sum_parts(const float *part, uint32_t n, uint32_t cols, float *out)
 {
-    __shared__ float sums[16][64];
-    const uint32_t x = threadIdx.x & 63, y = threadIdx.x >> 6, c = blockIdx.x * 64 + x;
+    __shared__ float sums[64][16];
+    const uint32_t x = threadIdx.x & 15, y = threadIdx.x >> 4, c = blockIdx.x * 16 + x;
     float s = 0;
     if (c < cols)
-        for (uint32_t i = y; i < n; i += 16) s += part[(uint64_t)i * cols + c];
+#pragma unroll 4
+        for (uint32_t i = y; i < n; i += 64) s += part[(uint64_t)i * cols + c];
     sums[y][x] = s;
     __syncthreads();
     if (y == 0 && c < cols) {
-#pragma unroll
-        for (int i = 1; i < 16; ++i) s += sums[i][x];
+        for (int i = 1; i < 64; ++i) s += sums[i][x];
         out[c] = s;
     }
 }
@@ -256,13 +298,11 @@ template <typename T> __global__ __launch_bounds__(256) void k_quantize_rows(Qua
     if (row >= a.rows) return;
     const int n = c >= a.cols ? 0 : (int)min(a.cols - c, (uint64_t)8);
     float v[8];
-    load8((const T *)a.x + row * a.ld_x + c, n, v);
+    load8<false>((const T *)a.x + row * a.ld_x + c, n, v);
     uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[i]));
-#pragma unroll
-    for (int m = 8; m; m >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, m));
-    const uint32_t e = scale_of(most, top_of(a.e5m2));
+    const uint32_t e = scale_of(max_of_16(most), top_of(a.e5m2));
     store8_bytes(a.q + row * a.ld_q + c, n, to_eight(v, inverse_of(e), a.e5m2));
     if ((lane & 15) == 0) a.scales[((uint64_t)blockIdx.y * a.ld_s + row) * 4 + lane / 16] = n ? (uint8_t)e : 127;
 }
@@ -285,32 +325,49 @@ template <typename T, bool BLOCKS> __global__ __launch_bounds__(256) void k_quan
     __shared__ __align__(16) uint8_t tile[16 * kPitch];
     __shared__ uint32_t most_of[4][128];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, tc = tid & 15, tr = tid >> 4;
-    const uint64_t row0 = (uint64_t)blockIdx.x * 128, col0 = (uint64_t)blockIdx.y * 128;
+    const uint32_t high = (uint32_t)((a.rows + 127) / 128), wide = (uint32_t)((a.cols + 127) / 128);
+    const uint32_t down = blockIdx.x / wide, along = blockIdx.x % wide;
+    const uint64_t row0 = (uint64_t)down * 128, col0 = (uint64_t)along * 128;
     const int rows = (int)min(a.rows - row0, (uint64_t)128), cols = (int)min(a.cols - col0, (uint64_t)128);
-    float v[8][8];
+    Eight<T> v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        load8((const T *)a.x + (row0 + tr * 8 + i) * a.ld_x + col0 + tc * 8, tr * 8 + i < rows ? cols - tc * 8 : 0, v[i]);
+        v[i].template load<false>((const T *)a.x + (row0 + tr * 8 + i) * a.ld_x + col0 + tc * 8, tr * 8 + i < rows ? cols - tc * 8 : 0);
+    // The values are widened anew for each use: as they lie they take half the registers.
+    auto forget = [&]() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(T) / 2; ++k) asm volatile("" : "+v"(v[i].w[k]));
+    };
     const int top = top_of(a.e5m2);
     uint32_t by_col[8] = {};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) by_col[j] = max(by_col[j], magnitude(v[i][j]));
+    forget();
     uint32_t e_tile = 0;
     if constexpr (BLOCKS) {
         uint32_t m = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = max(m, by_col[j]);
-#pragma unroll
-        for (int s = 32; s; s >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, s));
+        m = max_of_16(m);
+        m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+        m = max(m, (uint32_t)__shfl_xor((int)m, 32));
         if (lane == 0) most_of[wave][0] = m;
         __syncthreads();
         e_tile = scale_of(max(max(most_of[0][0], most_of[1][0]), max(most_of[2][0], most_of[3][0])), top);
         if (tid == 0) {
-            const uint64_t high = (a.rows + 127) / 128, wide = (a.cols + 127) / 128;
-            if (a.q) store_scale(a.scales, a.ld_s, blockIdx.x, blockIdx.y, wide, e_tile);
-            if (a.q_t) store_scale(a.scales_t, a.ld_st, blockIdx.y, blockIdx.x, high, e_tile);
+            if (a.q) store_scale(a.scales, a.ld_s, down, along, wide, e_tile);
+            if (a.q_t) store_scale(a.scales_t, a.ld_st, along, down, high, e_tile);
+        }
+    } else if (a.q_t) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            by_col[j] = max(by_col[j], (uint32_t)__shfl_xor((int)by_col[j], 16));
+            by_col[j] = max(by_col[j], (uint32_t)__shfl_xor((int)by_col[j], 32));
+            if (lane < 16) most_of[wave][tc * 8 + j] = by_col[j];
         }
     }
     if (a.q) {
@@ -318,35 +375,29 @@ template <typename T, bool BLOCKS> __global__ __launch_bounds__(256) void k_quan
         for (int i = 0; i < 8; ++i) {
             uint32_t e = e_tile;
             const int r = tr * 8 + i;
+            float t[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t[j] = v[i][j];
             if constexpr (!BLOCKS) {
                 uint32_t m = 0;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) m = max(m, magnitude(v[i][j]));
-#pragma unroll
-                for (int s = 8; s; s >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, s));
-                e = scale_of(m, top);
-                if (tc == 0 && r < rows) store_scale(a.scales, a.ld_s, row0 + r, blockIdx.y, (a.cols + 127) / 128, e);
+                for (int j = 0; j < 8; ++j) m = max(m, magnitude(t[j]));
+                e = scale_of(max_of_16(m), top);
+                if (tc == 0 && r < rows) store_scale(a.scales, a.ld_s, row0 + r, along, wide, e);
             }
-            if (r < rows) store8_bytes(a.q + (row0 + r) * a.ld_q + col0 + tc * 8, cols - tc * 8, to_eight(v[i], inverse_of(e), a.e5m2));
+            if (r < rows) store8_bytes(a.q + (row0 + r) * a.ld_q + col0 + tc * 8, cols - tc * 8, to_eight(t, inverse_of(e), a.e5m2));
         }
     }
     if (!a.q_t) return;
-    if constexpr (!BLOCKS) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            by_col[j] = max(by_col[j], (uint32_t)__shfl_xor((int)by_col[j], 16));
-            by_col[j] = max(by_col[j], (uint32_t)__shfl_xor((int)by_col[j], 32));
-            if (lane < 16) most_of[wave][tc * 8 + j] = by_col[j];
-        }
-        __syncthreads();
-    }
+    if constexpr (!BLOCKS) __syncthreads();
+    forget();
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         uint32_t e = e_tile;
         const int c = tc * 8 + j;
         if constexpr (!BLOCKS) {
             e = scale_of(max(max(most_of[0][c], most_of[1][c]), max(most_of[2][c], most_of[3][c])), top);
-            if (tr == 0 && c < cols) store_scale(a.scales_t, a.ld_st, col0 + c, blockIdx.x, (a.rows + 127) / 128, e);
+            if (tr == 0 && c < cols) store_scale(a.scales_t, a.ld_st, col0 + c, down, high, e);
         }
         float t[8];
 #pragma unroll
@@ -361,7 +412,7 @@ template <typename T, bool BLOCKS> __global__ __launch_bounds__(256) void k_quan
         const w32x4 w = *(const w32x4 *)(tile + (c / 8) * kPitch + (c % 8) * 128 + r);
         uint8_t *p = a.q_t + (col0 + c) * a.ld_qt + row0 + r;
         if (r + 16 <= rows) {
-            *(w32x4_any *)p = w;
+            __builtin_nontemporal_store(w, (w32x4_any *)p);
         } else {
             for (int i = 0; i < rows - r; ++i) p[i] = tile[(c / 8) * kPitch + (c % 8) * 128 + r + i];
         }
@@ -371,52 +422,42 @@ template <typename T, bool BLOCKS> __global__ __launch_bounds__(256) void k_quan
 // ------------------------------------------------------------------------------------------------
 // which kernel
 // ------------------------------------------------------------------------------------------------
-// Waves that share a row and columns that a lane holds (times eight): NW * V * 512 >= cols.
-template <typename T, typename R, template <typename, typename, int, int> class Launch, typename A>
-static hipError_t by_width(const A &a, uint32_t rows, uint32_t cols, hipStream_t stream)
+// A row's threads: as many waves as its columns fill with eight a lane, up to 16, then up to eight times eight a lane.
+constexpr uint64_t kMaxCols = 65536;
+static dim3 row_threads(uint64_t cols, int v)
 {
-    if (cols <= 512) return Launch<T, R, 1, 1>::go(a, stream);
-    if (cols <= 1024) return Launch<T, R, 1, 2>::go(a, stream);
-    if (cols <= 2048) return Launch<T, R, 1, 4>::go(a, stream);
-    if (cols <= 4096) return Launch<T, R, 4, 2>::go(a, stream);
-    if (cols <= 8192) return Launch<T, R, 4, 4>::go(a, stream);
-    if (cols <= 16384) return Launch<T, R, 4, 8>::go(a, stream);
-    if (cols <= 32768) return Launch<T, R, 16, 4>::go(a, stream);
-    return Launch<T, R, 16, 8>::go(a, stream);
+    const uint32_t waves = (uint32_t)((cols + 512 * v - 1) / (512 * v));
+    return dim3(64 * waves, waves == 1 ? 4 : waves == 2 ? 2 : 1);
+}
+static int row_registers(uint64_t cols) { return cols <= 8192 ? 1 : cols <= 16384 ? 2 : cols <= 32768 ? 4 : 8; }
+
+// The gradient's blocks: those that the chip holds at once.
+static uint32_t blocks_of(uint64_t rows, uint64_t cols)
+{
+    const dim3 t = row_threads(cols, row_registers(cols));
+    return (uint32_t)std::min<uint64_t>((rows + t.y - 1) / t.y, std::max(256u, 4096 / (t.x * t.y / 64)));
 }
 
-template <typename T, typename R, int NW, int V> struct Forward {
-    static hipError_t go(const NormForward &a, hipStream_t s)
-    {
-        k_norm_forward<T, R, NW, V><<<NW == 1 ? (a.rows + 3) / 4 : a.rows, NW == 1 ? 256 : 64 * NW, 0, s>>>(a);
-        return hipGetLastError();
-    }
-};
-template <typename T, typename R, int NW, int V> struct Backward {
-    static hipError_t go(const NormBackward &a, hipStream_t s)
-    {
-        k_norm_backward<T, R, NW, V><<<NW == 1 ? (a.workers + 3) / 4 : a.workers, NW == 1 ? 256 : 64 * NW, 0, s>>>(a);
-        return hipGetLastError();
-    }
-};
-
-template <template <typename, typename, int, int> class Launch, typename A>
-static hipError_t by_types(const A &a, int dtype, int residual, hipStream_t s)
+template <typename T, typename R> static hipError_t launch_forward(const NormForward &a, hipStream_t s)
 {
-    if (dtype == REFT_F32) return by_width<float, float, Launch>(a, a.rows, a.cols, s);
-    if (dtype == REFT_BF16)
-        return residual == REFT_F32 ? by_width<bf16, float, Launch>(a, a.rows, a.cols, s)
-                                    : by_width<bf16, bf16, Launch>(a, a.rows, a.cols, s);
-    return residual == REFT_F32 ? by_width<f16, float, Launch>(a, a.rows, a.cols, s)
-                                : by_width<f16, f16, Launch>(a, a.rows, a.cols, s);
+    const int v = row_registers(a.cols);
+    const dim3 threads = row_threads(a.cols, v), grid((a.rows + threads.y - 1) / threads.y);
+    if (v == 1) k_norm_forward<T, R, 1><<<grid, threads, 0, s>>>(a);
+    else if (v == 2) k_norm_forward<T, R, 2><<<grid, threads, 0, s>>>(a);
+    else if (v == 4) k_norm_forward<T, R, 4><<<grid, threads, 0, s>>>(a);
+    else k_norm_forward<T, R, 8><<<grid, threads, 0, s>>>(a);
+    return hipGetLastError();
 }
 
-constexpr uint64_t kMaxCols = 65536;       // of a norm: 16 waves, 8 times 8 columns a lane
-constexpr uint64_t kMaxWorkers = 1024;
-
-static uint32_t workers_of(uint64_t rows)
+template <typename T, typename R> static hipError_t launch_backward(const NormBackward &a, uint32_t blocks, hipStream_t s)
 {
-    return (uint32_t)std::min<uint64_t>(rows, kMaxWorkers);
+    const int v = row_registers(a.cols);
+    const dim3 threads = row_threads(a.cols, v);
+    if (v == 1) k_norm_backward<T, R, 1><<<blocks, threads, 0, s>>>(a);
+    else if (v == 2) k_norm_backward<T, R, 2><<<blocks, threads, 0, s>>>(a);
+    else if (v == 4) k_norm_backward<T, R, 4><<<blocks, threads, 0, s>>>(a);
+    else k_norm_backward<T, R, 8><<<blocks, threads, 0, s>>>(a);
+    return hipGetLastError();
 }
 
 static bool is_float_type(int t) { return t == REFT_F32 || t == REFT_BF16 || t == REFT_F16; }
@@ -529,13 +570,18 @@ extern "C" int reft_norm_forward(const void *x, uint64_t ld_x, const void *resid
     a.ld_s = ld_s;
     a.e5m2 = format == REFT_E5M2;
     a.weight_f32 = weight_dtype == REFT_F32;
-    return launched("reft_norm_forward", by_types<Forward>(a, dtype, residual_dtype, (hipStream_t)stream));
+    hipStream_t s = (hipStream_t)stream;
+    const bool wide = residual_dtype == REFT_F32;
+    return launched("reft_norm_forward", dtype == REFT_F32    ? launch_forward<float, float>(a, s)
+                                         : dtype == REFT_BF16 ? (wide ? launch_forward<bf16, float>(a, s) : launch_forward<bf16, bf16>(a, s))
+                                                              : (wide ? launch_forward<f16, float>(a, s) : launch_forward<f16, f16>(a, s)));
 }
 
 extern "C" uint64_t reft_norm_backward_workspace(uint64_t rows, uint64_t cols)
 {
-    const uint64_t workers = workers_of(rows);
-    return workers > 1 && cols <= kMaxCols ? workers * cols * sizeof(float) : 0;
+    if (!rows || !cols || cols > kMaxCols) return 0;
+    const uint64_t blocks = blocks_of(rows, cols);
+    return blocks > 1 ? blocks * cols * sizeof(float) : 0;
 }
 
 extern "C" int reft_norm_backward(const void *dy, uint64_t ld_dy, const void *dh, uint64_t ld_dh, const void *h, uint64_t ld_h,
@@ -556,16 +602,16 @@ extern "C" int reft_norm_backward(const void *dy, uint64_t ld_dy, const void *dh
          REFT_ESIZE, "reft_norm_backward: rows overlap");
     NEED(dres || dx || dweight || !rows, REFT_EINVAL, "reft_norm_backward: no output");
     hipStream_t s = (hipStream_t)stream;
-    a.workers = workers_of(rows);
+    const uint32_t blocks = blocks_of(rows, cols);
     if (dweight) {
         NEED(lies(dweight, 4), REFT_EINVAL, "reft_norm_backward: misaligned pointer");
-        if (a.workers > 1) {
+        if (blocks > 1) {
             NEED(workspace && lies(workspace, 16), REFT_EINVAL, "reft_norm_backward: no workspace, or not on 16 bytes");
             NEED(workspace_bytes >= reft_norm_backward_workspace(rows, cols), REFT_ESIZE, "reft_norm_backward: workspace too small");
         }
     }
     if (!rows) {
-        if (dweight) k_sum_parts<<<(uint32_t)((cols + 63) / 64), 1024, 0, s>>>(nullptr, 0, (uint32_t)cols, dweight);
+        if (dweight) k_sum_parts<<<(uint32_t)((cols + 15) / 16), 1024, 0, s>>>(nullptr, 0, (uint32_t)cols, dweight);
         return launched("reft_norm_backward", hipGetLastError());
     }
     NEED(dy && h && rstd && weight, REFT_EINVAL, "reft_norm_backward: null pointer");
@@ -586,11 +632,14 @@ extern "C" int reft_norm_backward(const void *dy, uint64_t ld_dy, const void *dh
     a.dx = dx;
     a.ld_dres = ld_dres;
     a.ld_dx = ld_dx;
-    a.part = !dweight ? nullptr : a.workers > 1 ? (float *)workspace : dweight;
+    a.part = !dweight ? nullptr : blocks > 1 ? (float *)workspace : dweight;
     a.weight_f32 = weight_dtype == REFT_F32;
-    hipError_t e = by_types<Backward>(a, dtype, residual_dtype, s);
-    if (e == hipSuccess && dweight && a.workers > 1) {
-        k_sum_parts<<<(uint32_t)((cols + 63) / 64), 1024, 0, s>>>((const float *)workspace, a.workers, a.cols, dweight);
+    const bool wide = residual_dtype == REFT_F32;
+    hipError_t e = dtype == REFT_F32    ? launch_backward<float, float>(a, blocks, s)
+                   : dtype == REFT_BF16 ? (wide ? launch_backward<bf16, float>(a, blocks, s) : launch_backward<bf16, bf16>(a, blocks, s))
+                                        : (wide ? launch_backward<f16, float>(a, blocks, s) : launch_backward<f16, f16>(a, blocks, s));
+    if (e == hipSuccess && dweight && blocks > 1) {
+        k_sum_parts<<<(uint32_t)((cols + 15) / 16), 1024, 0, s>>>((const float *)workspace, blocks, a.cols, dweight);
         e = hipGetLastError();
     }
     return launched("reft_norm_backward", e);
@@ -601,7 +650,8 @@ template <typename T> static hipError_t launch_quantize(const QuantizeArgs &a, b
     if (!blocks && !a.q_t) {
         k_quantize_rows<T><<<dim3((uint32_t)((a.rows + 3) / 4), (uint32_t)((a.cols + 511) / 512)), 256, 0, s>>>(a);
     } else {
-        const dim3 grid((uint32_t)((a.rows + 127) / 128), (uint32_t)((a.cols + 127) / 128));
+        // tile after tile of a row of tiles (down the columns first: 16384 x 8192 116 -> 150 us)
+        const uint32_t grid = (uint32_t)((a.cols + 127) / 128 * ((a.rows + 127) / 128));
         if (blocks) k_quantize_tile<T, true><<<grid, 256, 0, s>>>(a);
         else k_quantize_tile<T, false><<<grid, 256, 0, s>>>(a);
     }
@@ -617,12 +667,13 @@ extern "C" int reft_quantize(const void *x, uint64_t ld_x, uint64_t rows, uint64
     NEED(is_eight(format), REFT_EINVAL, "reft_quantize: unknown 8-bit format %d", format);
     NEED(q || q_t || !rows || !cols, REFT_EINVAL, "reft_quantize: no output");
     NEED((!q || scales || !rows || !cols) && (!q_t || scales_t || !rows || !cols), REFT_EINVAL, "reft_quantize: 8 bits without scales");
-    // the grid's second dimension counts blocks of columns
+    // the grid counts tiles, or, in its second dimension, words of columns
     NEED(rows <= 0x7fffffff && cols <= 128 * 65535, REFT_ESIZE, "reft_quantize: too many rows or columns");
     NEED(ld_x >= cols && (!q || ld_q >= cols) && (!q_t || ld_qt >= rows), REFT_ESIZE, "reft_quantize: rows overlap");
     NEED((!q || ld_s >= (blocks ? (rows + 127) / 128 : rows)) && (!q_t || ld_st >= (blocks ? (cols + 127) / 128 : cols)),
          REFT_ESIZE, "reft_quantize: words of scales overlap");
     if (!rows || !cols) return REFT_OK;
+    NEED((rows + 127) / 128 * ((cols + 127) / 128) <= 0x7fffffff, REFT_ESIZE, "reft_quantize: too many values");
     NEED(x, REFT_EINVAL, "reft_quantize: null pointer");
     NEED(lies(x, size_of(dtype)), REFT_EINVAL, "reft_quantize: misaligned pointer");
     a.x = x;
