@@ -24,7 +24,7 @@ constexpr int kDropUnroll = 4;
 
 // A thread takes kDropUnroll groups.  Row and group of a block's first come of one division of whole numbers, those of
 // its threads of a multiplication.
-template <typename T> __global__ __launch_bounds__(256) void k_dropout(DropoutArgs a)
+template <typename T, bool STREAM> __global__ __launch_bounds__(256) void k_dropout(DropoutArgs a)
 {
     const uint64_t first = (uint64_t)blockIdx.x * (256 * kDropUnroll);
     const uint64_t row0 = first / a.groups;
@@ -41,7 +41,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_dropout(DropoutAr
         group[u] = at - r * groups;
         const uint64_t left = a.cols - (uint64_t)group[u] * 8;
         n[u] = first + local < a.total ? (int)(left < 8 ? left : 8) : 0;
-        load8<true>((const T *)a.x + (uint64_t)row[u] * a.ld_x + (uint64_t)group[u] * 8, n[u], v[u]);
+        load8<STREAM>((const T *)a.x + (uint64_t)row[u] * a.ld_x + (uint64_t)group[u] * 8, n[u], v[u]);
     }
 #pragma unroll
     for (int u = 0; u < kDropUnroll; ++u) {
@@ -143,7 +143,7 @@ template <typename T, typename R, int V> __global__ __launch_bounds__(1024) void
 #pragma unroll
             for (int i = 0; i < 8; ++i) most = max(most, magnitude(w[v][i]));
             const uint32_t e = scale_of(max_of_16(most), top_of(a.e5m2));
-            store8_bytes(a.q + row * a.ld_q + c, cols - c, to_eight(w[v], inverse_of(e), a.e5m2));
+            store8_bytes<true>(a.q + row * a.ld_q + c, cols - c, to_eight(w[v], inverse_of(e), a.e5m2));
             const int word = c / 512;                       // the same in the whole wave
             if ((lane & 15) == 0 && word * 512 < cols)
                 a.scales[(word * a.ld_s + row) * 4 + lane / 16] = c < cols ? (uint8_t)e : 127;
@@ -166,7 +166,7 @@ struct NormBackward {
 // Rows as above.  A block takes every so manyth row (or, of short rows, blockDim.y of them) and keeps its part of the weight's
 // gradient in registers; k_sum_parts adds the blocks' parts in their order.  Of rows with more than eight columns a lane the operands
 // are read again for the second half of the work (from the L2) rather than held.
-template <typename T, typename R, int V> __global__ __launch_bounds__(1024) void k_norm_backward(NormBackward a)
+template <typename T, typename R, int V, bool STREAM> __global__ __launch_bounds__(1024) void k_norm_backward(NormBackward a)
 {
     __shared__ float room[2][16];
     __shared__ float fold[V == 1 ? 3 * 512 : 1];
@@ -194,9 +194,9 @@ template <typename T, typename R, int V> __global__ __launch_bounds__(1024) void
     };
     auto fetch_next = [&](uint32_t row) {
         const int n = row < a.rows ? cols - first : 0;
-        next_h.template load<true>((const R *)a.h + row * a.ld_h + first, n);
-        next_dy.template load<true>((const T *)a.dy + row * a.ld_dy + first, n);
-        next_dh.template load<true>((const R *)a.dh + row * a.ld_dh + first, a.dh ? n : 0);
+        next_h.template load<STREAM>((const R *)a.h + row * a.ld_h + first, n);
+        next_dy.template load<STREAM>((const T *)a.dy + row * a.ld_dy + first, n);
+        next_dh.template load<STREAM>((const R *)a.dh + row * a.ld_dh + first, a.dh ? n : 0);
         next_rstd = row < a.rows ? a.rstd[row] : 0.f;
     };
     if (V == 1) fetch_next(blockIdx.x * blockDim.y + threadIdx.y);
@@ -303,7 +303,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_quantize_rows(Qua
 #pragma unroll
     for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[i]));
     const uint32_t e = scale_of(max_of_16(most), top_of(a.e5m2));
-    store8_bytes(a.q + row * a.ld_q + c, n, to_eight(v, inverse_of(e), a.e5m2));
+    store8_bytes<true>(a.q + row * a.ld_q + c, n, to_eight(v, inverse_of(e), a.e5m2));
     if ((lane & 15) == 0) a.scales[((uint64_t)blockIdx.y * a.ld_s + row) * 4 + lane / 16] = n ? (uint8_t)e : 127;
 }
 
@@ -318,8 +318,8 @@ __device__ __forceinline__ void store_scale(uint8_t *scales, uint64_t ld, uint64
 
 // A tile of 128 x 128 values, in registers: a thread holds 8 rows of 8 columns, so that each of its columns is 8 bytes of
 // the transpose, which leaves through LDS in whole rows.  BLOCKS: one scale for the tile, else one for each row and, in the
-// transpose, for each column.
-template <typename T, bool BLOCKS> __global__ __launch_bounds__(256) void k_quantize_tile(QuantizeArgs a)
+// transpose, for each column.  LINES: the results' rows lie on cache lines, which a tile then writes whole.
+template <typename T, bool BLOCKS, bool LINES> __global__ __launch_bounds__(256) void k_quantize_tile(QuantizeArgs a)
 {
     constexpr int kPitch = 1024 + 32;          // LDS bytes of eight columns of 128 rows: 16 lanes' writes meet no bank twice
     __shared__ __align__(16) uint8_t tile[16 * kPitch];
@@ -385,7 +385,7 @@ template <typename T, bool BLOCKS> __global__ __launch_bounds__(256) void k_quan
                 e = scale_of(max_of_16(m), top);
                 if (tc == 0 && r < rows) store_scale(a.scales, a.ld_s, row0 + r, along, wide, e);
             }
-            if (r < rows) store8_bytes(a.q + (row0 + r) * a.ld_q + col0 + tc * 8, cols - tc * 8, to_eight(t, inverse_of(e), a.e5m2));
+            if (r < rows) store8_bytes<LINES>(a.q + (row0 + r) * a.ld_q + col0 + tc * 8, cols - tc * 8, to_eight(t, inverse_of(e), a.e5m2));
         }
     }
     if (!a.q_t) return;
@@ -412,7 +412,8 @@ template <typename T, bool BLOCKS> __global__ __launch_bounds__(256) void k_quan
         const w32x4 w = *(const w32x4 *)(tile + (c / 8) * kPitch + (c % 8) * 128 + r);
         uint8_t *p = a.q_t + (col0 + c) * a.ld_qt + row0 + r;
         if (r + 16 <= rows) {
-            __builtin_nontemporal_store(w, (w32x4_any *)p);
+            if constexpr (LINES) __builtin_nontemporal_store(w, (w32x4_any *)p);
+            else *(w32x4_any *)p = w;
         } else {
             for (int i = 0; i < rows - r; ++i) p[i] = tile[(c / 8) * kPitch + (c % 8) * 128 + r + i];
         }
@@ -422,6 +423,16 @@ template <typename T, bool BLOCKS> __global__ __launch_bounds__(256) void k_quan
 // ------------------------------------------------------------------------------------------------
 // which kernel
 // ------------------------------------------------------------------------------------------------
+// Rows on cache lines are read past the L2.  (Gradient of 16384 x 8192 in bf16: 241 us kept, 227 not; dropout of 16384 x 11008: 120
+// and 115.  Of other rows each line is read twice: dropout of 4096 x 5003 in fp32 31 and 38, of 16384 x 1155 16.8 and 19.7.)
+static bool on_lines(const void *p, uint64_t row_bytes) { return ((uintptr_t)p | row_bytes) % 128 == 0; }
+
+template <typename T> static void launch_dropout(const DropoutArgs &a, bool lines, uint32_t blocks, hipStream_t s)
+{
+    if (lines) k_dropout<T, true><<<blocks, 256, 0, s>>>(a);
+    else k_dropout<T, false><<<blocks, 256, 0, s>>>(a);
+}
+
 // A row's threads: as many waves as its columns fill with eight a lane, up to 16, then up to eight times eight a lane.
 constexpr uint64_t kMaxCols = 65536;
 static dim3 row_threads(uint64_t cols, int v)
@@ -431,11 +442,14 @@ static dim3 row_threads(uint64_t cols, int v)
 }
 static int row_registers(uint64_t cols) { return cols <= 8192 ? 1 : cols <= 16384 ? 2 : cols <= 32768 ? 4 : 8; }
 
-// The gradient's blocks: those that the chip holds at once.
+// The gradient's blocks: what the 256 compute units hold at once, at up to 16 waves each (its registers allow no more), or 12 where
+// rows may lie on cache lines and fewer waves keep the memory busy.  With 16, 12 and 8 waves, us in bf16: 16384 x 2048 69, 64 and 62,
+// x 5120 179 (two rounds), 152 and 152, x 1155 79, 94 and 111.
 static uint32_t blocks_of(uint64_t rows, uint64_t cols)
 {
     const dim3 t = row_threads(cols, row_registers(cols));
-    return (uint32_t)std::min<uint64_t>((rows + t.y - 1) / t.y, std::max(256u, 4096 / (t.x * t.y / 64)));
+    const uint32_t waves = t.x * t.y / 64, room = cols % 64 ? 16 : 12;
+    return (uint32_t)std::min<uint64_t>((rows + t.y - 1) / t.y, 256 * std::max(1u, room / waves));
 }
 
 template <typename T, typename R> static hipError_t launch_forward(const NormForward &a, hipStream_t s)
@@ -453,10 +467,12 @@ template <typename T, typename R> static hipError_t launch_backward(const NormBa
 {
     const int v = row_registers(a.cols);
     const dim3 threads = row_threads(a.cols, v);
-    if (v == 1) k_norm_backward<T, R, 1><<<blocks, threads, 0, s>>>(a);
-    else if (v == 2) k_norm_backward<T, R, 2><<<blocks, threads, 0, s>>>(a);
-    else if (v == 4) k_norm_backward<T, R, 4><<<blocks, threads, 0, s>>>(a);
-    else k_norm_backward<T, R, 8><<<blocks, threads, 0, s>>>(a);
+    const bool lines = on_lines(a.dy, a.ld_dy * sizeof(T)) && on_lines(a.h, a.ld_h * sizeof(R)) && on_lines(a.dh, a.ld_dh * sizeof(R));
+    if (v == 1 && lines) k_norm_backward<T, R, 1, true><<<blocks, threads, 0, s>>>(a);
+    else if (v == 1) k_norm_backward<T, R, 1, false><<<blocks, threads, 0, s>>>(a);
+    else if (v == 2) k_norm_backward<T, R, 2, false><<<blocks, threads, 0, s>>>(a);
+    else if (v == 4) k_norm_backward<T, R, 4, false><<<blocks, threads, 0, s>>>(a);
+    else k_norm_backward<T, R, 8, false><<<blocks, threads, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -517,9 +533,10 @@ extern "C" int reft_dropout(const void *x, uint64_t ld_x, void *y, uint64_t ld_y
     const uint64_t blocks = (a.total + 256 * kDropUnroll - 1) / (256 * kDropUnroll);
     NEED(blocks <= 0x7fffffff, REFT_ESIZE, "reft_dropout: too many values");
     hipStream_t s = (hipStream_t)stream;
-    if (dtype == REFT_F32) k_dropout<float><<<(uint32_t)blocks, 256, 0, s>>>(a);
-    else if (dtype == REFT_BF16) k_dropout<bf16><<<(uint32_t)blocks, 256, 0, s>>>(a);
-    else k_dropout<f16><<<(uint32_t)blocks, 256, 0, s>>>(a);
+    const bool lines = on_lines(x, ld_x * size_of(dtype));
+    if (dtype == REFT_F32) launch_dropout<float>(a, lines, (uint32_t)blocks, s);
+    else if (dtype == REFT_BF16) launch_dropout<bf16>(a, lines, (uint32_t)blocks, s);
+    else launch_dropout<f16>(a, lines, (uint32_t)blocks, s);
     return launched("reft_dropout", hipGetLastError());
 }
 
@@ -652,8 +669,12 @@ template <typename T> static hipError_t launch_quantize(const QuantizeArgs &a, b
     } else {
         // tile after tile of a row of tiles (down the columns first: 16384 x 8192 116 -> 150 us)
         const uint32_t grid = (uint32_t)((a.cols + 127) / 128 * ((a.rows + 127) / 128));
-        if (blocks) k_quantize_tile<T, true><<<grid, 256, 0, s>>>(a);
-        else k_quantize_tile<T, false><<<grid, 256, 0, s>>>(a);
+        // (lines that tiles share are joined in the L2: 4099 x 4101 36 us past it, 25 through it)
+        const bool lines = (!a.q || on_lines(a.q, a.ld_q)) && (!a.q_t || on_lines(a.q_t, a.ld_qt));
+        if (blocks && lines) k_quantize_tile<T, true, true><<<grid, 256, 0, s>>>(a);
+        else if (blocks) k_quantize_tile<T, true, false><<<grid, 256, 0, s>>>(a);
+        else if (lines) k_quantize_tile<T, false, true><<<grid, 256, 0, s>>>(a);
+        else k_quantize_tile<T, false, false><<<grid, 256, 0, s>>>(a);
     }
     return hipGetLastError();
 }

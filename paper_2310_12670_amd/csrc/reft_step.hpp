@@ -185,10 +185,11 @@ __device__ __forceinline__ w32x2 to_eight(const float v[8], float inv, bool e5m2
     return w;
 }
 
-__device__ __forceinline__ void store8_bytes(uint8_t *p, int n, w32x2 w)
+template <bool STREAM> __device__ __forceinline__ void store8_bytes(uint8_t *p, int n, w32x2 w)
 {
     if (n >= 8) {
-        __builtin_nontemporal_store(w, (w32x2_any *)p);
+        if constexpr (STREAM) __builtin_nontemporal_store(w, (w32x2_any *)p);
+        else *(w32x2_any *)p = w;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
