@@ -209,8 +209,9 @@ template <int FA, int FB, bool EXACT> __global__ __launch_bounds__(256) void k_p
 
 // ---- few rows of A: the weights' bytes are the bound ------------------------------------------------------------------
 // A workgroup takes 16 rows of B, its waves blocks of 128 of K in turn; each lane loads its part of a product of 16 x 16 x 128 from
-// memory itself (any alignment), four blocks ahead, and multiplies it with up to MT times 16 rows of A.  The waves' sums meet in
-// LDS and are added in the waves' order.
+// memory itself (any alignment) and multiplies it with up to 16 rows of A.  The waves' sums meet in LDS and are
+// added in the waves' order.  WHOLE: K is a multiple of 128.  16 waves, two blocks ahead, in 64 registers, so that two workgroups share a
+// compute unit (one row, N x K = 11008 x 4096, 28672 x 8192: 11.6 and 41.1 us; 8 waves, four ahead: 17.3 and 57.3).
 template <int FA, int FB, bool EXACT>
 __device__ __forceinline__ f32x4 multiply16(i32x8 b, i32x8 a, f32x4 acc, uint32_t eb, uint32_t ea)
 {
@@ -227,58 +228,51 @@ __device__ __forceinline__ f32x4 multiply16(i32x8 b, i32x8 a, f32x4 acc, uint32_
     }
 }
 
-template <int FA, int FB, bool EXACT, int MT, int WAVES> __global__ __launch_bounds__(64 * WAVES) void k_product_few(ProductArgs p)
+template <int FA, int FB, bool EXACT, bool WHOLE, int WAVES> __global__ __launch_bounds__(64 * WAVES, 8) void k_product_few(ProductArgs p)
 {
-    constexpr int kAhead = MT == 1 ? 4 : 2;
-    __shared__ f32x4 sums[WAVES][MT][64];
+    constexpr int kAhead = 2;
+    __shared__ f32x4 sums[WAVES][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t n0 = blockIdx.x * 16, r = lane & 15, blocks = (p.K + 127) / 128;
     const uint32_t n = min(n0 + r, p.N - 1);                 // rows behind the last repeat it, and are not stored
-    const uint8_t *b = p.b + n * p.ld_b, *sb = (const uint8_t *)(p.sb + (n >> p.b_shift));
-    f32x4 acc[MT] = {};
+    const bool row = r < p.M;
+    const uint8_t *b = p.b + n * p.ld_b + (lane >> 4) * 32, *a = p.a + (row ? r : 0) * p.ld_a + (lane >> 4) * 32;
+    const uint32_t *sb = p.sb + (n >> p.b_shift), *sa = p.sa + (row ? r : 0);
+    f32x4 acc = {};
     for (uint32_t first = wave; first < blocks; first += WAVES * kAhead) {
-        w32x4 vb[kAhead][2], va[kAhead][MT][2];
-        uint32_t eb[kAhead], ea[kAhead][MT];
+        w32x4 vb[kAhead][2], va[kAhead][2];
+        uint32_t eb[kAhead], ea[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const uint32_t block = first + u * WAVES, k = block * 128 + (lane >> 4) * 32;
-            const bool there = block < blocks;
-            const int left = !there || k >= p.K ? 0 : (int)min(p.K - k, 32u);
+            const bool there = block < blocks;                   // the same for the whole wave
+            const int left = !there ? 0 : WHOLE ? 32 : k >= p.K ? 0 : (int)min(p.K - k, 32u);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) vb[u][h] = load16(b + k + h * 16, left - h * 16);
-            eb[u] = there ? sb[block / 4 * p.ld_sb * 4 + block % 4] : 127;
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const uint32_t m = i * 16 + r;
-                const bool row = there && m < p.M;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) va[u][i][h] = load16(p.a + m * p.ld_a + k + h * 16, row ? left - h * 16 : 0);
-                ea[u][i] = row ? ((const uint8_t *)p.sa)[(block / 4 * p.ld_sa + m) * 4 + block % 4] : 127;
+            for (int h = 0; h < 2; ++h) {
+                vb[u][h] = load16(b + block * 128ull + h * 16, left - h * 16);
+                va[u][h] = load16(a + block * 128ull + h * 16, row ? left - h * 16 : 0);
             }
+            eb[u] = there ? sb[block / 4 * p.ld_sb] >> block % 4 * 8 : 127;
+            ea[u] = there && row ? sa[block / 4 * p.ld_sa] >> block % 4 * 8 : 127;
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             i32x8 ob, oa;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ob[e] = (int)vb[u][e / 4][e % 4];
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) oa[e] = (int)va[u][i][e / 4][e % 4];
-                acc[i] = multiply16<FA, FB, EXACT>(ob, oa, acc[i], eb[u], ea[u][i]);
-            }
+            for (int e = 0; e < 8; ++e) ob[e] = (int)vb[u][e / 4][e % 4], oa[e] = (int)va[u][e / 4][e % 4];
+            acc = multiply16<FA, FB, EXACT>(ob, oa, acc, eb[u], ea[u]);
         }
     }
-#pragma unroll
-    for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+    sums[wave][lane] = acc;
     __syncthreads();
-    for (int t = threadIdx.x; t < MT * 256; t += 64 * WAVES) {
-        // column t % 16 of row t / 16: lane (column / 4) * 16 + row % 16 holds it, in place column % 4
-        const uint32_t col = t % 16, row = t / 16;
+    const uint32_t t = threadIdx.x;
+    if (t < 256) {
+        // column t % 16 of row t / 16: lane (column / 4) * 16 + row holds it, in place column % 4
+        const uint32_t col = t % 16, m = t / 16;
         float v = 0;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) v += sums[w][row / 16][col / 4 * 16 + row % 16][col % 4];
-        if (row < p.M && n0 + col < p.N) store1(p, row * p.ld_c + n0 + col, v);
+        for (int w = 0; w < WAVES; ++w) v += sums[w][col / 4 * 16 + m][col % 4];
+        if (m < p.M && n0 + col < p.N) store1(p, m * p.ld_c + n0 + col, v);
     }
 }
 
@@ -637,17 +631,17 @@ template <int FA, int FB, int MT, int NT> static hipError_t launch_tiles(const P
     return hipGetLastError();
 }
 
-template <int FA, int FB, int MT> static hipError_t launch_few(const ProductArgs &p, hipStream_t s)
+template <int FA, int FB, bool WHOLE> static hipError_t launch_few(const ProductArgs &p, hipStream_t s)
 {
     const uint32_t grid = (p.N + 15) / 16;
-    if (p.c_type == REFT_F32) k_product_few<FA, FB, true, MT, 8><<<grid, 512, 0, s>>>(p);
-    else k_product_few<FA, FB, false, MT, 8><<<grid, 512, 0, s>>>(p);
+    if (p.c_type == REFT_F32) k_product_few<FA, FB, true, WHOLE, 16><<<grid, 1024, 0, s>>>(p);
+    else k_product_few<FA, FB, false, WHOLE, 16><<<grid, 1024, 0, s>>>(p);
     return hipGetLastError();
 }
 
 template <int FA, int FB> static hipError_t launch_product(const ProductArgs &p, hipStream_t s)
 {
-    if (p.M <= 16) return launch_few<FA, FB, 1>(p, s);
+    if (p.M <= 16) return p.K % 128 ? launch_few<FA, FB, false>(p, s) : launch_few<FA, FB, true>(p, s);
     if (on_16_bytes(p)) {
         const Shape t = shape_of(p.M, p.N, p.K);
         ProductArgs q = p;
