@@ -521,7 +521,7 @@ int reft_norm_forward(const void *x, uint64_t ld_x, const void *residual, uint64
  *   dres = rstd (dy weight - h rstd mean(dy weight h rstd)) + dh,  dx = dropout(dres),  dweight[c] = sum over r of dy h rstd.
  * dy and dx have dtype, dh, h and dres residual_dtype; dweight is fp32.  dres, dx and dweight are each left out where NULL.
  * dres may be dh and dx may be dy (with the same ld).  rows == 0 gives dweight = 0.  workspace: on 16 bytes, of at least
- * reft_norm_backward_workspace(rows, cols) bytes where dweight is wanted; scratch, not shared with a call in flight.
+ * reft_norm_backward_workspace(rows, cols) bytes (0 for one row) where dweight is wanted; scratch, not shared with a call in flight.
  */
 uint64_t reft_norm_backward_workspace(uint64_t rows, uint64_t cols);
 int reft_norm_backward(const void *dy, uint64_t ld_dy, const void *dh, uint64_t ld_dh, const void *h, uint64_t ld_h,
@@ -540,7 +540,8 @@ int reft_quantize(const void *x, uint64_t ld_x, uint64_t rows, uint64_t cols, in
 
 /* c[m][n] = sum over k of a[m][k] b[n][k], each with its scale.  a has scales per 128 columns of a row; b too, or, with b_blocks != 0,
  * per 128 x 128 values.  A layer's output is a product of its inputs and weights; the gradient of its inputs one of the output's
- * gradient and the transposed weights; that of its weights one of both transposes.  What lies between K and ld is not used.
+ * gradient and the transposed weights; that of its weights one of both transposes.  What lies between K and ld is not used, but
+ * the last 16 bytes (on a multiple of 16) that hold a value of a row may be read as a whole.
  * K == 0 gives zeros.  Fastest where both matrices begin at multiples of 16 bytes and their rows too.  workspace: on 16 bytes, of
  * at least reft_product_workspace(M, N, K) bytes (0 for most sizes); scratch, not shared with a call in flight.
  * M <= 128 * 65535; N, K < 2^31.

@@ -403,9 +403,11 @@ __global__ __launch_bounds__(256, MT * NT >= 16 ? 1 : 2) void k_product(ProductA
     tile_of(blockIdx.x, (p.M + kRowsA - 1) / kRowsA, (p.N + kRowsB - 1) / kRowsB, tm, tn);
     const uint32_t m0 = tm * kRowsA, n0 = tn * kRowsB;
     const int wm = (wave & 1) * 32 * MT, wn = (wave >> 1) * 32 * NT;
-    // steps of whole chunks; where K ends in one, the last may be a part of a step, else that part is left to the end
-    const uint32_t all = p.K % 16 ? p.K / 128 : (p.K + 127) / 128, start = kWhole ? 0 : blockIdx.y * p.split_steps;
+    const uint32_t all = (p.K + 127) / 128, start = kWhole ? 0 : blockIdx.y * p.split_steps;
     const uint32_t steps = kWhole ? all : start < all ? min(all - start, p.split_steps) : 0, K = p.K - start * 128;
+    // a last step that ends inside a chunk is taken by itself
+    const bool cut = p.K % 16 && start + steps == all;
+    const uint32_t loops = cut ? steps - 1 : steps;
     // A wave's copy fills eight rows of a tile: lane i the place i % 8 of row i / 8.  Rows behind the matrix's last repeat that.
     const uint8_t *base_a = p.a + (uint64_t)m0 * p.ld_a + (uint64_t)start * 128, *base_b = p.b + (uint64_t)n0 * p.ld_b + (uint64_t)start * 128;
     uint32_t from_a[kCopiesA], from_b[kCopiesB];
@@ -416,7 +418,8 @@ __global__ __launch_bounds__(256, MT * NT >= 16 ? 1 : 2) void k_product(ProductA
 #pragma unroll
     for (int i = 0; i < kCopiesB; ++i)
         from_b[i] = min((uint32_t)((wave * kCopiesB + i) * 8 + (lane >> 3)), p.N - 1 - n0) * (uint32_t)p.ld_b + chunk(i);
-    // chunks behind K lie outside the buffer, and arrive as zeroes
+    // chunks behind K lie outside the buffer, and arrive as zeroes; one that holds a value of the row is memory of the row's to its end,
+    // as chunks lie on 16 bytes
     auto fill_a = [&](uint32_t step, uint8_t *a) {
         const Base from(base_a + (uint64_t)step * 128, step < steps);
         const uint32_t left = K - step * 128, out0 = chunk(0) < left ? 0 : kOutside, out1 = chunk(1) < left ? 0 : kOutside;
@@ -485,11 +488,11 @@ __global__ __launch_bounds__(256, MT * NT >= 16 ? 1 : 2) void k_product(ProductA
     // tiles have been read by all and the next step's have arrived; the ones after those are fetched all the time, A's in a step's
     // first half (into a third place), B's in the second: a half's copies more in flight than with two places each, and no more
     // at once than the way from the L2 takes (8192 x 28672 x 8192: 1460 -> 1360 us).  A word of scales serves four steps.
-    for (uint32_t step = 0; step < steps; step += 6) {
+    for (uint32_t step = 0; step < loops; step += 6) {
 #pragma unroll
         for (int j = 0; j < 6; ++j) {
             const uint32_t at = step + j;
-            if (at >= steps) break;
+            if (at >= loops) break;
             if (at % 4 == 0) {
                 take_words();
                 words(at / 4 + 1);
@@ -511,26 +514,27 @@ __global__ __launch_bounds__(256, MT * NT >= 16 ? 1 : 2) void k_product(ProductA
             for (int i = 0; i < NT; ++i) sb[i] >>= 8;
         }
     }
-    if (p.K % 16 && (kWhole || blockIdx.y + 1 == p.splits)) {        // the rest of K, with zeroes behind it: through registers
-        const uint32_t left = K - steps * 128;
-        meet<0>();
-#pragma unroll 1
-        for (int r = tid >> 3; r < kRowsA + kRowsB; r += 32) {
-            const int row = r < kRowsA ? r : r - kRowsA, k = (tid & 7) * 16;
-            const uint32_t at = r < kRowsA ? min((uint32_t)row, p.M - 1 - m0) : min((uint32_t)row, p.N - 1 - n0);
-            const uint8_t *from = (r < kRowsA ? base_a + at * p.ld_a : base_b + at * p.ld_b) + (uint64_t)steps * 128 + k;
-            *(w32x4 *)((r < kRowsA ? ta0 : tb0) + place(row, k / 16)) = load16(from, (int)left - k);
-        }
-        words(last_word);
-        take_words();
-#pragma unroll
-        for (int i = 0; i < MT; ++i) sa[i] >>= steps % 4 * 8;
-#pragma unroll
-        for (int i = 0; i < NT; ++i) sb[i] >>= steps % 4 * 8;
-        meet<0>();
+    if (cut) {                                               // what follows K in its chunk is anything: zeroed in registers
+        if (loops % 4 == 0) take_words();
+        const int left = (int)(K - loops * 128);
+        const uint8_t *const la = loops % 3 == 0 ? ta0 : loops % 3 == 1 ? ta1 : ta2, *const lb = loops % 2 ? tb1 : tb0;
 #pragma unroll 1
         for (int s = 0; s < 2; ++s) {
-            read(a0, b0, ta0, tb0, s);
+            read(a0, b0, la, lb, s);
+            int mask[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int there = left - (s * 64 + (lane >> 5) * 32 + e * 4);          // bytes of this word
+                mask[e] = there >= 4 ? -1 : there <= 0 ? 0 : (1 << 8 * there) - 1;
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a0[i][e] &= mask[e];
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) b0[i][e] &= mask[e];
             multiply_all(a0, b0);
         }
     }
@@ -583,15 +587,17 @@ struct Shape {
 };
 constexpr uint64_t kMaxParts = 64ull << 20;            // bytes of the workspace
 
-// Time goes by the tiles that fall to a compute unit, which runs two of 128 x 128 at once or one of 256 x 256; one of these takes
-// three of those (measured at N x K = 11008 x 4096, us for 128 and 256: M = 512 29 and 41, 768 47 and 42, 1280 61 and 50, 1536 76
-// and 88, 2560 113 and 101; 5120 x 13824: M = 1536 112 and 136, 2048 185 and 139, 3200 218 and 269).  K is cut where there are
-// at most half as many tiles as units (M = 128 and 512 of 4096 x 11008: 46 -> 21, 46 -> 33; one in two of 512 places: 46 -> 44).
+// Time goes by the tiles that fall to a compute unit, which runs two of 128 x 128 at once or one of 256 x 256; one of these takes two
+// and a half times one of those, and 720 values of K more for its start and end, which nothing runs beside.  Measured, us for 128
+// and 256: N x K = 11008 x 4096, M = 512 29 and 41, 768 47 and 42, 1280 61 and 50, 1536 76 and 88, 2560 113 and 101; 5120 x 13824, M =
+// 1536 112 and 136, 2048 185 and 139, 3200 218 and 269; M x N = 10730 x 4416, K = 50 29 and 38, 1024 65 and 67, 2048 105 and 98.
+// K is cut where there are at most half as many tiles as units (M = 128 and 512 of 4096 x 11008: 46 -> 21, 46 -> 33; cut for twice as
+// many places the second takes 44).
 static Shape shape_of(uint64_t M, uint64_t N, uint64_t K)
 {
     Shape t;
     const uint64_t big = (M + 255) / 256 * ((N + 255) / 256), small = (M + 127) / 128 * ((N + 127) / 128), steps = (K + 127) / 128;
-    t.tile = M <= 64 ? 0 : 3 * ((big + 255) / 256) <= (small + 255) / 256 ? 2 : 1;
+    t.tile = M <= 64 ? 0 : 5 * ((big + 255) / 256) * (K + 720) <= 2 * ((small + 255) / 256) * K ? 2 : 1;
     t.splits = 1;
     t.split_steps = (uint32_t)((steps + 3) / 4 * 4);
     if (M <= 16 || t.tile == 2) return t;

@@ -449,6 +449,7 @@ static uint32_t blocks_of(uint64_t rows, uint64_t cols)
 {
     const dim3 t = row_threads(cols, row_registers(cols));
     const uint32_t waves = t.x * t.y / 64, room = cols % 64 ? 16 : 12;
+    if (rows <= 4 * t.y) return rows ? 1 : 0;                // one block is done before a second launch would be
     return (uint32_t)std::min<uint64_t>((rows + t.y - 1) / t.y, 256 * std::max(1u, room / waves));
 }
 
@@ -596,9 +597,8 @@ extern "C" int reft_norm_forward(const void *x, uint64_t ld_x, const void *resid
 
 extern "C" uint64_t reft_norm_backward_workspace(uint64_t rows, uint64_t cols)
 {
-    if (!rows || !cols || cols > kMaxCols) return 0;
-    const uint64_t blocks = blocks_of(rows, cols);
-    return blocks > 1 ? blocks * cols * sizeof(float) : 0;
+    if (rows <= 1 || !cols || cols > kMaxCols) return 0;
+    return (uint64_t)blocks_of(rows, cols) * cols * sizeof(float);
 }
 
 extern "C" int reft_norm_backward(const void *dy, uint64_t ld_dy, const void *dh, uint64_t ld_dh, const void *h, uint64_t ld_h,
@@ -622,7 +622,7 @@ extern "C" int reft_norm_backward(const void *dy, uint64_t ld_dy, const void *dh
     const uint32_t blocks = blocks_of(rows, cols);
     if (dweight) {
         NEED(lies(dweight, 4), REFT_EINVAL, "reft_norm_backward: misaligned pointer");
-        if (blocks > 1) {
+        if (rows > 1) {
             NEED(workspace && lies(workspace, 16), REFT_EINVAL, "reft_norm_backward: no workspace, or not on 16 bytes");
             NEED(workspace_bytes >= reft_norm_backward_workspace(rows, cols), REFT_ESIZE, "reft_norm_backward: workspace too small");
         }
