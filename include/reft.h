@@ -532,7 +532,7 @@ int reft_norm_backward(const void *dy, uint64_t ld_dy, const void *dh, uint64_t 
 
 /* q = x in 8 bits, and q_t = the transpose of x in 8 bits ([cols][ld_qt]); either is left out where NULL.  blocks == 0:
  * scales per 128 columns of a row of q, and per 128 columns of a row of q_t (which are rows of x).  blocks != 0: one
- * per 128 x 128 values, the same ones for both, laid out for each with rows of blocks as rows.  rows < 2^31, cols <= 128 * 65535.
+ * per 128 x 128 values, the same ones for both, laid out for each with rows of blocks as rows.  rows < 2^26, cols <= 128 * 65535.
  */
 int reft_quantize(const void *x, uint64_t ld_x, uint64_t rows, uint64_t cols, int dtype, int format, int blocks,
                   void *q, uint64_t ld_q, void *scales, uint64_t ld_s, void *q_t, uint64_t ld_qt, void *scales_t,
@@ -544,7 +544,7 @@ int reft_quantize(const void *x, uint64_t ld_x, uint64_t rows, uint64_t cols, in
  * the last 16 bytes (on a multiple of 16) that hold a value of a row may be read as a whole.
  * K == 0 gives zeros.  Fastest where both matrices begin at multiples of 16 bytes and their rows too.  workspace: on 16 bytes, of
  * at least reft_product_workspace(M, N, K) bytes (0 for most sizes); scratch, not shared with a call in flight.
- * M <= 128 * 65535; N, K < 2^31.
+ * M <= 128 * 65535; N, K < 2^31; M N < 2^37.
  */
 uint64_t reft_product_workspace(uint64_t M, uint64_t N, uint64_t K);
 int reft_product(const void *a, uint64_t ld_a, int a_format, const void *a_scales, uint64_t ld_as, const void *b,

@@ -647,7 +647,7 @@ template <int FA, int FB, bool WHOLE> static hipError_t launch_few(const Product
 
 template <int FA, int FB> static hipError_t launch_product(const ProductArgs &p, hipStream_t s)
 {
-    if (p.M <= 16) return p.K % 128 ? launch_few<FA, FB, false>(p, s) : launch_few<FA, FB, true>(p, s);
+    if (p.M <= 16 && p.N < (1u << 26)) return p.K % 128 ? launch_few<FA, FB, false>(p, s) : launch_few<FA, FB, true>(p, s);
     if (on_16_bytes(p)) {
         const Shape t = shape_of(p.M, p.N, p.K);
         ProductArgs q = p;
@@ -688,8 +688,9 @@ extern "C" int reft_product(const void *a, uint64_t ld_a, int a_format, const vo
     NEED((a_format == REFT_E4M3 || a_format == REFT_E5M2) && (b_format == REFT_E4M3 || b_format == REFT_E5M2), REFT_EINVAL,
          "unknown 8-bit format");
     NEED(c_dtype == REFT_F32 || c_dtype == REFT_BF16 || c_dtype == REFT_F16, REFT_EINVAL, "unknown type %d", c_dtype);
-    // rows of tiles are counted by the grid's second dimension
-    NEED(M <= 128 * 65535 && N <= 0x7fffffff && K <= 0x7fffffff, REFT_ESIZE, "a matrix is too large");
+    // rows of tiles are counted by the grid's second dimension, all of them (of 64 x 128) by less than 2^32 threads
+    NEED(M <= 128 * 65535 && N <= 0x7fffffff && K <= 0x7fffffff && (M + 63) / 64 * ((N + 127) / 128) <= 0xffffff, REFT_ESIZE,
+         "a matrix is too large");
     NEED(!M || !N || (c && (!K || (a && b && a_scales && b_scales))), REFT_EINVAL, "null pointer");
     NEED(ld_c >= N && ld_a >= K && ld_b >= K, REFT_ESIZE, "rows overlap");
     NEED(ld_as >= M && ld_bs >= (b_blocks ? (N + 127) / 128 : N), REFT_ESIZE, "words of scales overlap");

@@ -56,7 +56,7 @@ template <typename T, bool STREAM> __global__ __launch_bounds__(256) void k_drop
 struct NormForward {
     const void *x, *residual, *weight;
     uint64_t ld_x, ld_r;
-    uint32_t rows, cols;
+    uint32_t first, rows, cols;    // rows first .. rows - 1
     float eps;
     Dropout d;
     void *h;
@@ -98,7 +98,7 @@ template <typename T, typename R, int V> __global__ __launch_bounds__(1024) void
 {
     __shared__ float room[16];
     const int lane = threadIdx.x & 63, first = threadIdx.x * 8, wide = blockDim.x * 8, cols = (int)a.cols;
-    const uint32_t row = blockIdx.x * blockDim.y + threadIdx.y;
+    const uint32_t row = a.first + blockIdx.x * blockDim.y + threadIdx.y;
     const bool there = row < a.rows;
     constexpr bool kAhead = V <= 2;                          // all is asked for at once, as far as registers go
     Eight<T> x[V];
@@ -435,6 +435,7 @@ template <typename T> static void launch_dropout(const DropoutArgs &a, bool line
 
 // A row's threads: as many waves as its columns fill with eight a lane, up to 16, then up to eight times eight a lane.
 constexpr uint64_t kMaxCols = 65536;
+constexpr uint32_t kRowsALaunch = 1u << 21;            // a grid has less than 2^32 threads, a row up to 1024
 static dim3 row_threads(uint64_t cols, int v)
 {
     const uint32_t waves = (uint32_t)((cols + 512 * v - 1) / (512 * v));
@@ -453,15 +454,23 @@ static uint32_t blocks_of(uint64_t rows, uint64_t cols)
     return (uint32_t)std::min<uint64_t>((rows + t.y - 1) / t.y, 256 * std::max(1u, room / waves));
 }
 
-template <typename T, typename R> static hipError_t launch_forward(const NormForward &a, hipStream_t s)
+template <typename T, typename R> static hipError_t launch_forward(NormForward a, hipStream_t s)
 {
     const int v = row_registers(a.cols);
-    const dim3 threads = row_threads(a.cols, v), grid((a.rows + threads.y - 1) / threads.y);
-    if (v == 1) k_norm_forward<T, R, 1><<<grid, threads, 0, s>>>(a);
-    else if (v == 2) k_norm_forward<T, R, 2><<<grid, threads, 0, s>>>(a);
-    else if (v == 4) k_norm_forward<T, R, 4><<<grid, threads, 0, s>>>(a);
-    else k_norm_forward<T, R, 8><<<grid, threads, 0, s>>>(a);
-    return hipGetLastError();
+    const dim3 threads = row_threads(a.cols, v);
+    const uint32_t rows = a.rows;
+    for (uint32_t first = 0; first < rows; first += kRowsALaunch) {
+        const uint32_t n = std::min(rows - first, kRowsALaunch), grid = (n + threads.y - 1) / threads.y;
+        a.first = first;
+        a.rows = first + n;
+        if (v == 1) k_norm_forward<T, R, 1><<<grid, threads, 0, s>>>(a);
+        else if (v == 2) k_norm_forward<T, R, 2><<<grid, threads, 0, s>>>(a);
+        else if (v == 4) k_norm_forward<T, R, 4><<<grid, threads, 0, s>>>(a);
+        else k_norm_forward<T, R, 8><<<grid, threads, 0, s>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <typename T, typename R> static hipError_t launch_backward(const NormBackward &a, uint32_t blocks, hipStream_t s)
@@ -476,6 +485,8 @@ template <typename T, typename R> static hipError_t launch_backward(const NormBa
     else k_norm_backward<T, R, 8, false><<<blocks, threads, 0, s>>>(a);
     return hipGetLastError();
 }
+
+constexpr uint64_t kMaxBlocks256 = 0xffffff;            // a grid has less than 2^32 threads: blocks of 256
 
 static bool is_float_type(int t) { return t == REFT_F32 || t == REFT_BF16 || t == REFT_F16; }
 static bool is_eight(int t) { return t == REFT_E4M3 || t == REFT_E5M2; }
@@ -532,7 +543,7 @@ extern "C" int reft_dropout(const void *x, uint64_t ld_x, void *y, uint64_t ld_y
     a.total = a.groups * rows;
     a.inverse = (uint32_t)std::min<uint64_t>((1ull << 32) / a.groups, 0xffffffffu);
     const uint64_t blocks = (a.total + 256 * kDropUnroll - 1) / (256 * kDropUnroll);
-    NEED(blocks <= 0x7fffffff, REFT_ESIZE, "reft_dropout: too many values");
+    NEED(blocks <= kMaxBlocks256, REFT_ESIZE, "reft_dropout: too many values");
     hipStream_t s = (hipStream_t)stream;
     const bool lines = on_lines(x, ld_x * size_of(dtype));
     if (dtype == REFT_F32) launch_dropout<float>(a, lines, (uint32_t)blocks, s);
@@ -689,12 +700,12 @@ extern "C" int reft_quantize(const void *x, uint64_t ld_x, uint64_t rows, uint64
     NEED(q || q_t || !rows || !cols, REFT_EINVAL, "reft_quantize: no output");
     NEED((!q || scales || !rows || !cols) && (!q_t || scales_t || !rows || !cols), REFT_EINVAL, "reft_quantize: 8 bits without scales");
     // the grid counts tiles, or, in its second dimension, words of columns
-    NEED(rows <= 0x7fffffff && cols <= 128 * 65535, REFT_ESIZE, "reft_quantize: too many rows or columns");
+    NEED(rows < (1u << 26) && cols <= 128 * 65535, REFT_ESIZE, "reft_quantize: too many rows or columns");
     NEED(ld_x >= cols && (!q || ld_q >= cols) && (!q_t || ld_qt >= rows), REFT_ESIZE, "reft_quantize: rows overlap");
     NEED((!q || ld_s >= (blocks ? (rows + 127) / 128 : rows)) && (!q_t || ld_st >= (blocks ? (cols + 127) / 128 : cols)),
          REFT_ESIZE, "reft_quantize: words of scales overlap");
     if (!rows || !cols) return REFT_OK;
-    NEED((rows + 127) / 128 * ((cols + 127) / 128) <= 0x7fffffff, REFT_ESIZE, "reft_quantize: too many values");
+    NEED((rows + 127) / 128 * ((cols + 127) / 128) <= kMaxBlocks256, REFT_ESIZE, "reft_quantize: too many values");
     NEED(x, REFT_EINVAL, "reft_quantize: null pointer");
     NEED(lies(x, size_of(dtype)), REFT_EINVAL, "reft_quantize: misaligned pointer");
     a.x = x;

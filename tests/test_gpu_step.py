@@ -440,6 +440,32 @@ def test_product_of_whole_numbers(dev, M, N, K, blocks, out, fa, fb, pad, lead):
     assert untouched(raw, c)
 
 
+# The largest tiles (three rounds of small ones and more, K from 3600 on), and K cut into parts whose last ends anywhere.
+LARGE = [(2900, 3000, 3712), (2900, 3000, 3632), (2817, 3100, 3701), (60, 520, 4097), (33, 2000, 3000), (200, 300, 9001), (512, 1024, 3200),
+         (1001, 770, 5128)]
+
+
+@pytest.mark.parametrize("M,N,K", LARGE)
+@pytest.mark.parametrize("out,blocks,fa", [("bf16", True, "e4m3"), ("f32", False, "e5m2"), ("f16", False, "e4m3")])
+def test_product_of_whole_numbers_large(dev, M, N, K, out, blocks, fa):
+    """As above; the reference is multiplied in fp64 on the GPU, where sums of whole numbers are exact too."""
+    a, va = whole_numbers(dev, M + K, M, K, fa, -K % 16, 0)
+    b, vb = whole_numbers(dev, N + 2 * K, N, K, "e4m3", -K % 16, 0)
+    tall = -(-N // 128) if blocks else N
+    sa, sb = powers(dev, 1, M, K, -1, 1), powers(dev, 2, tall, K, -1, 1)
+    raw, c = padded(dev, M, N, DT[out], 3, 1)
+    ws = torch.empty(reft.reft_product_workspace(M, N, K), dtype=torch.uint8, device=dev)
+    reft.reft_product(a, sa, b, sb, c, ws, b_blocks=blocks)
+
+    def factors(s, rows, tall):
+        f = torch.exp2(s.double() - 127).transpose(0, 1).reshape(s.shape[1], -1)[:, :-(-K // 128)]
+        return f.repeat_interleave(tall, 0)[:rows].repeat_interleave(128, 1)[:, :K]
+
+    want = (va.double() * factors(sa, M, 1)) @ (vb.double() * factors(sb, N, 128 if blocks else 1)).t()
+    assert torch.equal(c, want.float().to(DT[out]))
+    assert untouched(raw, c)
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 272, 4096), (5, 700, 1000), (60, 520, 2000), (130, 300, 4097), (700, 520, 1600)])
 @pytest.mark.parametrize("blocks", [False, True])
 @pytest.mark.parametrize("out,limit", [("f32", 1e-6), ("bf16", 2.0 ** -9), ("f16", 2.0 ** -11)])
