@@ -9,6 +9,7 @@ Pointers may be given as ``torch.Tensor`` (its ``data_ptr()`` is used), as ``int
 from __future__ import annotations
 
 import ctypes
+import importlib
 import os
 from typing import Optional, Sequence
 
@@ -42,6 +43,7 @@ REFT_F32, REFT_BF16, REFT_F16, REFT_E4M3, REFT_E5M2 = 0, 1, 2, 3, 4
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libreft.so")
 _lib = None
+_marshal = None
 
 
 class ReftError(RuntimeError):
@@ -127,6 +129,14 @@ def _load():
     return lib
 
 
+def _load_marshal():
+    global _marshal
+    if _marshal is None:
+        _load()
+        _marshal = importlib.import_module("._marshal", __package__)
+    return _marshal
+
+
 # ------------------------------------------------------------------------------------------------
 # marshalling
 # ------------------------------------------------------------------------------------------------
@@ -167,6 +177,11 @@ def _stream(s) -> Optional[int]:
     if isinstance(s, int):
         return s or None
     return s.cuda_stream or None
+
+
+def _done(rc: int) -> None:
+    if rc < 0:
+        _check(rc)
 
 
 def _check(rc: int) -> int:
@@ -425,7 +440,7 @@ def reft_restore_wait(plan) -> None:
 # ------------------------------------------------------------------------------------------------
 _TYPES = {"torch.float32": REFT_F32, "torch.bfloat16": REFT_BF16, "torch.float16": REFT_F16,
           "torch.float8_e4m3fn": REFT_E4M3, "torch.float8_e5m2": REFT_E5M2}
-_TYPE_OF: dict = {}                       # the same by torch.dtype, filled as they are met
+_TYPE_OF: dict = {}                       # the same by torch.dtype, filled as they are met (and told to _marshal)
 _FLOATS, _EIGHTS = (REFT_F32, REFT_BF16, REFT_F16), (REFT_E4M3, REFT_E5M2)
 _OR_F32 = {REFT_F32: (REFT_F32,), REFT_BF16: (REFT_BF16, REFT_F32), REFT_F16: (REFT_F16, REFT_F32)}
 _ONLY = {c: (c,) for c in _FLOATS + _EIGHTS}
@@ -437,23 +452,22 @@ def _refuse(who: str, what: str):
     raise ReftError(REFT_EINVAL, f"{who}: {what}")
 
 
-# A call's time on the host is mostly spent here: the usual case first, everything else in the functions behind.
+def _type(t):
+    """The number of a tensor's type; None if no operator takes it."""
+    code = _TYPE_OF.get(t.dtype)
+    if code is None and str(t.dtype) in _TYPES:
+        code = _TYPE_OF[t.dtype] = _TYPES[str(t.dtype)]
+        _load_marshal().know(t.dtype, code)
+    return code
+
+
+# Each operator's call goes through _marshal first (reft_marshal.c), which makes it where every operand is as expected.  What
+# follows takes what is unusual but right (a type met for the first time, one row of any stride, no weight), and says what is wrong.
 def _matrix(who: str, name: str, t, shape, types):
     """(address, row length, type) of a 2-D tensor of that shape whose rows are contiguous."""
-    if t.shape == shape:
-        code = _TYPE_OF.get(t.dtype)
-        down, along = t.stride()
-        if along == 1 and down >= shape[1] and code in types:
-            return t.data_ptr(), down, code
-    return _other_matrix(who, name, t, shape, types)
-
-
-def _other_matrix(who, name, t, shape, types):
     if len(shape) != 2 or tuple(t.shape) != tuple(shape):
         _refuse(who, f"{name} has the shape {tuple(t.shape)}" + (f", not {tuple(shape)}" if len(shape) == 2 else ""))
-    if str(t.dtype) in _TYPES:
-        _TYPE_OF[t.dtype] = _TYPES[str(t.dtype)]
-    code = _TYPE_OF.get(t.dtype)
+    code = _type(t)
     if code not in types:
         _refuse(who, f"{name} is {t.dtype}")
     down, along = t.stride()
@@ -462,25 +476,12 @@ def _other_matrix(who, name, t, shape, types):
     return t.data_ptr(), down if shape[0] > 1 else shape[1], code
 
 
-def _first(who: str, name: str, t, types):
-    """The same of a call's first matrix, whose shape the others go by."""
-    code = _TYPE_OF.get(t.dtype)
-    if code in types and t.dim() == 2:
-        down, along = t.stride()
-        if along == 1 and down >= t.shape[1]:
-            return t.data_ptr(), down, code
-    return _other_matrix(who, name, t, t.shape, types)
-
-
 def _vector(who: str, name: str, t, n: int, types):
     """(address, type) of a contiguous vector of n values."""
-    code = _TYPE_OF.get(t.dtype)
-    if code in types and t.shape == (n,) and t.is_contiguous():
-        return t.data_ptr(), code
-    if code is None and str(t.dtype) in _TYPES:
-        _TYPE_OF[t.dtype] = _TYPES[str(t.dtype)]
-        return _vector(who, name, t, n, types)
-    _refuse(who, f"{name} is no contiguous vector of {n} values of a type that it may have")
+    code = _type(t)
+    if code not in types or t.shape != (n,) or not t.is_contiguous():
+        _refuse(who, f"{name} is no contiguous vector of {n} values of a type that it may have")
+    return t.data_ptr(), code
 
 
 def _scales(who: str, name: str, t, rows: int, cols: int):
@@ -489,8 +490,6 @@ def _scales(who: str, name: str, t, rows: int, cols: int):
     if t.shape != (words, rows, 4) or t.element_size() != 1:
         _refuse(who, f"{name} are not bytes [{words}][{rows}][4]")
     wide, row, one = t.stride()
-    if one == 1 and row == 4 and wide == 4 * rows:
-        return t.data_ptr(), rows
     if (one != 1 or (rows > 1 and row != 4) or (words > 1 and wide % 4)) and t.numel():
         _refuse(who, f"{name}: the words of a row's scales are not contiguous")
     return t.data_ptr(), wide // 4 if words > 1 else rows
@@ -502,7 +501,10 @@ def _scratch(t):
 
 def reft_dropout(x, y, p: float, seed: int, offset: int = 0, stream=None) -> None:
     """``y`` (may be ``x``) gets ``x`` with elements dropped by the counter (seed, offset)."""
-    ax, ld_x, code = _first("reft_dropout", "x", x, _FLOATS)
+    rc = (_marshal or _load_marshal()).dropout(x, y, p, seed, offset, stream)
+    if rc is not None:
+        return _done(rc)
+    ax, ld_x, code = _matrix("reft_dropout", "x", x, x.shape, _FLOATS)
     rows, cols = shape = x.shape
     ay, ld_y, _ = _matrix("reft_dropout", "y", y, shape, _ONLY[code])
     _check(_load().reft_dropout(ax, ld_x, ay, ld_y, rows, cols, code, p, seed, offset, _stream(stream)))
@@ -510,8 +512,11 @@ def reft_dropout(x, y, p: float, seed: int, offset: int = 0, stream=None) -> Non
 
 def reft_norm_forward(x, residual, weight, eps: float, p: float = 0.0, seed: int = 0, offset: int = 0, *, h=None,
                       rstd=None, y=None, q=None, scales=None, stream=None) -> None:
+    rc = (_marshal or _load_marshal()).norm_forward(x, residual, weight, eps, p, seed, offset, h, rstd, y, q, scales, stream)
+    if rc is not None:
+        return _done(rc)
     who = "reft_norm_forward"
-    ax, ld_x, code = _first(who, "x", x, _FLOATS)
+    ax, ld_x, code = _matrix(who, "x", x, x.shape, _FLOATS)
     rows, cols = shape = x.shape
     wide = _OR_F32[code]
     ar, ld_r, r_code = (None, 0, None) if residual is None else _matrix(who, "residual", residual, shape, wide)
@@ -528,8 +533,11 @@ def reft_norm_forward(x, residual, weight, eps: float, p: float = 0.0, seed: int
 
 def reft_norm_backward(dy, dh, h, rstd, weight, p: float = 0.0, seed: int = 0, offset: int = 0, *, dres=None, dx=None,
                        dweight=None, workspace=None, stream=None) -> None:
+    rc = (_marshal or _load_marshal()).norm_backward(dy, dh, h, rstd, weight, p, seed, offset, dres, dx, dweight, workspace, stream)
+    if rc is not None:
+        return _done(rc)
     who = "reft_norm_backward"
-    ady, ld_dy, code = _first(who, "dy", dy, _FLOATS)
+    ady, ld_dy, code = _matrix(who, "dy", dy, dy.shape, _FLOATS)
     rows, cols = shape = dy.shape
     wide = _OR_F32[code]
     ah, ld_h, r_code = _matrix(who, "h", h, shape, wide)
@@ -551,8 +559,11 @@ def reft_norm_backward_workspace(rows: int, cols: int) -> int:
 
 def reft_quantize(x, q=None, scales=None, q_t=None, scales_t=None, *, blocks: bool = False, stream=None) -> None:
     """``q`` and ``q_t`` are float8 tensors of the shape of ``x`` and of its transpose."""
+    rc = (_marshal or _load_marshal()).quantize(x, q, scales, q_t, scales_t, blocks, stream)
+    if rc is not None:
+        return _done(rc)
     who = "reft_quantize"
-    ax, ld_x, code = _first(who, "x", x, _FLOATS)
+    ax, ld_x, code = _matrix(who, "x", x, x.shape, _FLOATS)
     rows, cols = shape = x.shape
     aq, ld_q, fmt = (None, 0, None) if q is None else _matrix(who, "q", q, shape, _EIGHTS)
     at, ld_t, fmt_t = _NONE if q_t is None else _matrix(who, "q_t", q_t, (cols, rows), _EIGHTS if fmt is None else _ONLY[fmt])
@@ -565,9 +576,12 @@ def reft_quantize(x, q=None, scales=None, q_t=None, scales_t=None, *, blocks: bo
 
 def reft_product(a, a_scales, b, b_scales, c, workspace=None, *, b_blocks: bool = False, stream=None) -> None:
     """``c`` [M, N] = ``a`` [M, K] times the transpose of ``b`` [N, K], both float8 with their scales."""
+    rc = (_marshal or _load_marshal()).product(a, a_scales, b, b_scales, c, workspace, b_blocks, stream)
+    if rc is not None:
+        return _done(rc)
     who = "reft_product"
-    aa, ld_a, fa = _first(who, "a", a, _EIGHTS)
-    ab, ld_b, fb = _first(who, "b", b, _EIGHTS)
+    aa, ld_a, fa = _matrix(who, "a", a, a.shape, _EIGHTS)
+    ab, ld_b, fb = _matrix(who, "b", b, b.shape, _EIGHTS)
     M, K = a.shape
     N, K2 = b.shape
     if K != K2:

@@ -1,14 +1,16 @@
-"""Compile libreft.so for gfx950 with hipcc (cross-compiles without a GPU)."""
+"""Compile libreft.so for gfx950 with hipcc (cross-compiles without a GPU), and the binding's C part with gcc."""
 from __future__ import annotations
 
 import os
 import re
 import subprocess
+import sysconfig
 import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libreft.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")      # the operators' arguments from Python, in C (reft_marshal.c)
 SOURCES = ["reft_api.hip", "reft_kernels.hip", "reft_stream.hip", "reft_step.hip",
            "reft_product.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
@@ -72,6 +74,11 @@ def build(verbose: bool = False) -> str:
                               stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
         if link.returncode != 0:
             raise RuntimeError("hipcc failed:\n" + link.stdout)
+    marshal = subprocess.run(["gcc", "-O2", "-std=c11", "-Wall", "-fPIC", "-shared", "-I", sysconfig.get_paths()["include"], "-o", MARSHAL,
+                              os.path.join(CSRC, "reft_marshal.c"), "-L", HERE, "-l:libreft.so", "-Wl,-rpath,$ORIGIN"],
+                             stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if marshal.returncode != 0:
+        raise RuntimeError("gcc failed:\n" + marshal.stdout)
     output = "\n".join(outs)
     counts = check_burst_registers(output)
     if verbose:

@@ -555,6 +555,38 @@ def test_on_another_stream(dev):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_unusual_operands_that_are_right(dev):
+    """One row of any stride, one column, a stream as a number, scales whose words have gaps: as the usual ones."""
+    row = normal(dev, 1, 40, 1).t()                      # (1, 40) with strides (1, 1)
+    usual = row.contiguous()
+    a, b = torch.empty(1, 40, device=dev), torch.empty(1, 40, device=dev)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    reft.reft_dropout(row, a, 0.3, 5, 6, side.cuda_stream)
+    reft.reft_dropout(usual, b, 0.3, 5, 6, side)
+    side.synchronize()
+    assert torch.equal(a, b)
+    w = torch.ones(40, device=dev)
+    reft.reft_norm_forward(row, None, w, 1e-5, y=a)
+    reft.reft_norm_forward(usual, None, w, 1e-5, y=b)
+    assert torch.equal(a, b)
+    column = normal(dev, 2, 1, 40).t()                   # (40, 1) with strides (1, 40)
+    c, d = torch.empty(40, 1, device=dev), torch.empty(40, 1, device=dev)
+    reft.reft_dropout(column, c, 0.3, 5, 6)
+    reft.reft_dropout(column.contiguous(), d, 0.3, 5, 6)
+    assert torch.equal(c, d)
+    x = normal(dev, 3, 7, 1100)
+    q, r = (torch.empty(7, 1100, dtype=torch.uint8, device=dev).view(F8["e4m3"]) for _ in range(2))
+    gaps, tight = torch.zeros(3, 9, 4, dtype=torch.uint8, device=dev), scales_like(dev, 7, 1100)
+    reft.reft_quantize(x, q, gaps[:, :7])
+    reft.reft_quantize(x, r, tight)
+    assert torch.equal(q.view(torch.uint8), r.view(torch.uint8)) and torch.equal(gaps[:, :7], tight) and not gaps[:, 7:].any()
+    e, f = torch.empty(7, 7, device=dev), torch.empty(7, 7, device=dev)
+    reft.reft_product(q, gaps[:, :7], q, tight, e)
+    reft.reft_product(q, tight, q, tight, f)
+    assert torch.equal(e, f) and e.any()
+
+
 def test_in_a_graph(dev):
     s = chain_state(dev)
     want = [t.clone() for t in chain(dev, s)]
