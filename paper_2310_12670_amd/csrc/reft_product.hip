@@ -136,6 +136,8 @@ __device__ __forceinline__ void store_tile(const ProductArgs &p, uint32_t m, uin
 }
 
 // ---- any sizes, any alignment: tiles of 128 x 128, four waves of 64 x 64 -----------------------------------------
+// The next tile is loaded to registers while one is multiplied, and then written to LDS: what 16-byte copies to LDS need of alignment,
+// this does not.  8192 x 4096 x 4096 to bf16: 276 us, where rows on 16 bytes take 111.
 template <int FA, int FB, bool EXACT> __global__ __launch_bounds__(256) void k_product_any(ProductArgs p)
 {
     __shared__ __align__(16) uint8_t tile[2][2][128 * 128];
@@ -388,7 +390,10 @@ __device__ __forceinline__ void store_all(T *c, uint64_t ld_c, const ProductArgs
     }
 }
 
-// T: what is stored, into C or, of several parts of K, into a part's place.
+// T: what is stored, into C or, of several parts of K, into a part's place.  The waves are one to a SIMD with the largest tile (its sums
+// take 256 registers), so that all overlap is in the order of a wave's own instructions.  8192 x 28672 x 8192 to bf16: 1354 us, 2.84
+// PFLOP/s, at 1.76 GHz (power) with the matrix cores busy 76 % of the cycles; 11008 x 4096 x 8192 to fp32: 555 us, 1.33 PFLOP/s, bound by the
+// widening of operands; 1001 x 5120 x 1728 to bf16: 17.4 us, bound by the latency of 14 steps.
 template <int FA, int FB, bool EXACT, typename T, int MT, int NT>
 __global__ __launch_bounds__(256, MT * NT >= 16 ? 1 : 2) void k_product(ProductArgs p)
 {
@@ -545,7 +550,7 @@ __global__ __launch_bounds__(256, MT * NT >= 16 ? 1 : 2) void k_product(ProductA
     else store_all((T *)p.c, p.ld_c, p, room, m, n, lane, acc);
 }
 
-// C from the parts of K, added in their order; four neighbouring columns a thread.
+// C from the parts of K, added in their order; four neighbouring columns a thread.  A launch more: 2 to 3 us.
 template <typename T> __global__ __launch_bounds__(256) void k_add_parts(ProductArgs p)
 {
     const uint32_t wide = (p.N + 3) / 4;

@@ -22,8 +22,9 @@ struct DropoutArgs {
 
 constexpr int kDropUnroll = 4;
 
-// A thread takes kDropUnroll groups.  Row and group of a block's first come of one division of whole numbers, those of
-// its threads of a multiplication.
+// y = keep ? x s : 0.  A thread takes kDropUnroll groups.  Row and group of a block's first come of one division of whole numbers,
+// those of its threads of a multiplication.  Bound by HBM: 16384 x 11008 in bf16 114 us, 6.3 TB/s, and as much without a mask, so that
+// the generator's ten rounds cost nothing.
 template <typename T, bool STREAM> __global__ __launch_bounds__(256) void k_dropout(DropoutArgs a)
 {
     const uint64_t first = (uint64_t)blockIdx.x * (256 * kDropUnroll);
@@ -92,8 +93,10 @@ __device__ __forceinline__ float row_sum(float v, float *room)
     return v;
 }
 
-// A row belongs to the threads of one y (64 to 1024 of them); each holds V times eight neighbouring columns of it in registers: one
+// h = residual + dropout(x), h / rms(h) weight, in 8 bits too.  A row belongs to the threads of one y (64 to 1024 of them); each holds V times eight neighbouring columns of it in registers: one
 // pass over the inputs whatever the row's length.  A wave's 512 columns are four blocks of 128, 16 lanes each: one word of scales.
+// Bound by HBM: 16384 x 5120 in bf16 with an fp32 residual and 8-bit output 161 us, 5.7 TB/s; one row of 8192 3.2 us.  (Fewer, wider waves:
+// 171 us; blocks that loop over rows with the next one in flight: 201; reading past the L2: 173.)
 template <typename T, typename R, int V> __global__ __launch_bounds__(1024) void k_norm_forward(NormForward a)
 {
     __shared__ float room[16];
@@ -164,22 +167,18 @@ struct NormBackward {
 };
 
 // Rows as above.  A block takes every so manyth row (or, of short rows, blockDim.y of them) and keeps its part of the weight's
-// gradient in registers; k_sum_parts adds the blocks' parts in their order.  Of rows with more than eight columns a lane the operands
-// are read again for the second half of the work (from the L2) rather than held.
+// gradient in registers; k_sum_parts adds the blocks' parts in their order.  Of rows with eight columns a lane the next one is fetched
+// while one is worked on; of wider ones the operands are read again for the second half of the work (from the L2) rather than held.
+// Bound by HBM: 16384 x 8192 in bf16 with residual 228 us, 5.9 TB/s.
 template <typename T, typename R, int V, bool STREAM> __global__ __launch_bounds__(1024) void k_norm_backward(NormBackward a)
 {
     __shared__ float room[2][16];
     __shared__ float fold[V == 1 ? 3 * 512 : 1];
     const int first = threadIdx.x * 8, wide = blockDim.x * 8, cols = (int)a.cols;
     const uint32_t step = gridDim.x * blockDim.y;
-    constexpr bool kHeld = V <= 2;                           // the weights
     float dw[V][8] = {}, w[V][8];
-    auto fetch_w = [&](int v) {
-        load8_of<T>(a.weight, a.weight_f32, first + v * wide, cols - first - v * wide, w[v]);
-    };
-    if (kHeld)
 #pragma unroll
-        for (int v = 0; v < V; ++v) fetch_w(v);
+    for (int v = 0; v < V; ++v) load8_of<T>(a.weight, a.weight_f32, first + v * wide, cols - first - v * wide, w[v]);
     Eight<T> dy[V], next_dy;
     Eight<R> h[V], dh[V], next_h, next_dh;
     float rstd, next_rstd;
@@ -217,14 +216,12 @@ template <typename T, typename R, int V, bool STREAM> __global__ __launch_bounds
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (V > 1) fetch(v, row);
-            if (!kHeld) fetch_w(v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float part = dy[v][i] * (h[v][i] * rstd);
                 dw[v][i] += part;
                 dot += part * w[v][i];
             }
-            if (!kHeld) asm volatile("" ::: "memory");       // eight columns at a time: registers
         }
         dot = row_sum(dot, room[half]) / (float)cols;        // this half is written again two rows on, behind another barrier
         if (!there) continue;
@@ -233,7 +230,6 @@ template <typename T, typename R, int V, bool STREAM> __global__ __launch_bounds
             const int c = first + v * wide;
             float o[8];
             if (V > 1) fetch(v, row), fetch_dh(v, row);
-            if (!kHeld) fetch_w(v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] = dh[v][i] + rstd * (dy[v][i] * w[v][i] - h[v][i] * rstd * dot);
             if (a.dres) store8((R *)a.dres + row * a.ld_dres + c, cols - c, o);
@@ -241,7 +237,6 @@ template <typename T, typename R, int V, bool STREAM> __global__ __launch_bounds
                 if (a.d.threshold) drop8(a.d, row, (uint32_t)c / 8, o);
                 store8((T *)a.dx + row * a.ld_dx + c, cols - c, o);
             }
-            if (!kHeld) asm volatile("" ::: "memory");
         }
     }
     if (!a.part) return;
@@ -262,7 +257,75 @@ template <typename T, typename R, int V, bool STREAM> __global__ __launch_bounds
     }
 }
 
+// Rows of more than 16384 columns: nothing is held, the operands are read again for the second half (from the L2), and the weight's
+// gradient, which would take all registers, is k_weight_parts'.  4096 x 65536 in bf16:
+// 787 us with that, 3.4 TB/s of what has to move (1821 with all sums in registers, which spill).
+template <typename T, typename R> __global__ __launch_bounds__(1024) void k_norm_backward_wide(NormBackward a)
+{
+    __shared__ float room[2][16];
+    const int cols = (int)a.cols;
+    int half = 0;
+    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x, half ^= 1) {
+        const R *h_row = (const R *)a.h + row * a.ld_h, *dh_row = (const R *)a.dh + row * a.ld_dh;
+        const T *dy_row = (const T *)a.dy + row * a.ld_dy;
+        const float rstd = a.rstd[row];
+        float dot = 0;
+#pragma unroll 2
+        for (int c = threadIdx.x * 8; c < cols; c += blockDim.x * 8) {
+            float h[8], dy[8], w[8];
+            load8<false>(h_row + c, cols - c, h);
+            load8<false>(dy_row + c, cols - c, dy);
+            load8_of<T>(a.weight, a.weight_f32, c, cols - c, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dot += dy[i] * (h[i] * rstd) * w[i];
+        }
+        dot = row_sum(dot, room[half]) / (float)cols;
+        for (int c = threadIdx.x * 8; c < cols; c += blockDim.x * 8) {
+            float h[8], dy[8], w[8], o[8];
+            load8<false>(h_row + c, cols - c, h);
+            load8<false>(dy_row + c, cols - c, dy);
+            load8<false>(dh_row + c, a.dh ? cols - c : 0, o);
+            load8_of<T>(a.weight, a.weight_f32, c, cols - c, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] += rstd * (dy[i] * w[i] - h[i] * rstd * dot);
+            if (a.dres) store8((R *)a.dres + row * a.ld_dres + c, cols - c, o);
+            if (a.dx) {
+                if (a.d.threshold) drop8(a.d, row, (uint32_t)c / 8, o);
+                store8((T *)a.dx + row * a.ld_dx + c, cols - c, o);
+            }
+        }
+    }
+}
+
+// The weight's gradient alone: a block takes 512 columns and, with each of its four waves, every so manyth row.
+template <typename T, typename R> __global__ __launch_bounds__(256) void k_weight_parts(NormBackward a)
+{
+    __shared__ float fold[3][512];
+    const int c = blockIdx.x * 512 + threadIdx.x * 8, n = (int)a.cols - c;
+    float dw[8] = {};
+#pragma unroll 2
+    for (uint32_t row = blockIdx.y * 4 + threadIdx.y; row < a.rows; row += gridDim.y * 4) {
+        const float rstd = a.rstd[row];
+        float h[8], dy[8];
+        load8<false>((const R *)a.h + row * a.ld_h + c, n, h);
+        load8<false>((const T *)a.dy + row * a.ld_dy + c, n, dy);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[i] += dy[i] * (h[i] * rstd);
+    }
+    if (threadIdx.y > 0)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) fold[threadIdx.y - 1][threadIdx.x * 8 + i] = dw[i];
+    __syncthreads();
+    if (threadIdx.y > 0) return;
+#pragma unroll
+    for (int y = 0; y < 3; ++y)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[i] += fold[y][threadIdx.x * 8 + i];
+    store8(a.part + (uint64_t)blockIdx.y * a.cols + c, n, dw);
+}
+
 // out[c] = sum of n rows of part, in an order that depends on n alone: 64 interleaved sums, then those one after the other.
+// 256 parts of 8192 columns: 5.3 us.
 __global__ __launch_bounds__(1024) void k_sum_parts(const float *part, uint32_t n, uint32_t cols, float *out)
 {
     __shared__ float sums[64][16];
@@ -290,7 +353,8 @@ struct QuantizeArgs {
     uint8_t e5m2;
 };
 
-// A scale for each 128 columns of a row: a wave takes 512 columns of a row, 16 lanes each block.
+// A scale for each 128 columns of a row: a wave takes 512 columns of a row, 16 lanes each block.  Bound by HBM: 16384 x 8192 in bf16 77 us,
+// 5.3 TB/s.
 template <typename T> __global__ __launch_bounds__(256) void k_quantize_rows(QuantizeArgs a)
 {
     const int lane = threadIdx.x & 63;
@@ -318,7 +382,8 @@ __device__ __forceinline__ void store_scale(uint8_t *scales, uint64_t ld, uint64
 
 // A tile of 128 x 128 values, in registers: a thread holds 8 rows of 8 columns, so that each of its columns is 8 bytes of
 // the transpose, which leaves through LDS in whole rows.  BLOCKS: one scale for the tile, else one for each row and, in the
-// transpose, for each column.  LINES: the results' rows lie on cache lines, which a tile then writes whole.
+// transpose, for each column.  LINES: the results' rows lie on cache lines, which a tile then writes whole.  Bound by HBM where large:
+// 3584 x 8192 in bf16, blocks and both orders, 19.4 us, 6.0 TB/s (31 with values widened once and held in fp32).
 template <typename T, bool BLOCKS, bool LINES> __global__ __launch_bounds__(256) void k_quantize_tile(QuantizeArgs a)
 {
     constexpr int kPitch = 1024 + 32;          // LDS bytes of eight columns of 128 rows: 16 lanes' writes meet no bank twice
@@ -448,6 +513,7 @@ static int row_registers(uint64_t cols) { return cols <= 8192 ? 1 : cols <= 1638
 // x 5120 179 (two rounds), 152 and 152, x 1155 79, 94 and 111.
 static uint32_t blocks_of(uint64_t rows, uint64_t cols)
 {
+    if (row_registers(cols) > 2) return (uint32_t)std::min<uint64_t>((rows + 3) / 4, 32);
     const dim3 t = row_threads(cols, row_registers(cols));
     const uint32_t waves = t.x * t.y / 64, room = cols % 64 ? 16 : 12;
     if (rows <= 4 * t.y) return rows ? 1 : 0;                // one block is done before a second launch would be
@@ -481,8 +547,11 @@ template <typename T, typename R> static hipError_t launch_backward(const NormBa
     if (v == 1 && lines) k_norm_backward<T, R, 1, true><<<blocks, threads, 0, s>>>(a);
     else if (v == 1) k_norm_backward<T, R, 1, false><<<blocks, threads, 0, s>>>(a);
     else if (v == 2) k_norm_backward<T, R, 2, false><<<blocks, threads, 0, s>>>(a);
-    else if (v == 4) k_norm_backward<T, R, 4, false><<<blocks, threads, 0, s>>>(a);
-    else k_norm_backward<T, R, 8, false><<<blocks, threads, 0, s>>>(a);
+    else {
+        // the weight's gradient first: the others may take the place of what it reads
+        if (a.part) k_weight_parts<T, R><<<dim3((a.cols + 511) / 512, blocks), dim3(64, 4), 0, s>>>(a);
+        if (a.dres || a.dx) k_norm_backward_wide<T, R><<<std::min(a.rows, 512u), 1024, 0, s>>>(a);
+    }
     return hipGetLastError();
 }
 
