@@ -137,20 +137,22 @@ __device__ __forceinline__ void store_tile(const ProductArgs &p, uint32_t m, uin
 
 // ---- any sizes, any alignment: tiles of 128 x 128, four waves of 64 x 64 -----------------------------------------
 // The next tile is loaded to registers while one is multiplied, and then written to LDS: what 16-byte copies to LDS need of alignment,
-// this does not.  8192 x 4096 x 4096 to bf16: 276 us, where rows on 16 bytes take 111.
+// this does not.  8192 x 4096 x 4096 to bf16: 276 us, where rows on 16 bytes take 111.  K is multiplied in the order of k_product and cut
+// into the same parts, so that where and how far apart the rows lie does not change a bit of the result.
 template <int FA, int FB, bool EXACT> __global__ __launch_bounds__(256) void k_product_any(ProductArgs p)
 {
     __shared__ __align__(16) uint8_t tile[2][2][128 * 128];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint32_t m0 = blockIdx.y * 128, n0 = blockIdx.x * 128;
     const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
-    const uint32_t steps = (p.K + 127) / 128;
+    const uint32_t all = (p.K + 127) / 128, start = blockIdx.z * p.split_steps;
+    const uint32_t steps = p.splits > 1 ? min(all - start, p.split_steps) : all;        // no part is empty
     w32x4 next[2][4];
     auto load = [&](uint32_t step) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = (tid >> 3) + 32 * i;
-            const uint32_t k = step * 128 + (tid & 7) * 16;
+            const uint32_t k = (start + step) * 128 + (tid & 7) * 16;
             const int n = k < p.K ? (int)min(p.K - k, 16u) : 0;
             next[0][i] = load16(p.a + (m0 + r) * p.ld_a + k, m0 + r < p.M ? n : 0);
             next[1][i] = load16(p.b + (n0 + r) * p.ld_b + k, n0 + r < p.N ? n : 0);
@@ -177,8 +179,8 @@ template <int FA, int FB, bool EXACT> __global__ __launch_bounds__(256) void k_p
         if (step % 4 == 0) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                sa[i] = p.sa[step / 4 * p.ld_sa + min(m0 + wm + i * 32 + (lane & 31), p.M - 1)];
-                sb[i] = p.sb[step / 4 * p.ld_sb + (min(n0 + wn + i * 32 + (lane & 31), p.N - 1) >> p.b_shift)];
+                sa[i] = p.sa[(start + step) / 4 * p.ld_sa + min(m0 + wm + i * 32 + (lane & 31), p.M - 1)];
+                sb[i] = p.sb[(start + step) / 4 * p.ld_sb + (min(n0 + wn + i * 32 + (lane & 31), p.N - 1) >> p.b_shift)];
             }
         }
 #pragma unroll
@@ -201,6 +203,11 @@ template <int FA, int FB, bool EXACT> __global__ __launch_bounds__(256) void k_p
             sb[i] >>= 8;
         }
         if (step + 1 < steps) keep(half ^ 1);
+    }
+    if (p.splits > 1) {
+        p.c = p.parts + (uint64_t)blockIdx.z * p.M * p.N;
+        p.c_type = REFT_F32;
+        p.ld_c = p.N;
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -620,6 +627,15 @@ static bool on_16_bytes(const ProductArgs &p)
     return p.K && ((uintptr_t)p.a | (uintptr_t)p.b | p.ld_a | p.ld_b) % 16 == 0 && p.ld_a < (1u << 23) && p.ld_b < (1u << 23);
 }
 
+static hipError_t add_parts(const ProductArgs &p, hipStream_t s)
+{
+    const uint32_t blocks = (uint32_t)(((uint64_t)p.M * ((p.N + 3) / 4) + 255) / 256);
+    if (p.c_type == REFT_F32) k_add_parts<float><<<blocks, 256, 0, s>>>(p);
+    else if (p.c_type == REFT_BF16) k_add_parts<bf16><<<blocks, 256, 0, s>>>(p);
+    else k_add_parts<f16><<<blocks, 256, 0, s>>>(p);
+    return hipGetLastError();
+}
+
 template <int FA, int FB, int MT, int NT> static hipError_t launch_tiles(const ProductArgs &p, hipStream_t s)
 {
     const dim3 grid((p.M + 64 * MT - 1) / (64 * MT) * ((p.N + 64 * NT - 1) / (64 * NT)), p.splits);
@@ -633,13 +649,8 @@ template <int FA, int FB, int MT, int NT> static hipError_t launch_tiles(const P
     } else {
         k_product<FA, FB, false, f16, MT, NT><<<grid, 256, 0, s>>>(p);
     }
-    if (p.splits > 1) {
-        const uint32_t blocks = (uint32_t)(((uint64_t)p.M * ((p.N + 3) / 4) + 255) / 256);
-        if (p.c_type == REFT_F32) k_add_parts<float><<<blocks, 256, 0, s>>>(p);
-        else if (p.c_type == REFT_BF16) k_add_parts<bf16><<<blocks, 256, 0, s>>>(p);
-        else k_add_parts<f16><<<blocks, 256, 0, s>>>(p);
-    }
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess && p.splits > 1 ? add_parts(p, s) : e;
 }
 
 template <int FA, int FB, bool WHOLE> static hipError_t launch_few(const ProductArgs &p, hipStream_t s)
@@ -653,21 +664,22 @@ template <int FA, int FB, bool WHOLE> static hipError_t launch_few(const Product
 template <int FA, int FB> static hipError_t launch_product(const ProductArgs &p, hipStream_t s)
 {
     if (p.M <= 16 && p.N < (1u << 26)) return p.K % 128 ? launch_few<FA, FB, false>(p, s) : launch_few<FA, FB, true>(p, s);
+    const Shape t = shape_of(p.M, p.N, p.K);
+    ProductArgs q = p;
+    q.splits = t.splits;
+    q.split_steps = t.split_steps;
     if (on_16_bytes(p)) {
-        const Shape t = shape_of(p.M, p.N, p.K);
-        ProductArgs q = p;
-        q.splits = t.splits;
-        q.split_steps = t.split_steps;
         switch (t.tile) {
         case 2: return launch_tiles<FA, FB, 4, 4>(q, s);
         case 1: return launch_tiles<FA, FB, 2, 2>(q, s);
         default: return launch_tiles<FA, FB, 1, 2>(q, s);
         }
     }
-    const dim3 grid((p.N + 127) / 128, (p.M + 127) / 128);
-    if (p.c_type == REFT_F32) k_product_any<FA, FB, true><<<grid, 256, 0, s>>>(p);
-    else k_product_any<FA, FB, false><<<grid, 256, 0, s>>>(p);
-    return hipGetLastError();
+    const dim3 grid((q.N + 127) / 128, (q.M + 127) / 128, q.splits);
+    if (q.c_type == REFT_F32) k_product_any<FA, FB, true><<<grid, 256, 0, s>>>(q);
+    else k_product_any<FA, FB, false><<<grid, 256, 0, s>>>(q);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess && q.splits > 1 ? add_parts(q, s) : e;
 }
 
 }  // namespace reft
