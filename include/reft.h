@@ -477,8 +477,8 @@ const char *reft_version(void);
  * matrix cores, the products of the forward pass and of both gradients.
  *
  * Matrices are device pointers with a row length in elements ("ld", at least the number of columns); rows may begin at
- * any element.  Sums, statistics and products are held in fp32; a result is rounded once, to nearest even, where it is
- * stored in fewer bits.  The calls enqueue kernels on `stream`, allocate nothing, wait for nothing, keep nothing from call to
+ * any element.  Sums and statistics are held in fp32 (what reft_product leaves out of an addend stands there); a result is rounded
+ * once, to nearest even, where it is stored in fewer bits.  The calls enqueue kernels on `stream`, allocate nothing, wait for nothing, keep nothing from call to
  * call and may be captured in a graph; operands must stay as they are until the stream has passed the call.  They run on the
  * current GPU.  Arguments are checked before anything is enqueued.  No outputs overlap an input or another output except as said.
  *
@@ -542,6 +542,10 @@ int reft_quantize(const void *x, uint64_t ld_x, uint64_t rows, uint64_t cols, in
  * per 128 x 128 values.  A layer's output is a product of its inputs and weights; the gradient of its inputs one of the output's
  * gradient and the transposed weights; that of its weights one of both transposes.  What lies between K and ld is not used, but
  * the last 16 bytes (on a multiple of 16) that hold a value of a row may be read as a whole.
+ * The sums are held in fp32, but of eight neighbouring k (8 i to 8 i + 7) the matrix cores cut each product towards zero at 2^-13 of
+ * the largest one's power of two where c is bf16, and at 2^-24 where it is f16 or fp32 (which halves the rate).  That is, a bf16 c errs,
+ * beside its rounding of 2^-8, by less than 7 2^-13 times the sum over the eights of their largest products: a c[m][n] that is small only
+ * because large products cancel wants f16 or fp32.
  * K == 0 gives zeros.  Fastest where both matrices begin at multiples of 16 bytes and their rows too.  workspace: on 16 bytes, of
  * at least reft_product_workspace(M, N, K) bytes (0 for most sizes); scratch, not shared with a call in flight.
  * M <= 128 * 65535; N, K < 2^31; M N < 2^37.

@@ -41,10 +41,15 @@ __device__ __forceinline__ i32x8 operand(const uint8_t *tile, int row, int s, in
 }
 
 // What the matrix cores multiply.  Their 8-bit products apply the scales for nothing and run at 4.5 PFLOP/s (a loop of
-// independent ones), but align what they add to its largest part in fewer bits than fp32: measured, the
-// root-mean-square error is 1.5e-5 of the result's at every K from 16 to 8192.  That is lost in the rounding of a 16-bit
-// result (1.7e-3 in bf16, 2e-4 in f16).  Where the result is fp32 (EXACT), the values are turned into bf16, which
-// holds 8 bits times a power of two without error, and multiplied at 2.2 PFLOP/s, with an error of 8e-8.
+// independent ones), but add in fewer bits than fp32: of eight products of neighbouring k, each is cut (towards zero) where it lies
+// 2^13 below the power of two of the largest one, and one further down is lost; the sums of eight are then added in fp32.  Measured, of
+// normal numbers the root-mean-square error is 1.5e-5 of the result's at every K from 16 to 8192; at worst it is 7 2^-13 times
+// the sum over the eights of their largest products.  Adding up outside of the matrix cores would not help, as the loss is within an
+// eight.  A bf16 result's own rounding, 2^-8 of it (1.7e-3 of the norm), covers that, and takes the fast ones.  That of an f16 result,
+// 2^-11, does not: where the result is f16 or fp32 (EXACT), the values are turned into bf16, which holds 8 bits times a power of
+// two exactly from 2^-133 (below that, what bf16's smallest numbers keep) up to 2^128, and are multiplied at 2.2 PFLOP/s: there the cut
+// lies 2^24 below the largest, with an error of 8e-8.  (us in bf16 and f16: 1 x 11008 x 4096 11.6 and 13.0, 1001 x 5120 x 1728 17.2 and
+// 25.1, 8192 x 28672 x 8192 1317 and 2546.)
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
@@ -627,6 +632,9 @@ static bool on_16_bytes(const ProductArgs &p)
     return p.K && ((uintptr_t)p.a | (uintptr_t)p.b | p.ld_a | p.ld_b) % 16 == 0 && p.ld_a < (1u << 23) && p.ld_b < (1u << 23);
 }
 
+// Which results the bits that the 8-bit matrix instructions leave out would show in (see Operand).
+static bool exact(const ProductArgs &p) { return p.c_type != REFT_BF16; }
+
 static hipError_t add_parts(const ProductArgs &p, hipStream_t s)
 {
     const uint32_t blocks = (uint32_t)(((uint64_t)p.M * ((p.N + 3) / 4) + 255) / 256);
@@ -639,15 +647,15 @@ static hipError_t add_parts(const ProductArgs &p, hipStream_t s)
 template <int FA, int FB, int MT, int NT> static hipError_t launch_tiles(const ProductArgs &p, hipStream_t s)
 {
     const dim3 grid((p.M + 64 * MT - 1) / (64 * MT) * ((p.N + 64 * NT - 1) / (64 * NT)), p.splits);
-    if (p.c_type == REFT_F32) {
+    if (exact(p) && (p.c_type == REFT_F32 || p.splits > 1)) {
         k_product<FA, FB, true, float, MT, NT><<<grid, 256, 0, s>>>(p);
+    } else if (exact(p)) {
+        k_product<FA, FB, true, f16, MT, NT><<<grid, 256, 0, s>>>(p);
     } else if (p.splits > 1) {
         if constexpr (MT * NT < 16) k_product<FA, FB, false, float, MT, NT><<<grid, 256, 0, s>>>(p);
         else return hipErrorInvalidValue;                    // shape_of cuts K for the smaller tiles only
-    } else if (p.c_type == REFT_BF16) {
-        k_product<FA, FB, false, bf16, MT, NT><<<grid, 256, 0, s>>>(p);
     } else {
-        k_product<FA, FB, false, f16, MT, NT><<<grid, 256, 0, s>>>(p);
+        k_product<FA, FB, false, bf16, MT, NT><<<grid, 256, 0, s>>>(p);
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess && p.splits > 1 ? add_parts(p, s) : e;
@@ -656,7 +664,7 @@ template <int FA, int FB, int MT, int NT> static hipError_t launch_tiles(const P
 template <int FA, int FB, bool WHOLE> static hipError_t launch_few(const ProductArgs &p, hipStream_t s)
 {
     const uint32_t grid = (p.N + 15) / 16;
-    if (p.c_type == REFT_F32) k_product_few<FA, FB, true, WHOLE, 16><<<grid, 1024, 0, s>>>(p);
+    if (exact(p)) k_product_few<FA, FB, true, WHOLE, 16><<<grid, 1024, 0, s>>>(p);
     else k_product_few<FA, FB, false, WHOLE, 16><<<grid, 1024, 0, s>>>(p);
     return hipGetLastError();
 }
@@ -676,7 +684,7 @@ template <int FA, int FB> static hipError_t launch_product(const ProductArgs &p,
         }
     }
     const dim3 grid((q.N + 127) / 128, (q.M + 127) / 128, q.splits);
-    if (q.c_type == REFT_F32) k_product_any<FA, FB, true><<<grid, 256, 0, s>>>(q);
+    if (exact(q)) k_product_any<FA, FB, true><<<grid, 256, 0, s>>>(q);
     else k_product_any<FA, FB, false><<<grid, 256, 0, s>>>(q);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess && q.splits > 1 ? add_parts(q, s) : e;
