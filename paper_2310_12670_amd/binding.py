@@ -462,7 +462,8 @@ def _type(t):
 
 
 # Each operator's call goes through _marshal first (reft_marshal.c), which makes it where every operand is as expected.  What
-# follows takes what is unusual but right (a type met for the first time, one row of any stride, no weight), and says what is wrong.
+# follows takes what is unusual but right (a type met for the first time, one row of any stride, no weight, pinned host memory), and
+# says what is wrong.
 def _matrix(who: str, name: str, t, shape, types):
     """(address, row length, type) of a 2-D tensor of that shape whose rows are contiguous."""
     if len(shape) != 2 or tuple(t.shape) != tuple(shape):
@@ -499,6 +500,27 @@ def _scratch(t):
     return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
 
 
+_CHECK_ONLY = 2 ** 64 - 1                 # in place of a stream: the library checks its arguments and enqueues nothing
+
+
+def _seen(t) -> bool:
+    """Whether kernels on the current GPU may read and write the tensor: its own memory, or pinned host memory."""
+    if t is None or t.numel() == 0:
+        return True
+    if t.get_device() < 0:
+        return t.is_pinned()
+    device = ctypes.c_int()
+    return _load().hipGetDevice(ctypes.byref(device)) == 0 and t.get_device() == device.value
+
+
+def _call(who: str, fn, operands: dict, stream, *args) -> None:
+    """A library call where every operand is seen; else what is wrong with it, beginning with what the library says."""
+    unseen = [name for name, t in operands.items() if not _seen(t)]
+    _check(fn(*args, _CHECK_ONLY if unseen else _stream(stream)))
+    if unseen:
+        _refuse(who, f"{unseen[0]} is on {operands[unseen[0]].device}, and not in memory that the current GPU sees")
+
+
 def reft_dropout(x, y, p: float, seed: int, offset: int = 0, stream=None) -> None:
     """``y`` (may be ``x``) gets ``x`` with elements dropped by the counter (seed, offset)."""
     rc = (_marshal or _load_marshal()).dropout(x, y, p, seed, offset, stream)
@@ -507,7 +529,7 @@ def reft_dropout(x, y, p: float, seed: int, offset: int = 0, stream=None) -> Non
     ax, ld_x, code = _matrix("reft_dropout", "x", x, x.shape, _FLOATS)
     rows, cols = shape = x.shape
     ay, ld_y, _ = _matrix("reft_dropout", "y", y, shape, _ONLY[code])
-    _check(_load().reft_dropout(ax, ld_x, ay, ld_y, rows, cols, code, p, seed, offset, _stream(stream)))
+    _call("reft_dropout", _load().reft_dropout, dict(x=x, y=y), stream, ax, ld_x, ay, ld_y, rows, cols, code, p, seed, offset)
 
 
 def reft_norm_forward(x, residual, weight, eps: float, p: float = 0.0, seed: int = 0, offset: int = 0, *, h=None,
@@ -526,9 +548,9 @@ def reft_norm_forward(x, residual, weight, eps: float, p: float = 0.0, seed: int
     ay, ld_y, _ = _NONE if y is None else _matrix(who, "y", y, shape, _ONLY[code])
     aq, ld_q, fmt = _NONE if q is None else _matrix(who, "q", q, shape, _EIGHTS)
     asc, ld_s = (None, 0) if scales is None else _scales(who, "scales", scales, rows, cols)
-    _check(_load().reft_norm_forward(
-        ax, ld_x, ar, ld_r, aw, rows, cols, code, h_code if r_code is None else r_code, w_code, eps, p,
-        seed, offset, ah, ld_h, arstd, ay, ld_y, aq, ld_q, fmt, asc, ld_s, _stream(stream)))
+    _call(who, _load().reft_norm_forward, dict(x=x, residual=residual, weight=weight, h=h, rstd=rstd, y=y, q=q, scales=scales), stream,
+          ax, ld_x, ar, ld_r, aw, rows, cols, code, h_code if r_code is None else r_code, w_code, eps, p,
+          seed, offset, ah, ld_h, arstd, ay, ld_y, aq, ld_q, fmt, asc, ld_s)
 
 
 def reft_norm_backward(dy, dh, h, rstd, weight, p: float = 0.0, seed: int = 0, offset: int = 0, *, dres=None, dx=None,
@@ -548,9 +570,10 @@ def reft_norm_backward(dy, dh, h, rstd, weight, p: float = 0.0, seed: int = 0, o
     adx, ld_dx, _ = _NONE if dx is None else _matrix(who, "dx", dx, shape, _ONLY[code])
     adw = None if dweight is None else _vector(who, "dweight", dweight, cols, _JUST_F32)[0]
     ws, ws_bytes = _scratch(workspace)
-    _check(_load().reft_norm_backward(
-        ady, ld_dy, adh, ld_dh, ah, ld_h, arstd, aw, rows, cols, code, r_code, w_code, p, seed, offset, adres, ld_dres, adx,
-        ld_dx, adw, ws, ws_bytes, _stream(stream)))
+    _call(who, _load().reft_norm_backward, dict(dy=dy, dh=dh, h=h, rstd=rstd, weight=weight, dres=dres, dx=dx, dweight=dweight,
+                                                workspace=workspace), stream,
+          ady, ld_dy, adh, ld_dh, ah, ld_h, arstd, aw, rows, cols, code, r_code, w_code, p, seed, offset, adres, ld_dres, adx,
+          ld_dx, adw, ws, ws_bytes)
 
 
 def reft_norm_backward_workspace(rows: int, cols: int) -> int:
@@ -570,8 +593,8 @@ def reft_quantize(x, q=None, scales=None, q_t=None, scales_t=None, *, blocks: bo
     tall, wide = ((rows + 127) >> 7, (cols + 127) >> 7) if blocks else (rows, cols)
     asc, ld_s = (None, 0) if scales is None else _scales(who, "scales", scales, tall, cols)
     ast, ld_st = (None, 0) if scales_t is None else _scales(who, "scales_t", scales_t, wide, rows)
-    _check(_load().reft_quantize(ax, ld_x, rows, cols, code, fmt_t if fmt is None else fmt, 1 if blocks else 0, aq, ld_q, asc,
-                                 ld_s, at, ld_t, ast, ld_st, _stream(stream)))
+    _call(who, _load().reft_quantize, dict(x=x, q=q, scales=scales, q_t=q_t, scales_t=scales_t), stream,
+          ax, ld_x, rows, cols, code, fmt_t if fmt is None else fmt, 1 if blocks else 0, aq, ld_q, asc, ld_s, at, ld_t, ast, ld_st)
 
 
 def reft_product(a, a_scales, b, b_scales, c, workspace=None, *, b_blocks: bool = False, stream=None) -> None:
@@ -590,8 +613,8 @@ def reft_product(a, a_scales, b, b_scales, c, workspace=None, *, b_blocks: bool 
     asb, ld_bs = (None, 0) if b_scales is None else _scales(who, "b_scales", b_scales, (N + 127) >> 7 if b_blocks else N, K)
     ac, ld_c, fc = _matrix(who, "c", c, (M, N), _FLOATS)
     ws, ws_bytes = _scratch(workspace)
-    _check(_load().reft_product(aa, ld_a, fa, asa, ld_as, ab, ld_b, fb, asb, ld_bs, 1 if b_blocks else 0, M, N, K, ac, ld_c,
-                                fc, ws, ws_bytes, _stream(stream)))
+    _call(who, _load().reft_product, dict(a=a, a_scales=a_scales, b=b, b_scales=b_scales, c=c, workspace=workspace), stream,
+          aa, ld_a, fa, asa, ld_as, ab, ld_b, fb, asb, ld_bs, 1 if b_blocks else 0, M, N, K, ac, ld_c, fc, ws, ws_bytes)
 
 
 def reft_product_workspace(M: int, N: int, K: int) -> int:

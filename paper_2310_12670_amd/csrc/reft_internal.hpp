@@ -9,6 +9,10 @@ namespace reft {
 // Sets the calling thread's message (see reft_last_error) and returns code.
 int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 
+// In place of a stream: an operator of a training step checks its arguments and enqueues nothing.  The binding asks so about a call with
+// operands that the GPU does not see, whose other mistakes are reported first.
+constexpr uintptr_t kCheckOnly = ~(uintptr_t)0;
+
 constexpr int kThreads = 256;      // 4 wavefronts of 64 lanes per workgroup
 constexpr int kMaxSrc = 8;         // sources XORed by one launch of the burst and contiguous kernels
 constexpr int kMaxStreamSrc = 16;  // ... and of the stream kernel

@@ -13,7 +13,10 @@
 
 enum { FLOATS = 1 << REFT_F32 | 1 << REFT_BF16 | 1 << REFT_F16, EIGHTS = 1 << REFT_E4M3 | 1 << REFT_E5M2 };
 
-static PyObject *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_stream, *s_size;
+static PyObject *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_stream, *s_size, *s_device;
+static int here;                               /* the current GPU in the call under way (all calls hold the interpreter's lock) */
+
+int hipGetDevice(int *device);                 /* of the HIP runtime that the library is linked with; 0: success */
 static PyObject *known[5];                     /* torch's dtypes by the library's numbers, as they have been met */
 
 typedef struct {
@@ -47,8 +50,26 @@ static int type_of(PyObject *t, int *type)
     return *type >= 0;
 }
 
+/* A call of `want` arguments begins. */
+static int begin(Py_ssize_t n, Py_ssize_t want)
+{
+    if (hipGetDevice(&here)) here = -2;
+    return n == want;
+}
+
+/* The tensor is memory of the current GPU (of none: -1). */
+static int seen(PyObject *t)
+{
+    PyObject *d = PyObject_CallMethodNoArgs(t, s_device);
+    const int ok = d && here >= 0 && PyLong_AsLong(d) == here;
+    Py_XDECREF(d);
+    PyErr_Clear();
+    return ok;
+}
+
 static int address_of(PyObject *t, void **p)
 {
+    if (!seen(t)) return 0;
     PyObject *a = PyObject_CallMethodNoArgs(t, s_data_ptr);
     *p = a ? PyLong_AsVoidPtr(a) : NULL;
     Py_XDECREF(a);
@@ -154,7 +175,7 @@ static PyObject *py_dropout(PyObject *self, PyObject *const *v, Py_ssize_t n)
     double p;
     uint64_t seed, offset;
     void *stream;
-    OTHERWISE(n == 6 && matrix(v[0], 0, NULL, FLOATS, &x) && matrix(v[1], 0, x.n, 1 << x.type, &y) && real(v[2], &p) && whole(v[3], &seed) &&
+    OTHERWISE(begin(n, 6) && matrix(v[0], 0, NULL, FLOATS, &x) && matrix(v[1], 0, x.n, 1 << x.type, &y) && real(v[2], &p) && whole(v[3], &seed) &&
               whole(v[4], &offset) && stream_of(v[5], &stream));
     CALL(reft_dropout(x.p, x.ld, y.p, y.ld, x.n[0], x.n[1], x.type, p, seed, offset, stream));
 }
@@ -165,7 +186,7 @@ static PyObject *py_norm_forward(PyObject *self, PyObject *const *v, Py_ssize_t 
     double eps, p;
     uint64_t seed, offset;
     void *stream;
-    OTHERWISE(n == 13 && matrix(v[0], 0, NULL, FLOATS, &x) && matrix(v[1], 1, x.n, or_f32(x.type), &r) &&
+    OTHERWISE(begin(n, 13) && matrix(v[0], 0, NULL, FLOATS, &x) && matrix(v[1], 1, x.n, or_f32(x.type), &r) &&
               vector(v[2], 0, x.n[1], or_f32(x.type), &w) && real(v[3], &eps) && real(v[4], &p) && whole(v[5], &seed) && whole(v[6], &offset) &&
               matrix(v[7], 1, x.n, r.type < 0 ? or_f32(x.type) : 1 << r.type, &h) && vector(v[8], 1, x.n[0], 1 << REFT_F32, &rstd) &&
               matrix(v[9], 1, x.n, 1 << x.type, &y) && matrix(v[10], 1, x.n, EIGHTS, &q) && scales(v[11], 1, x.n[0], x.n[1], &s) &&
@@ -180,7 +201,7 @@ static PyObject *py_norm_backward(PyObject *self, PyObject *const *v, Py_ssize_t
     double p;
     uint64_t seed, offset;
     void *stream;
-    OTHERWISE(n == 13 && matrix(v[0], 0, NULL, FLOATS, &dy) && matrix(v[2], 0, dy.n, or_f32(dy.type), &h) &&
+    OTHERWISE(begin(n, 13) && matrix(v[0], 0, NULL, FLOATS, &dy) && matrix(v[2], 0, dy.n, or_f32(dy.type), &h) &&
               matrix(v[1], 1, dy.n, 1 << h.type, &dh) && vector(v[3], 0, dy.n[0], 1 << REFT_F32, &rstd) &&
               vector(v[4], 0, dy.n[1], or_f32(dy.type), &w) && real(v[5], &p) && whole(v[6], &seed) && whole(v[7], &offset) &&
               matrix(v[8], 1, dy.n, 1 << h.type, &dres) && matrix(v[9], 1, dy.n, 1 << dy.type, &dx) &&
@@ -193,7 +214,7 @@ static PyObject *py_quantize(PyObject *self, PyObject *const *v, Py_ssize_t n)
 {
     operand x, q, s, qt, st;
     void *stream;
-    OTHERWISE(n == 7 && matrix(v[0], 0, NULL, FLOATS, &x));
+    OTHERWISE(begin(n, 7) && matrix(v[0], 0, NULL, FLOATS, &x));
     const int blocks = PyObject_IsTrue(v[5]);
     const uint64_t turned[2] = {x.n[1], x.n[0]};
     PyErr_Clear();
@@ -208,7 +229,7 @@ static PyObject *py_product(PyObject *self, PyObject *const *v, Py_ssize_t n)
 {
     operand a, sa, b, sb, c, room;
     void *stream;
-    OTHERWISE(n == 8 && matrix(v[0], 0, NULL, EIGHTS, &a) && matrix(v[2], 0, NULL, EIGHTS, &b) && a.n[1] == b.n[1]);
+    OTHERWISE(begin(n, 8) && matrix(v[0], 0, NULL, EIGHTS, &a) && matrix(v[2], 0, NULL, EIGHTS, &b) && a.n[1] == b.n[1]);
     const int blocks = PyObject_IsTrue(v[6]);
     const uint64_t shape[2] = {a.n[0], b.n[0]};
     PyErr_Clear();
@@ -245,6 +266,7 @@ PyMODINIT_FUNC PyInit__marshal(void)
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_stream = PyUnicode_InternFromString("cuda_stream");
     s_size = PyUnicode_InternFromString("itemsize");
-    if (!s_dtype || !s_shape || !s_stride || !s_data_ptr || !s_stream || !s_size) return NULL;
+    s_device = PyUnicode_InternFromString("get_device");
+    if (!s_dtype || !s_shape || !s_stride || !s_data_ptr || !s_stream || !s_size || !s_device) return NULL;
     return PyModule_Create(&module);
 }

@@ -1,0 +1,70 @@
+"""Operands that a kernel must not be given, through the binding and without a GPU: tensors in host memory or on another GPU."""
+import pytest
+import torch
+
+import paper_2310_12670_amd as reft
+
+E4 = torch.float8_e4m3fn
+
+
+def eight(rows, cols):
+    return torch.zeros(rows, cols, dtype=torch.uint8).view(E4)
+
+
+def words(rows, cols):
+    return torch.zeros(-(-cols // 512), rows, 4, dtype=torch.uint8)
+
+
+def calls():
+    x, w, r = torch.zeros(4, 32), torch.ones(32), torch.ones(4)
+    bytes_ = torch.zeros(1 << 16, dtype=torch.uint8)
+    return {
+        "dropout": lambda: reft.reft_dropout(x, x, 0.1, 1),
+        "norm_forward": lambda: reft.reft_norm_forward(x, None, w, 1e-5, y=x),
+        "norm_forward, 8 bits": lambda: reft.reft_norm_forward(x, x, w, 1e-5, h=x, rstd=r, q=eight(4, 32), scales=words(4, 32)),
+        "norm_backward": lambda: reft.reft_norm_backward(x, x, x, r, w, dres=x, dx=x, dweight=w, workspace=bytes_),
+        "quantize": lambda: reft.reft_quantize(x, eight(4, 32), words(4, 32), eight(32, 4), words(32, 4)),
+        "quantize, blocks": lambda: reft.reft_quantize(x, eight(4, 32), words(1, 32), blocks=True),
+        "product": lambda: reft.reft_product(eight(4, 32), words(4, 32), eight(6, 32), words(6, 32), torch.zeros(4, 6), bytes_),
+    }
+
+
+@pytest.mark.parametrize("name", list(calls()))
+def test_host_memory_is_refused(name):
+    """Right in everything else: the call must not come to a launch, which would read host addresses on the GPU."""
+    for _ in range(2):                                       # the second time the types are known to the binding's C part
+        with pytest.raises(reft.ReftError) as e:
+            calls()[name]()
+        assert e.value.code == reft.REFT_EINVAL and "cpu" in e.value.message
+
+
+class Elsewhere:
+    """A tensor's attributes with another GPU's memory behind them."""
+
+    device = "cuda:77"
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def get_device(self):
+        return 77
+
+
+def test_another_gpus_memory_is_refused():
+    x, q, s = Elsewhere(torch.zeros(4, 32)), Elsewhere(eight(4, 32)), Elsewhere(words(4, 32))
+    for call in (lambda: reft.reft_dropout(x, x, 0.1, 1), lambda: reft.reft_quantize(x, q, s)):
+        for _ in range(2):
+            with pytest.raises(reft.ReftError) as e:
+                call()
+            assert e.value.code == reft.REFT_EINVAL and "cuda:77" in e.value.message
+
+
+def test_what_else_is_wrong_is_said_first():
+    x, w = torch.zeros(4, 32), torch.ones(32)
+    with pytest.raises(reft.ReftError) as e:
+        reft.reft_norm_backward(x, None, x, torch.ones(4), w, dweight=w, workspace=torch.zeros(8, dtype=torch.uint8))
+    assert e.value.code == reft.REFT_ESIZE
+    reft.reft_dropout(torch.zeros(0, 32), torch.zeros(0, 32), 0.1, 1)          # nothing to read: nothing to refuse
