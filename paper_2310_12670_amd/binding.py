@@ -496,8 +496,13 @@ def _scales(who: str, name: str, t, rows: int, cols: int):
     return t.data_ptr(), wide // 4 if words > 1 else rows
 
 
-def _scratch(t):
-    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
+def _scratch(who: str, t):
+    """(address, bytes) of memory without gaps: what lies in them is not the call's to write."""
+    if t is None:
+        return None, 0
+    if not t.is_contiguous():
+        _refuse(who, "the workspace is not contiguous")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 _CHECK_ONLY = 2 ** 64 - 1                 # in place of a stream: the library checks its arguments and enqueues nothing
@@ -569,7 +574,7 @@ def reft_norm_backward(dy, dh, h, rstd, weight, p: float = 0.0, seed: int = 0, o
     adres, ld_dres, _ = _NONE if dres is None else _matrix(who, "dres", dres, shape, _ONLY[r_code])
     adx, ld_dx, _ = _NONE if dx is None else _matrix(who, "dx", dx, shape, _ONLY[code])
     adw = None if dweight is None else _vector(who, "dweight", dweight, cols, _JUST_F32)[0]
-    ws, ws_bytes = _scratch(workspace)
+    ws, ws_bytes = _scratch(who, workspace)
     _call(who, _load().reft_norm_backward, dict(dy=dy, dh=dh, h=h, rstd=rstd, weight=weight, dres=dres, dx=dx, dweight=dweight,
                                                 workspace=workspace), stream,
           ady, ld_dy, adh, ld_dh, ah, ld_h, arstd, aw, rows, cols, code, r_code, w_code, p, seed, offset, adres, ld_dres, adx,
@@ -612,7 +617,7 @@ def reft_product(a, a_scales, b, b_scales, c, workspace=None, *, b_blocks: bool 
     asa, ld_as = (None, 0) if a_scales is None else _scales(who, "a_scales", a_scales, M, K)
     asb, ld_bs = (None, 0) if b_scales is None else _scales(who, "b_scales", b_scales, (N + 127) >> 7 if b_blocks else N, K)
     ac, ld_c, fc = _matrix(who, "c", c, (M, N), _FLOATS)
-    ws, ws_bytes = _scratch(workspace)
+    ws, ws_bytes = _scratch(who, workspace)
     _call(who, _load().reft_product, dict(a=a, a_scales=a_scales, b=b, b_scales=b_scales, c=c, workspace=workspace), stream,
           aa, ld_a, fa, asa, ld_as, ab, ld_b, fb, asb, ld_bs, 1 if b_blocks else 0, M, N, K, ac, ld_c, fc, ws, ws_bytes)
 

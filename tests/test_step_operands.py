@@ -68,3 +68,15 @@ def test_what_else_is_wrong_is_said_first():
         reft.reft_norm_backward(x, None, x, torch.ones(4), w, dweight=w, workspace=torch.zeros(8, dtype=torch.uint8))
     assert e.value.code == reft.REFT_ESIZE
     reft.reft_dropout(torch.zeros(0, 32), torch.zeros(0, 32), 0.1, 1)          # nothing to read: nothing to refuse
+
+
+@pytest.mark.parametrize("workspace", [torch.zeros(1 << 16, dtype=torch.uint8)[::2], torch.zeros(256, 256, dtype=torch.uint8).t(),
+                                       torch.zeros(128, 256, dtype=torch.uint8)[:, :128], torch.zeros(1 << 14)[::3]])
+def test_a_workspace_with_gaps_is_refused(workspace):
+    """Its bytes are counted without the gaps, but would be written into them."""
+    x, w = torch.zeros(4, 32), torch.ones(32)
+    for call in (lambda: reft.reft_norm_backward(x, None, x, torch.ones(4), w, dweight=w, workspace=workspace),
+                 lambda: reft.reft_product(eight(60, 2000), words(60, 2000), eight(520, 2000), words(520, 2000), torch.zeros(60, 520), workspace)):
+        with pytest.raises(reft.ReftError) as e:
+            call()
+        assert e.value.code == reft.REFT_EINVAL and "contiguous" in e.value.message
