@@ -748,7 +748,7 @@ extern "C" int reft_norm_backward(const void *dy, uint64_t ld_dy, const void *dh
 
 template <typename T> static hipError_t launch_quantize(const QuantizeArgs &a, bool blocks, hipStream_t s)
 {
-    if (!blocks && !a.q_t) {
+    if (!blocks && !a.q_t && (a.rows + 3) / 4 <= kMaxBlocks256) {
         k_quantize_rows<T><<<dim3((uint32_t)((a.rows + 3) / 4), (uint32_t)((a.cols + 511) / 512)), 256, 0, s>>>(a);
     } else {
         // tile after tile of a row of tiles (down the columns first: 16384 x 8192 116 -> 150 us)

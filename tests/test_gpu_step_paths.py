@@ -53,3 +53,17 @@ def test_product_where_rows_lie_changes_no_bit(dev, M, N, K, out):
         assert torch.isfinite(c).all() and c.any()
         want = c if want is None else want
         assert torch.equal(c, want), (ld_a, lead_a, ld_b, lead_b)
+
+
+# ---- the largest sizes that the header allows ---------------------------------------------------------------------
+def test_quantize_of_the_most_rows(dev):
+    rows, half = (1 << 26) - 1, 1 << 25
+    x = normal(dev, 1, rows, 1)
+    q, s = torch.empty(rows, 1, dtype=torch.uint8, device=dev).view(E4), torch.empty(1, rows, 4, dtype=torch.uint8, device=dev)
+    reft.reft_quantize(x, q, s)
+    for at in (slice(0, half), slice(half, rows)):
+        n = at.stop - at.start
+        r, t = torch.empty(n, 1, dtype=torch.uint8, device=dev).view(E4), torch.empty(1, n, 4, dtype=torch.uint8, device=dev)
+        reft.reft_quantize(x[at], r, t)
+        assert torch.equal(q[at].view(torch.uint8), r.view(torch.uint8)) and torch.equal(s[:, at], t)
+    assert q.view(torch.uint8).any()

@@ -127,3 +127,19 @@ def test_parts_of_K_go_by_sizes_alone(step, M, N, K, out):
     assert len(cuts) == 1
     need = step.lib.reft_product_workspace(M, N, K)
     assert need == (M * N * 4 * cuts.pop() if need else 0)
+
+
+# ---- sizes that the header allows are launched ------------------------------------------------------------------------
+ONE_COLUMN = [(1 << 26) - n for n in (1, 2, 3, 4, 5)]
+
+
+@pytest.mark.parametrize("rows", [1, 5, 1 << 20] + ONE_COLUMN)
+@pytest.mark.parametrize("blocks", [0, 1])
+def test_quantize_takes_its_most_rows(step, rows, blocks):
+    """One row more a block than a grid has room for would make 2^32 threads, which HIP refuses."""
+    tall = -(-rows // 128) if blocks else rows
+    assert step.lib.reft_quantize(ADDRESS, 1, rows, 1, F32, E4M3, blocks, ADDRESS, 1, ADDRESS, tall, None, 0, None, 0, None) == reft.REFT_OK
+    ((name, grid, block),) = step.launches()
+    each = 4 if "k_quantize_rows" in name else 128
+    assert grid[0] == -(-rows // each)
+    assert ("k_quantize_rows" in name) == (not blocks and rows <= (1 << 26) - 4)
