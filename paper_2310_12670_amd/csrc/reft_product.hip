@@ -671,7 +671,8 @@ template <int FA, int FB, bool WHOLE> static hipError_t launch_few(const Product
 
 template <int FA, int FB> static hipError_t launch_product(const ProductArgs &p, hipStream_t s)
 {
-    if (p.M <= 16 && p.N < (1u << 26)) return p.K % 128 ? launch_few<FA, FB, false>(p, s) : launch_few<FA, FB, true>(p, s);
+    if (p.M <= 16 && (p.N + 15) / 16 < (1u << 22)) return      // a grid has less than 2^32 threads
+        p.K % 128 ? launch_few<FA, FB, false>(p, s) : launch_few<FA, FB, true>(p, s);
     const Shape t = shape_of(p.M, p.N, p.K);
     ProductArgs q = p;
     q.splits = t.splits;

@@ -67,3 +67,19 @@ def test_quantize_of_the_most_rows(dev):
         reft.reft_quantize(x[at], r, t)
         assert torch.equal(q[at].view(torch.uint8), r.view(torch.uint8)) and torch.equal(s[:, at], t)
     assert q.view(torch.uint8).any()
+
+
+def test_product_of_few_rows_and_the_most_columns(dev):
+    M, N, K, half = 3, (1 << 26) - 1, 16, 1 << 25
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(1)
+    few = torch.arange(-2, 3, device=dev).to(torch.float32).to(E4).view(torch.uint8)
+    a, b = (few[torch.randint(0, 5, (n, K), device=dev, generator=gen, dtype=torch.int32)].view(E4) for n in (M, N))
+    sa, sb = torch.full((1, M, 4), 127, dtype=torch.uint8, device=dev), torch.full((1, -(-N // 128), 4), 126, dtype=torch.uint8, device=dev)
+    c = torch.empty(M, N, dtype=torch.bfloat16, device=dev)
+    reft.reft_product(a, sa, b, sb, c, b_blocks=True)
+    for at in (slice(0, half), slice(half, N)):
+        n = at.stop - at.start
+        d, scales = torch.empty(M, n, dtype=torch.bfloat16, device=dev), sb[:, :-(-n // 128)]
+        reft.reft_product(a, sa, b[at], scales.contiguous(), d, b_blocks=True)
+        assert torch.equal(c[:, at], d) and d.any()

@@ -143,3 +143,14 @@ def test_quantize_takes_its_most_rows(step, rows, blocks):
     each = 4 if "k_quantize_rows" in name else 128
     assert grid[0] == -(-rows // each)
     assert ("k_quantize_rows" in name) == (not blocks and rows <= (1 << 26) - 4)
+
+
+@pytest.mark.parametrize("N", [1, 300, 1 << 20] + [(1 << 26) - n for n in (1, 15, 16, 17)] + [1 << 26, (1 << 26) + 1, 1 << 30])
+@pytest.mark.parametrize("M", [1, 16])
+@pytest.mark.parametrize("lead", [0, 1])
+def test_product_of_few_rows_takes_its_most_columns(step, M, N, lead):
+    rc, kernels = step.product(M, N, 16, lead=lead)
+    assert rc == reft.REFT_OK
+    ((name, grid, block),) = kernels
+    few = "k_product_few" in name
+    assert few == (N <= (1 << 26) - 16) and grid[0] == -(-N // (16 if few else 128))
