@@ -501,7 +501,7 @@ const char *reft_version(void);
  * 65536 / (65536 - t); else it is 0, whatever x holds there.  The bits are number c % 8 (the low half of a word before the
  * high one) of Philox4x32-10 with key seed and counter (c / 8, r, offset), low words first: they depend on
  * neither strides nor launch.  The gradient of x is the same call on the gradient of y.  With p == 0 x is copied.  y may be x
- * (with the same ld).  0 <= p <= 1; rows, cols < 2^31.
+ * (with the same ld).  0 <= p <= 1; rows, cols < 2^31, rows ceil(cols / 8) <= 2^34 - 1024.
  */
 int reft_dropout(const void *x, uint64_t ld_x, void *y, uint64_t ld_y, uint64_t rows, uint64_t cols, int dtype,
                  double p, uint64_t seed, uint64_t offset, reft_stream stream);
@@ -509,7 +509,7 @@ int reft_dropout(const void *x, uint64_t ld_x, void *y, uint64_t ld_y, uint64_t 
 /* h = residual + dropout(x) (residual == NULL: h = dropout(x)), rstd[r] = 1 / sqrt(mean(h[r]^2) + eps), and h rstd weight,
  * taken from h before it is rounded, as y in x's type and, or, as q in 8 bits with scales per 128 columns.  h, rstd, y and q
  * are each left out where NULL.  h and residual have residual_dtype (dtype or fp32), the weight has weight_dtype (dtype or
- * fp32).  h may be residual, or x where the types are the same, and y may be x (each with the same ld).  1 <= cols <= 65536.
+ * fp32).  h may be residual, or x where the types are the same, and y may be x (each with the same ld).  1 <= cols <= 65536; rows < 2^31.
  */
 int reft_norm_forward(const void *x, uint64_t ld_x, const void *residual, uint64_t ld_r, const void *weight,
                       uint64_t rows, uint64_t cols, int dtype, int residual_dtype, int weight_dtype, double eps,
@@ -520,7 +520,7 @@ int reft_norm_forward(const void *x, uint64_t ld_x, const void *residual, uint64
  * from elsewhere; NULL = 0), with its h and rstd and the same p, seed and offset:
  *   dres = rstd (dy weight - h rstd mean(dy weight h rstd)) + dh,  dx = dropout(dres),  dweight[c] = sum over r of dy h rstd.
  * dy and dx have dtype, dh, h and dres residual_dtype; dweight is fp32.  dres, dx and dweight are each left out where NULL.
- * dres may be dh and dx may be dy (with the same ld).  rows == 0 gives dweight = 0.  workspace: on 16 bytes, of at least
+ * dres may be dh and dx may be dy (with the same ld).  Sizes as above; rows == 0 gives dweight = 0.  workspace: on 16 bytes, of at least
  * reft_norm_backward_workspace(rows, cols) bytes (0 for one row) where dweight is wanted; scratch, not shared with a call in flight.
  */
 uint64_t reft_norm_backward_workspace(uint64_t rows, uint64_t cols);
@@ -532,7 +532,8 @@ int reft_norm_backward(const void *dy, uint64_t ld_dy, const void *dh, uint64_t 
 
 /* q = x in 8 bits, and q_t = the transpose of x in 8 bits ([cols][ld_qt]); either is left out where NULL.  blocks == 0:
  * scales per 128 columns of a row of q, and per 128 columns of a row of q_t (which are rows of x).  blocks != 0: one
- * per 128 x 128 values, the same ones for both, laid out for each with rows of blocks as rows.  rows < 2^26, cols <= 128 * 65535.
+ * per 128 x 128 values, the same ones for both, laid out for each with rows of blocks as rows.  rows < 2^26, cols <= 128 * 65535,
+ * ceil(rows / 128) ceil(cols / 128) < 2^24.
  */
 int reft_quantize(const void *x, uint64_t ld_x, uint64_t rows, uint64_t cols, int dtype, int format, int blocks,
                   void *q, uint64_t ld_q, void *scales, uint64_t ld_s, void *q_t, uint64_t ld_qt, void *scales_t,
@@ -548,7 +549,7 @@ int reft_quantize(const void *x, uint64_t ld_x, uint64_t rows, uint64_t cols, in
  * because large products cancel wants f16 or fp32.
  * K == 0 gives zeros.  Fastest where both matrices begin at multiples of 16 bytes and their rows too.  workspace: on 16 bytes, of
  * at least reft_product_workspace(M, N, K) bytes (0 for most sizes); scratch, not shared with a call in flight.
- * M <= 128 * 65535; N, K < 2^31; M N < 2^37.
+ * M <= 128 * 65535; N, K < 2^31; ceil(M / 64) ceil(N / 128) < 2^24.
  */
 uint64_t reft_product_workspace(uint64_t M, uint64_t N, uint64_t K);
 int reft_product(const void *a, uint64_t ld_a, int a_format, const void *a_scales, uint64_t ld_as, const void *b,

@@ -154,3 +154,42 @@ def test_product_of_few_rows_takes_its_most_columns(step, M, N, lead):
     ((name, grid, block),) = kernels
     few = "k_product_few" in name
     assert few == (N <= (1 << 26) - 16) and grid[0] == -(-N // (16 if few else 128))
+
+
+# ---- the limits that include/reft.h states: the last size on this side, the first on the other --------------------------------
+def test_limits_of_dropout(step):
+    def dropout(rows, cols):
+        f = step.lib.reft_dropout
+        u64 = ctypes.c_uint64
+        f.argtypes = [ctypes.c_void_p, u64, ctypes.c_void_p, u64, u64, u64, ctypes.c_int, ctypes.c_double, u64, u64, ctypes.c_void_p]
+        rc = f(ADDRESS, cols, ADDRESS, cols, rows, cols, F32, 0.1, 1, 1, None)
+        assert (rc == reft.REFT_OK) == (len(step.launches()) == 1)
+        return rc
+    assert dropout((1 << 31) - 1, 1) == reft.REFT_OK and dropout(1 << 31, 1) == reft.REFT_ESIZE
+    assert dropout(1, (1 << 31) - 1) == reft.REFT_OK and dropout(1, 1 << 31) == reft.REFT_ESIZE
+    # 2^34 - 1024 groups of eight columns: 0xffffff blocks of 1024
+    assert dropout(1024, 8 * 0xFFFFFF) == reft.REFT_OK and dropout(1025, 8 * 0xFFFFFF) == reft.REFT_ESIZE
+    assert dropout((1 << 30) - 64, 16 * 8) == reft.REFT_OK and dropout((1 << 30) - 63, 16 * 8) == reft.REFT_ESIZE
+
+
+@pytest.mark.parametrize("blocks", [0, 1])
+def test_limits_of_quantize(step, blocks):
+    def quantize(rows, cols):
+        tall = -(-rows // 128) if blocks else rows
+        rc = step.lib.reft_quantize(ADDRESS, cols, rows, cols, F32, E4M3, blocks, ADDRESS, cols, ADDRESS, tall, None, 0, None, 0, None)
+        assert (rc == reft.REFT_OK) == (len(step.launches()) == 1)
+        return rc
+    assert quantize((1 << 26) - 1, 31 * 128) == reft.REFT_OK and quantize((1 << 26) - 1, 32 * 128) == reft.REFT_ESIZE
+    assert quantize(1 << 26, 1) == reft.REFT_ESIZE
+    assert quantize(256 * 128, 128 * 65535) == reft.REFT_OK and quantize(256 * 128 + 1, 128 * 65535) == reft.REFT_ESIZE
+    assert quantize(1, 128 * 65535 + 1) == reft.REFT_ESIZE
+
+
+def test_limits_of_the_product(step):
+    last = 128 * 0xFFFFFF
+    assert step.product(64, last, 16)[0] == reft.REFT_OK and step.product(64, last + 1, 16)[0] == reft.REFT_ESIZE
+    assert step.product(1, last, 16, lead=1)[0] == reft.REFT_OK
+    assert step.product(65, 1 << 30, 16)[0] == reft.REFT_ESIZE and step.product(65, (1 << 30) - 128, 16)[0] == reft.REFT_OK
+    assert step.product(128 * 65535, 128 * 128, 16)[0] == reft.REFT_OK and step.product(128 * 65535, 128 * 129, 16)[0] == reft.REFT_ESIZE
+    assert step.product(128 * 65535 + 1, 1, 16)[0] == reft.REFT_ESIZE
+    assert step.product(1, 1, (1 << 31) - 1)[0] == reft.REFT_OK and step.product(1, 1, 1 << 31)[0] == reft.REFT_ESIZE
