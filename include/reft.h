@@ -547,6 +547,9 @@ int reft_quantize(const void *x, uint64_t ld_x, uint64_t rows, uint64_t cols, in
  * the largest one's power of two where c is bf16, and at 2^-24 where it is f16 or fp32 (which halves the rate).  That is, a bf16 c errs,
  * beside its rounding of 2^-8, by less than 7 2^-13 times the sum over the eights of their largest products: a c[m][n] that is small only
  * because large products cancel wants f16 or fp32.
+ * Where c is f16 or fp32, an operand's value times its scale is held in bf16 first, which is exact with scales from 2^-124 to 2^119 (e4m3)
+ * or from 2^-117 to 2^112 (e5m2): with smaller ones what lies below 2^-133 is lost, with larger ones values of 2^128 and more are infinite.
+ * Where c is bf16, the product has both scales applied at once, and any of them serve.
  * K == 0 gives zeros.  Fastest where both matrices begin at multiples of 16 bytes and their rows too.  workspace: on 16 bytes, of
  * at least reft_product_workspace(M, N, K) bytes (0 for most sizes); scratch, not shared with a call in flight.
  * M <= 128 * 65535; N, K < 2^31; ceil(M / 64) ceil(N / 128) < 2^24.

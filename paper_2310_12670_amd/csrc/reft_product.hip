@@ -47,7 +47,7 @@ __device__ __forceinline__ i32x8 operand(const uint8_t *tile, int row, int s, in
 // the sum over the eights of their largest products.  Adding up outside of the matrix cores would not help, as the loss is within an
 // eight.  A bf16 result's own rounding, 2^-8 of it (1.7e-3 of the norm), covers that, and takes the fast ones.  That of an f16 result,
 // 2^-11, does not: where the result is f16 or fp32 (EXACT), the values are turned into bf16, which holds 8 bits times a power of
-// two exactly from 2^-133 (below that, what bf16's smallest numbers keep) up to 2^128, and are multiplied at 2.2 PFLOP/s: there the cut
+// two exactly, as long as they lie between its smallest numbers, multiples of 2^-133, and 2^128, and are multiplied at 2.2 PFLOP/s: there the cut
 // lies 2^24 below the largest, with an error of 8e-8.  (us in bf16 and f16: 1 x 11008 x 4096 11.6 and 13.0, 1001 x 5120 x 1728 17.2 and
 // 25.1, 8192 x 28672 x 8192 1317 and 2546.)
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

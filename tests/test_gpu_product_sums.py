@@ -88,3 +88,31 @@ def test_small_products_beside_large_ones_that_cancel(dev, M, out):
     b[:, 0::8], b[:, 1::8] = 128, -128
     c, _, _ = multiply(dev, a, b, out)
     assert (c == 0.5 * 6 * K / 8).all()
+
+
+F8 = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+# scale bytes; f16 and fp32: the ends of the range that is exact
+ENDS = [("f32", "e4m3", "e4m3", 3, 246), ("f32", "e4m3", "e4m3", 246, 20), ("f32", "e5m2", "e4m3", 10, 246), ("f32", "e4m3", "e5m2", 3, 239),
+        ("f32", "e5m2", "e5m2", 239, 10), ("f16", "e4m3", "e4m3", 3, 246), ("f16", "e4m3", "e4m3", 246, 3), ("bf16", "e4m3", "e4m3", 0, 246),
+        ("bf16", "e4m3", "e4m3", 254, 20), ("bf16", "e4m3", "e4m3", 1, 230), ("bf16", "e4m3", "e5m2", 254, 1), ("bf16", "e5m2", "e5m2", 0, 230)]
+
+
+@pytest.mark.parametrize("out,fa,fb,ea,eb", ENDS)
+@pytest.mark.parametrize("M,ld", [(5, 16), (40, 16), (256, 16), (256, 17)])
+def test_scales_at_the_ends_of_the_range(dev, out, fa, fb, ea, eb, M, ld):
+    """K = 1: products of every value of a format with every one of the other's, 16 bits or less each and exact in fp32."""
+    every = torch.arange(256, dtype=torch.uint8, device=dev)
+
+    def operand(fmt, rows):
+        v = every.view(F8[fmt])
+        v = torch.where(torch.isfinite(v.float()), every, 0).repeat(2)[37:37 + rows]
+        q = torch.full((rows, ld), 0x7F, dtype=torch.uint8, device=dev)
+        q[:, 0] = v
+        return q.view(F8[fmt])[:, :1]
+
+    a, b = operand(fa, M), operand(fb, 256)
+    sa, sb = torch.full((1, M, 4), ea, dtype=torch.uint8, device=dev), torch.full((1, 256, 4), eb, dtype=torch.uint8, device=dev)
+    c = torch.empty(M, 256, dtype=DT[out], device=dev)
+    reft.reft_product(a, sa, b, sb, c, torch.empty(reft.reft_product_workspace(M, 256, 1), dtype=torch.uint8, device=dev))
+    want = (a.double() * b.double().t()) * 2.0 ** (ea + eb - 254)
+    assert torch.equal(want.float().double(), want) and torch.equal(c, want.float().to(DT[out]))
