@@ -80,3 +80,36 @@ def test_a_workspace_with_gaps_is_refused(workspace):
         with pytest.raises(reft.ReftError) as e:
             call()
         assert e.value.code == reft.REFT_EINVAL and "contiguous" in e.value.message
+
+
+def refused(code, fn, *args, **kw):
+    with pytest.raises(reft.ReftError) as e:
+        fn(*args, **kw)
+    assert e.value.code == code
+    return e.value.message
+
+
+def test_workspaces_that_do_not_hold_what_is_written():
+    """A product whose K is cut writes its parts there, the norm's gradient its blocks' sums: nothing else keeps them inside."""
+    M, N, K = 60, 520, 2000
+    need = reft.reft_product_workspace(M, N, K)
+    assert need == 2 * M * N * 4
+    a, sa, b, sb, c = eight(M, K), words(M, K), eight(N, K), words(N, K), torch.zeros(M, N)
+    room = torch.zeros(need + 16, dtype=torch.uint8)
+    assert room.data_ptr() % 16 == 0
+    product = (a, sa, b, sb, c)
+    assert "no workspace" in refused(reft.REFT_EINVAL, reft.reft_product, *product)
+    assert "16 bytes" in refused(reft.REFT_EINVAL, reft.reft_product, *product, room[8:])
+    assert "too small" in refused(reft.REFT_ESIZE, reft.reft_product, *product, room[:need - 1])
+    assert "cpu" in refused(reft.REFT_EINVAL, reft.reft_product, *product, room[:need])          # right but for the memory
+    assert "cpu" in refused(reft.REFT_EINVAL, reft.reft_product, eight(4, 32), words(4, 32), eight(6, 32), words(6, 32), torch.zeros(4, 6))
+    rows, cols = 700, 264
+    need = reft.reft_norm_backward_workspace(rows, cols)
+    assert need > cols * 4 and need % (cols * 4) == 0
+    x, r, w = torch.zeros(rows, cols), torch.ones(rows), torch.ones(cols)
+    room = torch.zeros(need + 16, dtype=torch.uint8)
+    norm = lambda room: reft.reft_norm_backward(x, None, x, r, w, dweight=w, workspace=room)      # noqa: E731
+    assert "no workspace" in refused(reft.REFT_EINVAL, norm, None)
+    assert "16 bytes" in refused(reft.REFT_EINVAL, norm, room[4:])
+    assert "too small" in refused(reft.REFT_ESIZE, norm, room[:need - 1])
+    assert "cpu" in refused(reft.REFT_EINVAL, norm, room[:need])
