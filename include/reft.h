@@ -497,7 +497,7 @@ const char *reft_version(void);
 #define REFT_E4M3 3
 #define REFT_E5M2 4
 
-/* y = dropout(x): element (r, c) is kept where its 16 random bits are at least t = round(65536 p), and multiplied by
+/* y = dropout(x): element (r, c) is kept where its 16 random bits are at least t = round(65536 p) (ties to even), and multiplied by
  * 65536 / (65536 - t); else it is 0, whatever x holds there.  The bits are number c % 8 (the low half of a word before the
  * high one) of Philox4x32-10 with key seed and counter (c / 8, r, offset), low words first: they depend on
  * neither strides nor launch.  The gradient of x is the same call on the gradient of y.  With p == 0 x is copied.  y may be x

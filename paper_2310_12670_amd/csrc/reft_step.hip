@@ -567,7 +567,7 @@ static bool lies(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
 static bool make_dropout(double p, uint64_t seed, uint64_t offset, Dropout *d)
 {
     if (!(p >= 0 && p <= 1)) return false;
-    const long t = std::lround(p * 65536);
+    const long t = (long)std::nearbyint(p * 65536);         // ties to even
     d->key0 = (uint32_t)seed;
     d->key1 = (uint32_t)(seed >> 32);
     d->off0 = (uint32_t)offset;

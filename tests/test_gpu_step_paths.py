@@ -119,6 +119,18 @@ def test_dropout_of_rows_on_lines(dev, rows, cols, dtype):
     assert torch.equal(x, want)
 
 
+@pytest.mark.parametrize("half_steps", [1, 3, 5, 65535, 65537, 131069, 131071])
+def test_dropout_of_shares_between_two_thresholds(dev, half_steps):
+    """p = half_steps / 131072 lies in the middle of two thresholds: the even one is taken, forward, backward and in the norm."""
+    p, rows, cols = half_steps / 131072, 1000, 1200
+    x = 1 + normal(dev, 1, rows, cols).abs()
+    y, h = torch.empty_like(x), torch.empty_like(x)
+    reft.reft_dropout(x, y, p, 11, 12)
+    reft.reft_norm_forward(x, None, None, 1e-5, p, 11, 12, h=h)
+    keep, _ = step.keep_mask(rows, cols, p, 11, 12)
+    assert torch.equal(y != 0, torch.from_numpy(keep).to(dev)) and torch.equal(h, y)
+
+
 def norm_back(dev, rows, cols, dtype, residual, place, p):
     """The gradients against the definition; err as in test_gpu_step.py: a sum of n terms errs by n U of their magnitudes."""
     dy, dh = place(dev, rows, cols, dtype, normal(dev, 1, rows, cols)), place(dev, rows, cols, residual, normal(dev, 2, rows, cols))
