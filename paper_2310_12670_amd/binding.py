@@ -2,7 +2,8 @@
 
 Pointers may be given as ``torch.Tensor`` (its ``data_ptr()`` is used), as ``int`` addresses or as
 ``None``; pointer arrays as sequences of those or as a ctypes array made with :func:`ptr_array`
-(worth it when the same list is passed many times).  Streams may be ``torch.cuda.Stream``,
+(worth it when the same list is passed many times).  The operators of a training step take tensors
+only, as they read sizes, row lengths and types off them.  Streams may be ``torch.cuda.Stream``,
 ``int`` (a ``hipStream_t``) or ``None`` (the default stream).  Every failing call raises
 :class:`ReftError` carrying the library's code and message.
 """
@@ -464,6 +465,16 @@ def _type(t):
 # Each operator's call goes through _marshal first (reft_marshal.c), which makes it where every operand is as expected.  What
 # follows takes what is unusual but right (a type met for the first time, one row of any stride, no weight, pinned host memory), and
 # says what is wrong.
+def _tensors(who: str, operands: dict, needed: str) -> None:
+    """Sizes, row lengths and types are read off the operands: an address alone will not do."""
+    for name, t in operands.items():
+        if t is None:
+            if name in needed.split():
+                _refuse(who, f"{name} is left out")
+        elif not (hasattr(t, "data_ptr") and hasattr(t, "stride")):
+            _refuse(who, f"{name} is no tensor but {type(t).__name__}")
+
+
 def _matrix(who: str, name: str, t, shape, types):
     """(address, row length, type) of a 2-D tensor of that shape whose rows are contiguous."""
     if len(shape) != 2 or tuple(t.shape) != tuple(shape):
@@ -531,10 +542,13 @@ def reft_dropout(x, y, p: float, seed: int, offset: int = 0, stream=None) -> Non
     rc = (_marshal or _load_marshal()).dropout(x, y, p, seed, offset, stream)
     if rc is not None:
         return _done(rc)
-    ax, ld_x, code = _matrix("reft_dropout", "x", x, x.shape, _FLOATS)
+    who, operands = "reft_dropout", dict(x=x, y=y)
+    _tensors(who, operands, "x y")
+    ax, ld_x, code = _matrix(who, "x", x, x.shape, _FLOATS)
     rows, cols = shape = x.shape
-    ay, ld_y, _ = _matrix("reft_dropout", "y", y, shape, _ONLY[code])
-    _call("reft_dropout", _load().reft_dropout, dict(x=x, y=y), stream, ax, ld_x, ay, ld_y, rows, cols, code, p, seed, offset)
+    ay, ld_y, _ = _matrix(who, "y", y, shape, _ONLY[code])
+    _call(who, _load().reft_dropout, operands, stream, ax, ld_x, ay, ld_y, rows, cols, code, p, seed,
+          offset)
 
 
 def reft_norm_forward(x, residual, weight, eps: float, p: float = 0.0, seed: int = 0, offset: int = 0, *, h=None,
@@ -542,7 +556,8 @@ def reft_norm_forward(x, residual, weight, eps: float, p: float = 0.0, seed: int
     rc = (_marshal or _load_marshal()).norm_forward(x, residual, weight, eps, p, seed, offset, h, rstd, y, q, scales, stream)
     if rc is not None:
         return _done(rc)
-    who = "reft_norm_forward"
+    who, operands = "reft_norm_forward", dict(x=x, residual=residual, weight=weight, h=h, rstd=rstd, y=y, q=q, scales=scales)
+    _tensors(who, operands, "x")
     ax, ld_x, code = _matrix(who, "x", x, x.shape, _FLOATS)
     rows, cols = shape = x.shape
     wide = _OR_F32[code]
@@ -553,9 +568,9 @@ def reft_norm_forward(x, residual, weight, eps: float, p: float = 0.0, seed: int
     ay, ld_y, _ = _NONE if y is None else _matrix(who, "y", y, shape, _ONLY[code])
     aq, ld_q, fmt = _NONE if q is None else _matrix(who, "q", q, shape, _EIGHTS)
     asc, ld_s = (None, 0) if scales is None else _scales(who, "scales", scales, rows, cols)
-    _call(who, _load().reft_norm_forward, dict(x=x, residual=residual, weight=weight, h=h, rstd=rstd, y=y, q=q, scales=scales), stream,
-          ax, ld_x, ar, ld_r, aw, rows, cols, code, h_code if r_code is None else r_code, w_code, eps, p,
-          seed, offset, ah, ld_h, arstd, ay, ld_y, aq, ld_q, fmt, asc, ld_s)
+    _call(who, _load().reft_norm_forward, operands, stream, ax, ld_x, ar, ld_r, aw, rows, cols, code,
+          h_code if r_code is None else r_code, w_code, eps, p, seed, offset, ah, ld_h,
+          arstd, ay, ld_y, aq, ld_q, fmt, asc, ld_s)
 
 
 def reft_norm_backward(dy, dh, h, rstd, weight, p: float = 0.0, seed: int = 0, offset: int = 0, *, dres=None, dx=None,
@@ -564,6 +579,8 @@ def reft_norm_backward(dy, dh, h, rstd, weight, p: float = 0.0, seed: int = 0, o
     if rc is not None:
         return _done(rc)
     who = "reft_norm_backward"
+    operands = dict(dy=dy, dh=dh, h=h, rstd=rstd, weight=weight, dres=dres, dx=dx, dweight=dweight, workspace=workspace)
+    _tensors(who, operands, "dy h")
     ady, ld_dy, code = _matrix(who, "dy", dy, dy.shape, _FLOATS)
     rows, cols = shape = dy.shape
     wide = _OR_F32[code]
@@ -575,10 +592,8 @@ def reft_norm_backward(dy, dh, h, rstd, weight, p: float = 0.0, seed: int = 0, o
     adx, ld_dx, _ = _NONE if dx is None else _matrix(who, "dx", dx, shape, _ONLY[code])
     adw = None if dweight is None else _vector(who, "dweight", dweight, cols, _JUST_F32)[0]
     ws, ws_bytes = _scratch(who, workspace)
-    _call(who, _load().reft_norm_backward, dict(dy=dy, dh=dh, h=h, rstd=rstd, weight=weight, dres=dres, dx=dx, dweight=dweight,
-                                                workspace=workspace), stream,
-          ady, ld_dy, adh, ld_dh, ah, ld_h, arstd, aw, rows, cols, code, r_code, w_code, p, seed, offset, adres, ld_dres, adx,
-          ld_dx, adw, ws, ws_bytes)
+    _call(who, _load().reft_norm_backward, operands, stream, ady, ld_dy, adh, ld_dh, ah, ld_h, arstd, aw, rows, cols, code, r_code,
+          w_code, p, seed, offset, adres, ld_dres, adx, ld_dx, adw, ws, ws_bytes)
 
 
 def reft_norm_backward_workspace(rows: int, cols: int) -> int:
@@ -590,7 +605,8 @@ def reft_quantize(x, q=None, scales=None, q_t=None, scales_t=None, *, blocks: bo
     rc = (_marshal or _load_marshal()).quantize(x, q, scales, q_t, scales_t, blocks, stream)
     if rc is not None:
         return _done(rc)
-    who = "reft_quantize"
+    who, operands = "reft_quantize", dict(x=x, q=q, scales=scales, q_t=q_t, scales_t=scales_t)
+    _tensors(who, operands, "x")
     ax, ld_x, code = _matrix(who, "x", x, x.shape, _FLOATS)
     rows, cols = shape = x.shape
     aq, ld_q, fmt = (None, 0, None) if q is None else _matrix(who, "q", q, shape, _EIGHTS)
@@ -598,8 +614,8 @@ def reft_quantize(x, q=None, scales=None, q_t=None, scales_t=None, *, blocks: bo
     tall, wide = ((rows + 127) >> 7, (cols + 127) >> 7) if blocks else (rows, cols)
     asc, ld_s = (None, 0) if scales is None else _scales(who, "scales", scales, tall, cols)
     ast, ld_st = (None, 0) if scales_t is None else _scales(who, "scales_t", scales_t, wide, rows)
-    _call(who, _load().reft_quantize, dict(x=x, q=q, scales=scales, q_t=q_t, scales_t=scales_t), stream,
-          ax, ld_x, rows, cols, code, fmt_t if fmt is None else fmt, 1 if blocks else 0, aq, ld_q, asc, ld_s, at, ld_t, ast, ld_st)
+    _call(who, _load().reft_quantize, operands, stream, ax, ld_x, rows, cols, code, fmt_t if fmt is None else fmt, 1 if blocks else 0,
+          aq, ld_q, asc, ld_s, at, ld_t, ast, ld_st)
 
 
 def reft_product(a, a_scales, b, b_scales, c, workspace=None, *, b_blocks: bool = False, stream=None) -> None:
@@ -607,7 +623,8 @@ def reft_product(a, a_scales, b, b_scales, c, workspace=None, *, b_blocks: bool 
     rc = (_marshal or _load_marshal()).product(a, a_scales, b, b_scales, c, workspace, b_blocks, stream)
     if rc is not None:
         return _done(rc)
-    who = "reft_product"
+    who, operands = "reft_product", dict(a=a, a_scales=a_scales, b=b, b_scales=b_scales, c=c, workspace=workspace)
+    _tensors(who, operands, "a b c")
     aa, ld_a, fa = _matrix(who, "a", a, a.shape, _EIGHTS)
     ab, ld_b, fb = _matrix(who, "b", b, b.shape, _EIGHTS)
     M, K = a.shape
@@ -618,8 +635,8 @@ def reft_product(a, a_scales, b, b_scales, c, workspace=None, *, b_blocks: bool 
     asb, ld_bs = (None, 0) if b_scales is None else _scales(who, "b_scales", b_scales, (N + 127) >> 7 if b_blocks else N, K)
     ac, ld_c, fc = _matrix(who, "c", c, (M, N), _FLOATS)
     ws, ws_bytes = _scratch(who, workspace)
-    _call(who, _load().reft_product, dict(a=a, a_scales=a_scales, b=b, b_scales=b_scales, c=c, workspace=workspace), stream,
-          aa, ld_a, fa, asa, ld_as, ab, ld_b, fb, asb, ld_bs, 1 if b_blocks else 0, M, N, K, ac, ld_c, fc, ws, ws_bytes)
+    _call(who, _load().reft_product, operands, stream, aa, ld_a, fa, asa, ld_as, ab, ld_b, fb, asb, ld_bs, 1 if b_blocks else 0, M, N, K,
+          ac, ld_c, fc, ws, ws_bytes)
 
 
 def reft_product_workspace(M: int, N: int, K: int) -> int:

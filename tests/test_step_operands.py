@@ -113,3 +113,19 @@ def test_workspaces_that_do_not_hold_what_is_written():
     assert "16 bytes" in refused(reft.REFT_EINVAL, norm, room[4:])
     assert "too small" in refused(reft.REFT_ESIZE, norm, room[:need - 1])
     assert "cpu" in refused(reft.REFT_EINVAL, norm, room[:need])
+
+
+@pytest.mark.parametrize("wrong", [1 << 40, 3.5, "x", [1.0], None])
+def test_operands_that_are_no_tensors(wrong):
+    x, w, r, q, s = torch.zeros(4, 32), torch.ones(32), torch.ones(4), eight(4, 32), words(4, 32)
+    refused(reft.REFT_EINVAL, reft.reft_dropout, wrong, x, 0.1, 1)
+    refused(reft.REFT_EINVAL, reft.reft_dropout, x, wrong, 0.1, 1)
+    refused(reft.REFT_EINVAL, reft.reft_norm_forward, wrong, None, w, 1e-5, y=x)
+    refused(reft.REFT_EINVAL, reft.reft_norm_forward, x, None, wrong, 1e-5, y=x)
+    refused(reft.REFT_EINVAL, reft.reft_norm_backward, x, None, wrong, r, w, dres=x)
+    refused(reft.REFT_EINVAL, reft.reft_norm_backward, x, None, x, wrong, w, dres=x)
+    refused(reft.REFT_EINVAL, reft.reft_quantize, wrong, q, s)
+    refused(reft.REFT_EINVAL, reft.reft_quantize, x, q, wrong)
+    refused(reft.REFT_EINVAL, reft.reft_product, q, s, q, s, wrong)
+    refused(reft.REFT_EINVAL, reft.reft_product, q, wrong, q, s, torch.zeros(4, 4))
+    refused(reft.REFT_EINVAL, reft.reft_product, eight(60, 2000), words(60, 2000), eight(520, 2000), words(520, 2000), torch.zeros(60, 520), wrong)
