@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import importlib
+import operator
 import os
 from typing import Optional, Sequence
 
@@ -475,6 +476,14 @@ def _tensors(who: str, operands: dict, needed: str) -> None:
             _refuse(who, f"{name} is no tensor but {type(t).__name__}")
 
 
+def _counter(who: str, name: str, v) -> int:
+    """A seed or an offset: 64 bits, where -1 stands for 2^64 - 1 and so on."""
+    v = operator.index(v)
+    if not -2 ** 63 <= v < 2 ** 64:
+        _refuse(who, f"{name} has more than 64 bits")
+    return v
+
+
 def _matrix(who: str, name: str, t, shape, types):
     """(address, row length, type) of a 2-D tensor of that shape whose rows are contiguous."""
     if len(shape) != 2 or tuple(t.shape) != tuple(shape):
@@ -547,8 +556,8 @@ def reft_dropout(x, y, p: float, seed: int, offset: int = 0, stream=None) -> Non
     ax, ld_x, code = _matrix(who, "x", x, x.shape, _FLOATS)
     rows, cols = shape = x.shape
     ay, ld_y, _ = _matrix(who, "y", y, shape, _ONLY[code])
-    _call(who, _load().reft_dropout, operands, stream, ax, ld_x, ay, ld_y, rows, cols, code, p, seed,
-          offset)
+    _call(who, _load().reft_dropout, operands, stream, ax, ld_x, ay, ld_y, rows, cols, code, p, _counter(who, "seed", seed),
+          _counter(who, "offset", offset))
 
 
 def reft_norm_forward(x, residual, weight, eps: float, p: float = 0.0, seed: int = 0, offset: int = 0, *, h=None,
@@ -569,7 +578,7 @@ def reft_norm_forward(x, residual, weight, eps: float, p: float = 0.0, seed: int
     aq, ld_q, fmt = _NONE if q is None else _matrix(who, "q", q, shape, _EIGHTS)
     asc, ld_s = (None, 0) if scales is None else _scales(who, "scales", scales, rows, cols)
     _call(who, _load().reft_norm_forward, operands, stream, ax, ld_x, ar, ld_r, aw, rows, cols, code,
-          h_code if r_code is None else r_code, w_code, eps, p, seed, offset, ah, ld_h,
+          h_code if r_code is None else r_code, w_code, eps, p, _counter(who, "seed", seed), _counter(who, "offset", offset), ah, ld_h,
           arstd, ay, ld_y, aq, ld_q, fmt, asc, ld_s)
 
 
@@ -593,7 +602,7 @@ def reft_norm_backward(dy, dh, h, rstd, weight, p: float = 0.0, seed: int = 0, o
     adw = None if dweight is None else _vector(who, "dweight", dweight, cols, _JUST_F32)[0]
     ws, ws_bytes = _scratch(who, workspace)
     _call(who, _load().reft_norm_backward, operands, stream, ady, ld_dy, adh, ld_dh, ah, ld_h, arstd, aw, rows, cols, code, r_code,
-          w_code, p, seed, offset, adres, ld_dres, adx, ld_dx, adw, ws, ws_bytes)
+          w_code, p, _counter(who, "seed", seed), _counter(who, "offset", offset), adres, ld_dres, adx, ld_dx, adw, ws, ws_bytes)
 
 
 def reft_norm_backward_workspace(rows: int, cols: int) -> int:

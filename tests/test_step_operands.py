@@ -129,3 +129,15 @@ def test_operands_that_are_no_tensors(wrong):
     refused(reft.REFT_EINVAL, reft.reft_product, q, s, q, s, wrong)
     refused(reft.REFT_EINVAL, reft.reft_product, q, wrong, q, s, torch.zeros(4, 4))
     refused(reft.REFT_EINVAL, reft.reft_product, eight(60, 2000), words(60, 2000), eight(520, 2000), words(520, 2000), torch.zeros(60, 520), wrong)
+
+
+@pytest.mark.parametrize("wrong", [1 << 64, -(1 << 63) - 1, 1 << 80])
+def test_seeds_and_offsets_have_64_bits(wrong):
+    """More would be cut off without a word: two counters that differ would give one mask."""
+    x, r, w = torch.zeros(4, 32), torch.ones(4), torch.ones(32)
+    for seed, offset in ((wrong, 0), (0, wrong)):
+        assert "64 bits" in refused(reft.REFT_EINVAL, reft.reft_dropout, x, x, 0.1, seed, offset)
+        assert "64 bits" in refused(reft.REFT_EINVAL, reft.reft_norm_forward, x, None, w, 1e-5, 0.1, seed, offset, y=x)
+        assert "64 bits" in refused(reft.REFT_EINVAL, reft.reft_norm_backward, x, None, x, r, w, 0.1, seed, offset, dres=x)
+    for seed in ((1 << 64) - 1, -1, -(1 << 63)):
+        assert "cpu" in refused(reft.REFT_EINVAL, reft.reft_dropout, x, x, 0.1, seed, seed)          # right but for the memory
