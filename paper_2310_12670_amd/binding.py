@@ -131,11 +131,21 @@ def _load():
     return lib
 
 
+class _NoMarshal:
+    """In place of the binding's C part where it could not be built: no call is the usual case."""
+
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
 def _load_marshal():
     global _marshal
     if _marshal is None:
         _load()
-        _marshal = importlib.import_module("._marshal", __package__)
+        try:
+            _marshal = importlib.import_module("._marshal", __package__)
+        except ModuleNotFoundError:
+            _marshal = _NoMarshal()
     return _marshal
 
 

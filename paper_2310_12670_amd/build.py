@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import os
 import re
+import shutil
 import subprocess
 import sysconfig
 import tempfile
@@ -10,7 +11,8 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libreft.so")
-MARSHAL = os.path.join(HERE, "_marshal.so")      # the operators' arguments from Python, in C (reft_marshal.c)
+# the operators' arguments from Python, in C (reft_marshal.c), for the interpreter that builds
+MARSHAL = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["reft_api.hip", "reft_kernels.hip", "reft_stream.hip", "reft_step.hip",
            "reft_product.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
@@ -56,6 +58,20 @@ def check_burst_registers(compiler_output: str) -> dict:
     return counts
 
 
+def build_marshal(out: str = MARSHAL, include: str = sysconfig.get_paths()["include"]) -> bool:
+    """The binding's C part.  It saves a few microseconds a call and nothing depends on it: without a C compiler or Python's headers it is
+    left out (False), and what an earlier build left goes too."""
+    if not (shutil.which("gcc") and os.path.exists(os.path.join(include, "Python.h"))):
+        if os.path.exists(out):
+            os.remove(out)
+        return False
+    cc = subprocess.run(["gcc", "-O2", "-std=c11", "-Wall", "-fPIC", "-shared", "-I", include, "-o", out, os.path.join(CSRC, "reft_marshal.c"),
+                         "-L", HERE, "-l:libreft.so", "-Wl,-rpath,$ORIGIN"], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if cc.returncode != 0:
+        raise RuntimeError("gcc failed:\n" + cc.stdout)
+    return True
+
+
 def build(verbose: bool = False) -> str:
     """Compile the sources side by side, then link."""
     with tempfile.TemporaryDirectory() as tmp:
@@ -74,11 +90,7 @@ def build(verbose: bool = False) -> str:
                               stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
         if link.returncode != 0:
             raise RuntimeError("hipcc failed:\n" + link.stdout)
-    marshal = subprocess.run(["gcc", "-O2", "-std=c11", "-Wall", "-fPIC", "-shared", "-I", sysconfig.get_paths()["include"], "-o", MARSHAL,
-                              os.path.join(CSRC, "reft_marshal.c"), "-L", HERE, "-l:libreft.so", "-Wl,-rpath,$ORIGIN"],
-                             stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    if marshal.returncode != 0:
-        raise RuntimeError("gcc failed:\n" + marshal.stdout)
+    marshal = build_marshal()
     output = "\n".join(outs)
     counts = check_burst_registers(output)
     if verbose:
@@ -86,6 +98,8 @@ def build(verbose: bool = False) -> str:
         print("\n".join(l for l in output.splitlines()
                         if "remark:" not in l and not re.match(r"\s*\d*\s*\|", l)
                         and HOST_PASS_NOTE not in l))
+        if not marshal:
+            print("no C compiler or no Python headers: the operators' arguments are taken in Python alone")
         print("burst kernels: %d instantiations, at most %d VGPRs" % (len(counts), max(counts.values())))
     return LIB
 
