@@ -448,7 +448,8 @@ def reft_restore_wait(plan) -> None:
 
 
 # ------------------------------------------------------------------------------------------------
-# operators of a training step: sizes, row lengths and types are those of the tensors given
+# operators of a training step: sizes, row lengths and types are those of the tensors given, which are written without a word to
+# autograd; kernels run on `stream`, or the default stream (not torch's current one) where it is None
 # ------------------------------------------------------------------------------------------------
 _TYPES = {"torch.float32": REFT_F32, "torch.bfloat16": REFT_BF16, "torch.float16": REFT_F16,
           "torch.float8_e4m3fn": REFT_E4M3, "torch.float8_e5m2": REFT_E5M2}

@@ -142,7 +142,7 @@ __device__ __forceinline__ void store_tile(const ProductArgs &p, uint32_t m, uin
 
 // ---- any sizes, any alignment: tiles of 128 x 128, four waves of 64 x 64 -----------------------------------------
 // The next tile is loaded to registers while one is multiplied, and then written to LDS: what 16-byte copies to LDS need of alignment,
-// this does not.  8192 x 4096 x 4096 to bf16: 276 us, where rows on 16 bytes take 111.  K is multiplied in the order of k_product and cut
+// this does not.  8192 x 4096 x 4096 to bf16: 277 us, where rows on 16 bytes take 111; 128 x 4096 x 11008, cut into 8 parts, 29 and 20.  K is multiplied in the order of k_product and cut
 // into the same parts, so that where and how far apart the rows lie does not change a bit of the result.
 template <int FA, int FB, bool EXACT> __global__ __launch_bounds__(256) void k_product_any(ProductArgs p)
 {

@@ -386,7 +386,9 @@ __device__ __forceinline__ void store_scale(uint8_t *scales, uint64_t ld, uint64
 // 3584 x 8192 in bf16, blocks and both orders, 19.4 us, 6.0 TB/s (31 with values widened once and held in fp32).
 template <typename T, bool BLOCKS, bool LINES> __global__ __launch_bounds__(256) void k_quantize_tile(QuantizeArgs a)
 {
-    constexpr int kPitch = 1024 + 32;          // LDS bytes of eight columns of 128 rows: 16 lanes' writes meet no bank twice
+    // LDS bytes of eight columns of 128 rows.  The pitch is eight banks, so that of 16 lanes' writes those four apart meet: 12 cycles of
+    // conflicts a write (3584 x 8192: 688128 in 57344 writes), beside what bounds the kernel.
+    constexpr int kPitch = 1024 + 32;
     __shared__ __align__(16) uint8_t tile[16 * kPitch];
     __shared__ uint32_t most_of[4][128];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, tc = tid & 15, tr = tid >> 4;
@@ -510,7 +512,9 @@ static int row_registers(uint64_t cols) { return cols <= 8192 ? 1 : cols <= 1638
 
 // The gradient's blocks: what the 256 compute units hold at once, at up to 16 waves each (its registers allow no more), or 12 where
 // rows may lie on cache lines and fewer waves keep the memory busy.  With 16, 12 and 8 waves, us in bf16: 16384 x 2048 69, 64 and 62,
-// x 5120 179 (two rounds), 152 and 152, x 1155 79, 94 and 111.
+// x 5120 179 (two rounds), 152 and 152, x 1155 79, 94 and 111.  Sums are taken in an order of the sizes alone, and the
+// workspace goes by them too: so a number of columns that makes whole lines of dense rows in 16 bits stands for the alignment, which is not
+// looked at.  A block that has one row, where there are places for all, leaves a part as long as the row in fp32.
 static uint32_t blocks_of(uint64_t rows, uint64_t cols)
 {
     if (row_registers(cols) > 2) return (uint32_t)std::min<uint64_t>((rows + 3) / 4, 32);
