@@ -560,6 +560,90 @@ int reft_product(const void *a, uint64_t ld_a, int a_format, const void *a_scale
                  uint64_t K, void *c, uint64_t ld_c, int c_dtype, void *workspace, uint64_t workspace_bytes,
                  reft_stream stream);
 
+/* ---- inside the sublayers -------------------------------------------------------------------------------
+ * What lies between the products: queries and keys on their way into attention, the activation of a feed-forward, and the
+ * 8-bit matrices that the forward pass keeps for the backward pass.  As above: no atomics, sums in an order of the sizes alone, fp32
+ * within, one rounding.
+ */
+
+/* Values [rows][heads][cols]: element (r, a, c) is number r * row + a * head + c behind p.  Heads may lie one after the other
+ * within a row, rows within a head, or both with gaps; results have their elements in places of their own, inputs need not (row or head may be 0).
+ */
+typedef struct reft_heads {
+    void *p;
+    uint64_t row, head;
+} reft_heads;
+
+/* An 8-bit matrix with scales per 128 columns of a row (see above). */
+typedef struct reft_eight {
+    void *q;
+    uint64_t ld;
+    void *scales;
+    uint64_t ld_s;
+} reft_eight;
+
+/* Each head x of queries (q) and keys (k; NULL: none) is normed, z = x weight / sqrt(mean(x^2) + eps), and its first 2 pairs columns are
+ * turned by the position of the row: pair i is (i, i + pairs) or, with adjacent != 0, (2 i, 2 i + 1), its angle t = positions[r] freqs[i], and
+ *   out[first] = z[first] cos t - z[second] sin t,  out[second] = z[second] cos t + z[first] sin t,  out[c] = z[c] behind the pairs.
+ * Angles are products in 64 bits (exact for positions below 2^29; at most 2^50), sines and cosines of them err by less than 2^-22.  A weight is a
+ * vector of cols values for all heads of its kind in weight_dtype (dtype or fp32), NULL: ones.  positions and freqs may be NULL with pairs == 0.
+ * An output may be its input (with the same strides).  rows < 2^31, 1 to 65535 heads of each kind, 1 <= cols <= 512, 2 pairs <= cols.
+ */
+int reft_heads_forward(const reft_heads *q, uint64_t q_heads, const reft_heads *k, uint64_t k_heads, const void *q_weight,
+                       const void *k_weight, const int64_t *positions, const float *freqs, uint64_t pairs, int adjacent,
+                       uint64_t rows, uint64_t cols, int dtype, int weight_dtype, double eps, const reft_heads *q_out,
+                       const reft_heads *k_out, reft_stream stream);
+
+/* The gradients of reft_heads_forward's inputs and weights, from those of its outputs (dq_out, dk_out) and its other arguments.  With u the
+ * gradient of z (dout turned back) and x' = x / sqrt(mean(x^2) + eps):
+ *   dx = (u weight - x' mean(u weight x')) / sqrt(mean(x^2) + eps),  dweight[c] = sum over rows and heads of u x'.
+ * dq, dk and the weights' gradients (fp32) are each left out where NULL; dq may be dq_out or q, dk dk_out or k (with the same strides).
+ * rows == 0 gives dweight = 0.  workspace: on 16 bytes, of at least reft_heads_backward_workspace(rows, q_heads, k_heads, cols) bytes where a
+ * weight's gradient is wanted; scratch, not shared with a call in flight.
+ */
+uint64_t reft_heads_backward_workspace(uint64_t rows, uint64_t q_heads, uint64_t k_heads, uint64_t cols);
+int reft_heads_backward(const reft_heads *dq_out, const reft_heads *dk_out, const reft_heads *q, uint64_t q_heads,
+                        const reft_heads *k, uint64_t k_heads, const void *q_weight, const void *k_weight,
+                        const int64_t *positions, const float *freqs, uint64_t pairs, int adjacent, uint64_t rows,
+                        uint64_t cols, int dtype, int weight_dtype, double eps, const reft_heads *dq, const reft_heads *dk,
+                        float *dq_weight, float *dk_weight, void *workspace, uint64_t workspace_bytes, reft_stream stream);
+
+/* y = act(g) u (u == NULL: act(g)), as y in dtype and, or, in 8 bits as y8; g and u themselves in 8 bits as g8 and u8: what
+ * reft_gate_backward reads, a byte a value instead of two or four.  act(g) is
+ *   REFT_SILU       g / (1 + exp(-g))
+ *   REFT_GELU       g (1 + erf(g / sqrt(2))) / 2
+ *   REFT_GELU_TANH  g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2
+ *   REFT_RELU2      max(g, 0)^2
+ * Outputs are each left out where NULL.  y may be g or u (with the same ld).  Where a block of 128 values of g8, u8 or y8 holds an infinity or
+ * a NaN, all of it is NaN.  rows < 2^31, cols <= 128 * 65535, ceil(rows / 4) ceil(cols / 512) < 2^24.
+ */
+#define REFT_SILU      0
+#define REFT_GELU      1
+#define REFT_GELU_TANH 2
+#define REFT_RELU2     3
+int reft_gate_forward(const void *g, uint64_t ld_g, const void *u, uint64_t ld_u, uint64_t rows, uint64_t cols, int dtype,
+                      int act, void *y, uint64_t ld_y, const reft_eight *y8, int y_format, const reft_eight *g8,
+                      const reft_eight *u8, int kept_format, reft_stream stream);
+
+/* The gradients of g and u from dy, at the values that g8 and u8 (NULL: there is no u) stand for:
+ *   dg = dy u act'(g),  du = dy act(g),
+ * as dg and du in dtype; in 8 bits (grad_format) as dg8 and du8, for the product that gives the gradient of the products' inputs, and transposed, as
+ * dg8_t and du8_t ([cols][rows], scales per 128 rows), for that of their weights; and y = act(g) u, transposed, as y8_t in y_format, for the gradient
+ * of the weights that y is multiplied by.  Outputs are each left out where NULL.  dg or du may be dy (with the same ld).
+ * rows, cols < 2^31, ceil(rows / 128) ceil(cols / 128) < 2^23.
+ */
+int reft_gate_backward(const void *dy, uint64_t ld_dy, const reft_eight *g8, const reft_eight *u8, int kept_format,
+                       uint64_t rows, uint64_t cols, int dtype, int act, void *dg, uint64_t ld_dg, void *du, uint64_t ld_du,
+                       const reft_eight *dg8, const reft_eight *du8, const reft_eight *dg8_t, const reft_eight *du8_t,
+                       int grad_format, const reft_eight *y8_t, int y_format, reft_stream stream);
+
+/* q_t = the transpose of the 8-bit matrix q ([rows][cols]), with scales per 128 rows of q: what the norm or the gate has kept, for the product of the
+ * weights' gradient.  A value keeps all its bits where its new block's power of two is not larger than its old one, or not by so much that it
+ * becomes subnormal, and the formats are the same.  Limits as for reft_gate_backward.
+ */
+int reft_transpose(const reft_eight *q, int format, uint64_t rows, uint64_t cols, const reft_eight *q_t, int format_t,
+                   reft_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -4,6 +4,8 @@ Nothing here is shared with the product.  Matrices are float64 arrays; 8-bit val
 """
 from __future__ import annotations
 
+import math
+
 import numpy as np
 
 LARGEST = {"e4m3": 448.0, "e5m2": 57344.0}
@@ -111,3 +113,59 @@ def scaled(q, scales, blocks: bool):
 
 def product(a, a_scales, b, b_scales, b_blocks: bool):
     return scaled(a, a_scales, False) @ scaled(b, b_scales, b_blocks).T
+
+
+# ---- inside the sublayers ---------------------------------------------------------------------------------
+def turned(x, positions, freqs, adjacent: bool, back: bool = False):
+    """The pairs of columns of x [rows][heads][cols] turned by the angles of their rows, as complex numbers; or back."""
+    n = len(freqs)
+    first, second = (slice(0, 2 * n, 2), slice(1, 2 * n, 2)) if adjacent else (slice(0, n), slice(n, 2 * n))
+    angle = np.asarray(positions, dtype=np.float64)[:, None, None] * np.asarray(freqs, dtype=np.float64)
+    z = (x[..., first] + 1j * x[..., second]) * np.exp(-1j * angle if back else 1j * angle)
+    out = x.copy()
+    out[..., first], out[..., second] = z.real, z.imag
+    return out
+
+
+def heads_forward(x, weight, positions, freqs, eps, adjacent):
+    z = x / np.sqrt((x * x).mean(axis=-1, keepdims=True) + eps) * weight
+    return turned(z, positions, freqs, adjacent)
+
+
+def heads_backward(dout, x, weight, positions, freqs, eps, adjacent):
+    """(dx, dweight)"""
+    r = 1 / np.sqrt((x * x).mean(axis=-1, keepdims=True) + eps)
+    u, xhat = turned(dout, positions, freqs, adjacent, back=True), x * r
+    g = u * weight
+    return r * (g - xhat * (g * xhat).mean(axis=-1, keepdims=True)), (u * xhat).sum(axis=(0, 1))
+
+
+def act(g, kind: str):
+    """(act(g), its slope)"""
+    if kind == "silu":
+        p = 1 / (1 + np.exp(-g))
+        return g * p, p + g * p * (1 - p)
+    if kind == "gelu":
+        p = 0.5 * _erfc(-g / np.sqrt(2))
+        return g * p, p + g * np.exp(-g * g / 2) / np.sqrt(2 * np.pi)
+    if kind == "gelu_tanh":
+        c = np.sqrt(2 / np.pi)
+        z = c * (g + 0.044715 * g ** 3)
+        p = 1 / (1 + np.exp(-2 * z))
+        return g * p, p + g * p * (1 - p) * 2 * c * (1 + 3 * 0.044715 * g * g)
+    m = np.where(g <= 0, 0.0, g)
+    return m * m, 2 * m
+
+
+_erfc = np.vectorize(math.erfc, otypes=[np.float64])
+
+
+def gate_backward(dy, g, u, kind: str):
+    """(dg, du, y)"""
+    a, slope = act(g, kind)
+    return (dy * slope, None, a) if u is None else (dy * u * slope, dy * a, a * u)
+
+
+def transpose(q, scales, to: str):
+    """(8-bit values, biased exponents [cols][blocks of rows]) of the transpose"""
+    return quantize(np.ascontiguousarray(scaled(q, scales, False).T), to, False)

@@ -35,12 +35,15 @@ __all__ = [
     "REFT_F32", "REFT_BF16", "REFT_F16", "REFT_E4M3", "REFT_E5M2", "reft_dropout", "reft_norm_forward",
     "reft_norm_backward", "reft_norm_backward_workspace", "reft_quantize", "reft_product",
     "reft_product_workspace",
+    "reft_heads_forward", "reft_heads_backward", "reft_heads_backward_workspace", "reft_gate_forward", "reft_gate_backward",
+    "reft_transpose", "REFT_SILU", "REFT_GELU", "REFT_GELU_TANH", "REFT_RELU2",
 ]
 
 REFT_OK, REFT_EINVAL, REFT_ESIZE, REFT_EHIP, REFT_EUNRECOVERABLE, REFT_EBUSY = 0, -1, -2, -3, -4, -5
 REFT_MAX_K = 32
 REFT_RECOVER_COPY, REFT_RECOVER_DECODE = 1, 2
 REFT_F32, REFT_BF16, REFT_F16, REFT_E4M3, REFT_E5M2 = 0, 1, 2, 3, 4
+REFT_SILU, REFT_GELU, REFT_GELU_TANH, REFT_RELU2 = 0, 1, 2, 3
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libreft.so")
@@ -120,6 +123,13 @@ def _load():
         "reft_quantize": (i, [vp, u64, u64, u64, i, i, i, vp, u64, vp, u64, vp, u64, vp, u64, vp]),
         "reft_product_workspace": (u64, [u64, u64, u64]),
         "reft_product": (i, [vp, u64, i, vp, u64, vp, u64, i, vp, u64, i, u64, u64, u64, vp, u64, i, vp, u64, vp]),
+        "reft_heads_forward": (i, [vp, u64, vp, u64, vp, vp, vp, vp, u64, i, u64, u64, i, i, f64, vp, vp, vp]),
+        "reft_heads_backward_workspace": (u64, [u64, u64, u64, u64]),
+        "reft_heads_backward": (i, [vp, vp, vp, u64, vp, u64, vp, vp, vp, vp, u64, i, u64, u64, i, i, f64, vp, vp, vp, vp,
+                                    vp, u64, vp]),
+        "reft_gate_forward": (i, [vp, u64, vp, u64, u64, u64, i, i, vp, u64, vp, i, vp, vp, i, vp]),
+        "reft_gate_backward": (i, [vp, u64, vp, vp, i, u64, u64, i, i, vp, u64, vp, u64, vp, vp, vp, vp, i, vp, i, vp]),
+        "reft_transpose": (i, [vp, i, u64, u64, vp, i, vp]),
         "reft_last_error": (ctypes.c_char_p, []),
         "reft_version": (ctypes.c_char_p, []),
     }
@@ -661,6 +671,209 @@ def reft_product(a, a_scales, b, b_scales, c, workspace=None, *, b_blocks: bool 
 
 def reft_product_workspace(M: int, N: int, K: int) -> int:
     return int(_load().reft_product_workspace(int(M), int(N), int(K)))
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("row", ctypes.c_uint64), ("head", ctypes.c_uint64)]
+
+
+class _Eight(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("ld", ctypes.c_uint64), ("scales", ctypes.c_void_p), ("ld_s", ctypes.c_uint64)]
+
+
+def _heads(who: str, name: str, t, shape, types):
+    """(heads, type) of a tensor [rows][heads][cols] whose heads are contiguous."""
+    if len(shape) != 3 or tuple(t.shape) != tuple(shape):
+        _refuse(who, f"{name} has the shape {tuple(t.shape)}" + (f", not {tuple(shape)}" if len(shape) == 3 else ""))
+    code = _type(t)
+    if code not in types:
+        _refuse(who, f"{name} is {t.dtype}")
+    row, head, along = t.stride()
+    if along != 1 and shape[2] > 1:
+        _refuse(who, f"{name}'s heads are not contiguous")
+    return _Heads(t.data_ptr(), row, head), code
+
+
+def _eight(who: str, name: str, pair, rows: int, cols: int, types, operands: dict):
+    """(8-bit matrix, type) of a pair (q, scales), whose tensors join the operands; (None, -1) where it is left out."""
+    if pair is None:
+        return None, -1
+    if not isinstance(pair, (tuple, list)) or len(pair) != 2 or pair[0] is None or pair[1] is None:
+        _refuse(who, f"{name} is no pair (values, scales)")
+    here = {name: pair[0], name + "'s scales": pair[1]}
+    _tensors(who, here, "")
+    operands.update(here)
+    q, ld, code = _matrix(who, name, pair[0], (rows, cols), types)
+    scales, ld_s = _scales(who, name + "'s scales", pair[1], rows, cols)
+    return _Eight(q, ld, scales, ld_s), code
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def _int64s(who: str, name: str, t, n: int):
+    if str(t.dtype) != "torch.int64" or tuple(t.shape) != (n,) or not t.is_contiguous():
+        _refuse(who, f"{name} is no contiguous vector of {n} values of int64")
+    _load_marshal().know(t.dtype, 5)
+    return t.data_ptr()
+
+
+def _turn(who: str, positions, freqs, rows: int):
+    """(positions, freqs, pairs): the rotation's part of a call."""
+    if freqs is None:
+        return None, None, 0
+    af = _vector(who, "freqs", freqs, freqs.numel(), _JUST_F32)[0]
+    if positions is None:
+        if freqs.numel():
+            _refuse(who, "positions is left out")
+        return None, None, 0
+    return _int64s(who, "positions", positions, rows), af, freqs.numel()
+
+
+def _two_weights(who: str, q_weight, k_weight, cols: int, types):
+    """(address, address, type) of the weights: of one type where both are given."""
+    aq, code = (None, None) if q_weight is None else _vector(who, "q_weight", q_weight, cols, types)
+    ak, k_code = (None, code) if k_weight is None else _vector(who, "k_weight", k_weight, cols, types if code is None else _ONLY[code])
+    return aq, ak, types[0] if k_code is None else k_code
+
+
+def reft_heads_forward(q, k, q_weight, k_weight, positions, freqs, eps: float, q_out, k_out=None, *, adjacent: bool = False,
+                       stream=None) -> None:
+    """Tensors [rows][heads][cols] of any strides but the last; ``k`` and ``k_out`` may be None.  ``positions`` are int64, ``freqs``
+    fp32: one for each pair of columns that turn."""
+    rc = (_marshal or _load_marshal()).heads_forward(q, k, q_weight, k_weight, positions, freqs, eps, q_out, k_out, adjacent, stream)
+    if rc is not None:
+        return _done(rc)
+    who = "reft_heads_forward"
+    operands = dict(q=q, k=k, q_weight=q_weight, k_weight=k_weight, positions=positions, freqs=freqs, q_out=q_out, k_out=k_out)
+    _tensors(who, operands, "q q_out" if k is None else "q q_out k_out")
+    if k is None and k_out is not None:
+        _refuse(who, "k_out without k")
+    hq, code = _heads(who, "q", q, q.shape, _FLOATS)
+    rows, q_heads, cols = q.shape
+    ho, _ = _heads(who, "q_out", q_out, q.shape, _ONLY[code])
+    hk = hko = None
+    k_heads = 0
+    if k is not None:
+        k_heads = k.shape[1] if len(k.shape) == 3 else 0
+        hk, _ = _heads(who, "k", k, (rows, k_heads, cols), _ONLY[code])
+        hko, _ = _heads(who, "k_out", k_out, (rows, k_heads, cols), _ONLY[code])
+    aq, ak, w_code = _two_weights(who, q_weight, k_weight, cols, _OR_F32[code])
+    at, af, pairs = _turn(who, positions, freqs, rows)
+    _call(who, _load().reft_heads_forward, operands, stream, _ref(hq), q_heads, _ref(hk), k_heads, aq, ak, at, af, pairs,
+          1 if adjacent else 0, rows, cols, code, w_code, eps, _ref(ho), _ref(hko))
+
+
+def reft_heads_backward(dq_out, dk_out, q, k, q_weight, k_weight, positions, freqs, eps: float, *, adjacent: bool = False, dq=None,
+                        dk=None, dq_weight=None, dk_weight=None, workspace=None, stream=None) -> None:
+    rc = (_marshal or _load_marshal()).heads_backward(dq_out, dk_out, q, k, q_weight, k_weight, positions, freqs, eps, adjacent, dq, dk,
+                                                      dq_weight, dk_weight, workspace, stream)
+    if rc is not None:
+        return _done(rc)
+    who = "reft_heads_backward"
+    operands = dict(dq_out=dq_out, dk_out=dk_out, q=q, k=k, q_weight=q_weight, k_weight=k_weight, positions=positions, freqs=freqs, dq=dq,
+                    dk=dk, dq_weight=dq_weight, dk_weight=dk_weight, workspace=workspace)
+    _tensors(who, operands, "dq_out q" if k is None else "dq_out q dk_out")
+    if k is None and not (dk_out is None and dk is None and dk_weight is None):
+        _refuse(who, "a gradient of k without k")
+    hq, code = _heads(who, "q", q, q.shape, _FLOATS)
+    rows, q_heads, cols = q.shape
+    hdo, _ = _heads(who, "dq_out", dq_out, q.shape, _ONLY[code])
+    hdq = None if dq is None else _heads(who, "dq", dq, q.shape, _ONLY[code])[0]
+    hk = hdko = hdk = None
+    k_heads = 0
+    if k is not None:
+        k_heads = k.shape[1] if len(k.shape) == 3 else 0
+        shape = (rows, k_heads, cols)
+        hk, _ = _heads(who, "k", k, shape, _ONLY[code])
+        hdko, _ = _heads(who, "dk_out", dk_out, shape, _ONLY[code])
+        hdk = None if dk is None else _heads(who, "dk", dk, shape, _ONLY[code])[0]
+    aq, ak, w_code = _two_weights(who, q_weight, k_weight, cols, _OR_F32[code])
+    at, af, pairs = _turn(who, positions, freqs, rows)
+    adq = None if dq_weight is None else _vector(who, "dq_weight", dq_weight, cols, _JUST_F32)[0]
+    adk = None if dk_weight is None else _vector(who, "dk_weight", dk_weight, cols, _JUST_F32)[0]
+    ws, ws_bytes = _scratch(who, workspace)
+    _call(who, _load().reft_heads_backward, operands, stream, _ref(hdo), _ref(hdko), _ref(hq), q_heads, _ref(hk), k_heads, aq, ak, at, af,
+          pairs, 1 if adjacent else 0, rows, cols, code, w_code, eps, _ref(hdq), _ref(hdk), adq, adk, ws, ws_bytes)
+
+
+def reft_heads_backward_workspace(rows: int, q_heads: int, k_heads: int, cols: int) -> int:
+    return int(_load().reft_heads_backward_workspace(int(rows), int(q_heads), int(k_heads), int(cols)))
+
+
+_ACTS = {"silu": REFT_SILU, "gelu": REFT_GELU, "gelu_tanh": REFT_GELU_TANH, "relu2": REFT_RELU2}
+
+
+def _act(who: str, act) -> int:
+    """An activation by its name, or its number."""
+    code = _ACTS.get(act, act) if isinstance(act, (str, int)) else None
+    if not isinstance(code, int):
+        _refuse(who, f"unknown activation {act!r}")
+    return code
+
+
+def reft_gate_forward(g, u, act, *, y=None, y8=None, g8=None, u8=None, stream=None) -> None:
+    """``act`` is "silu", "gelu", "gelu_tanh" or "relu2" (or its REFT_ number); ``y8``, ``g8`` and ``u8`` are pairs (float8 tensor, its scales).
+    ``u`` may be None."""
+    who = "reft_gate_forward"
+    code_act = _act(who, act)
+    rc = (_marshal or _load_marshal()).gate_forward(g, u, code_act, y, y8, g8, u8, stream)
+    if rc is not None:
+        return _done(rc)
+    operands = dict(g=g, u=u, y=y)
+    _tensors(who, operands, "g")
+    ag, ld_g, code = _matrix(who, "g", g, g.shape, _FLOATS)
+    rows, cols = shape = g.shape
+    au, ld_u, _ = _NONE if u is None else _matrix(who, "u", u, shape, _ONLY[code])
+    ay, ld_y, _ = _NONE if y is None else _matrix(who, "y", y, shape, _ONLY[code])
+    ey, y_fmt = _eight(who, "y8", y8, rows, cols, _EIGHTS, operands)
+    eg, fmt = _eight(who, "g8", g8, rows, cols, _EIGHTS, operands)
+    eu, u_fmt = _eight(who, "u8", u8, rows, cols, _EIGHTS if fmt < 0 else _ONLY[fmt], operands)
+    _call(who, _load().reft_gate_forward, operands, stream, ag, ld_g, au, ld_u, rows, cols, code, code_act, ay, ld_y, _ref(ey), y_fmt,
+          _ref(eg), _ref(eu), max(fmt, u_fmt))
+
+
+def reft_gate_backward(dy, g8, u8, act, *, dg=None, du=None, dg8=None, du8=None, dg8_t=None, du8_t=None, y8_t=None, stream=None) -> None:
+    """``g8`` and ``u8`` (may be None) as the forward pass has left them; 8-bit results are pairs (float8 tensor, its scales), those of
+    gradients of one type, and ``_t`` of the transpose's shape."""
+    who = "reft_gate_backward"
+    code_act = _act(who, act)
+    rc = (_marshal or _load_marshal()).gate_backward(dy, g8, u8, code_act, dg, du, dg8, du8, dg8_t, du8_t, y8_t, stream)
+    if rc is not None:
+        return _done(rc)
+    operands = dict(dy=dy, dg=dg, du=du)
+    _tensors(who, operands, "dy")
+    ady, ld_dy, code = _matrix(who, "dy", dy, dy.shape, _FLOATS)
+    rows, cols = shape = dy.shape
+    adg, ld_dg, _ = _NONE if dg is None else _matrix(who, "dg", dg, shape, _ONLY[code])
+    adu, ld_du, _ = _NONE if du is None else _matrix(who, "du", du, shape, _ONLY[code])
+    if g8 is None:
+        _refuse(who, "g8 is left out")
+    eg, kept = _eight(who, "g8", g8, rows, cols, _EIGHTS, operands)
+    eu, _ = _eight(who, "u8", u8, rows, cols, _ONLY[kept], operands)
+    fmt, grads = -1, []
+    for name, pair, r, c in (("dg8", dg8, rows, cols), ("du8", du8, rows, cols), ("dg8_t", dg8_t, cols, rows), ("du8_t", du8_t, cols, rows)):
+        e, f = _eight(who, name, pair, r, c, _EIGHTS if fmt < 0 else _ONLY[fmt], operands)
+        fmt = max(fmt, f)
+        grads.append(_ref(e))
+    ey, y_fmt = _eight(who, "y8_t", y8_t, cols, rows, _EIGHTS, operands)
+    _call(who, _load().reft_gate_backward, operands, stream, ady, ld_dy, _ref(eg), _ref(eu), kept, rows, cols, code, code_act, adg, ld_dg, adu,
+          ld_du, *grads, fmt, _ref(ey), y_fmt)
+
+
+def reft_transpose(q, scales, q_t, scales_t, *, stream=None) -> None:
+    """``q_t``, a float8 tensor of the shape of the transpose of ``q``, and its scales get what ``q`` and its scales stand for."""
+    rc = (_marshal or _load_marshal()).transpose(q, scales, q_t, scales_t, stream)
+    if rc is not None:
+        return _done(rc)
+    who, operands = "reft_transpose", dict(q=q, scales=scales, q_t=q_t, scales_t=scales_t)
+    _tensors(who, operands, "q scales q_t scales_t")
+    _matrix(who, "q", q, q.shape, _EIGHTS)
+    rows, cols = q.shape
+    e, fmt = _eight(who, "q", (q, scales), rows, cols, _EIGHTS, {})
+    t, fmt_t = _eight(who, "q_t", (q_t, scales_t), cols, rows, _EIGHTS, {})
+    _call(who, _load().reft_transpose, operands, stream, _ref(e), fmt, rows, cols, _ref(t), fmt_t)
 
 
 def reft_set_tunable(name: str, value: int) -> None:

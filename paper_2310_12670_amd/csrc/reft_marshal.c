@@ -17,7 +17,8 @@ static PyObject *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_stream, *s_size, 
 static int here;                               /* the current GPU in the call under way (all calls hold the interpreter's lock) */
 
 int hipGetDevice(int *device);                 /* of the HIP runtime that the library is linked with; 0: success */
-static PyObject *known[5];                     /* torch's dtypes by the library's numbers, as they have been met */
+enum { INT64 = 5, KNOWN };                     /* beside the library's types: the positions' */
+static PyObject *known[KNOWN];                 /* torch's dtypes by the library's numbers, as they have been met */
 
 typedef struct {
     void *p;
@@ -43,7 +44,7 @@ static int type_of(PyObject *t, int *type)
 {
     PyObject *d = PyObject_GetAttr(t, s_dtype);
     *type = -1;
-    for (int i = 0; i < 5 && d; ++i)
+    for (int i = 0; i < KNOWN && d; ++i)
         if (d == known[i]) *type = i;
     Py_XDECREF(d);
     PyErr_Clear();
@@ -159,7 +160,10 @@ static int whole(PyObject *v, uint64_t *out)
     return ok;
 }
 
-#define OTHERWISE(cond) if (!(cond)) Py_RETURN_NONE
+#define OTHERWISE(cond)                                                                           \
+    do {                                                                                          \
+        if (!(cond)) Py_RETURN_NONE;                                                              \
+    } while (0)
 #define CALL(expr)                                                                                \
     do {                                                                                          \
         int rc;                                                                                   \
@@ -239,12 +243,138 @@ static PyObject *py_product(PyObject *self, PyObject *const *v, Py_ssize_t n)
                       room.n[0], stream));
 }
 
+/* Values [rows][heads][cols] with contiguous heads; of a shape where `like` is given. */
+static int heads(PyObject *t, int optional, const uint64_t *like, int types, operand *o, reft_heads *h)
+{
+    o->type = -1, h->p = NULL;
+    if (t == Py_None) return optional;
+    return numbers(PyObject_GetAttr(t, s_shape), 3, o->n) &&
+           (!like || (o->n[0] == like[0] && o->n[1] == like[1] && o->n[2] == like[2])) &&
+           numbers(PyObject_CallMethodNoArgs(t, s_stride), 3, o->step) && o->step[2] == 1 && type_of(t, &o->type) && (types >> o->type & 1) &&
+           address_of(t, &h->p) && (h->row = o->step[0], h->head = o->step[1], 1);
+}
+
+/* A pair (8-bit matrix, its scales), or None. */
+static int eight(PyObject *t, uint64_t rows, uint64_t cols, int types, int *type, reft_eight *e)
+{
+    operand q, s;
+    const uint64_t like[2] = {rows, cols};
+    e->q = NULL, *type = -1;
+    if (t == Py_None) return 1;
+    if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 2 || !matrix(PyTuple_GET_ITEM(t, 0), 0, like, types, &q) ||
+        !scales(PyTuple_GET_ITEM(t, 1), 0, rows, cols, &s))
+        return 0;
+    e->q = q.p, e->ld = q.ld, e->scales = s.p, e->ld_s = s.ld, *type = q.type;
+    return 1;
+}
+
+/* Positions and frequencies. */
+static int rotation(PyObject *positions, PyObject *freqs, uint64_t rows, operand *at, operand *f)
+{
+    return numbers(PyObject_GetAttr(freqs, s_shape), 1, f->n) && vector(freqs, 0, f->n[0], 1 << REFT_F32, f) &&
+           vector(positions, 0, rows, 1 << INT64, at);
+}
+
+/* Weights of one type where both are given. */
+static int two_weights(PyObject *vq, PyObject *vk, uint64_t cols, int type, operand *wq, operand *wk)
+{
+    return vector(vq, 1, cols, or_f32(type), wq) && vector(vk, 1, cols, wq->type < 0 ? or_f32(type) : 1 << wq->type, wk);
+}
+
+static PyObject *py_heads_forward(PyObject *self, PyObject *const *v, Py_ssize_t n)
+{
+    operand q, k, wq, wk, at, f, o;
+    reft_heads hq, hk, ho, hko;
+    double eps;
+    void *stream;
+    OTHERWISE(begin(n, 11) && heads(v[0], 0, NULL, FLOATS, &q, &hq));
+    OTHERWISE(heads(v[1], 1, NULL, 1 << q.type, &k, &hk) && (k.type < 0 || (k.n[0] == q.n[0] && k.n[2] == q.n[2])) &&
+              two_weights(v[2], v[3], q.n[2], q.type, &wq, &wk) && rotation(v[4], v[5], q.n[0], &at, &f) && real(v[6], &eps) &&
+              heads(v[7], 0, q.n, 1 << q.type, &o, &ho) && (k.type < 0 ? v[8] == Py_None : heads(v[8], 0, k.n, 1 << q.type, &o, &hko)));
+    const int adjacent = PyObject_IsTrue(v[9]);
+    PyErr_Clear();
+    OTHERWISE(adjacent >= 0 && stream_of(v[10], &stream));
+    CALL(reft_heads_forward(&hq, q.n[1], k.type < 0 ? NULL : &hk, k.type < 0 ? 0 : k.n[1], wq.p, wk.p, at.p, f.p, f.n[0], adjacent, q.n[0], q.n[2],
+                            q.type, wq.type >= 0 ? wq.type : wk.type >= 0 ? wk.type : q.type, eps, &ho, k.type < 0 ? NULL : &hko, stream));
+}
+
+static PyObject *py_heads_backward(PyObject *self, PyObject *const *v, Py_ssize_t n)
+{
+    operand q, k, wq, wk, at, f, o, dq, dk, gq, gk, room;
+    reft_heads hq, hk, hdo, hdko, hdq, hdk;
+    double eps;
+    void *stream;
+    OTHERWISE(begin(n, 16) && heads(v[2], 0, NULL, FLOATS, &q, &hq));
+    OTHERWISE(heads(v[3], 1, NULL, 1 << q.type, &k, &hk) && (k.type < 0 || (k.n[0] == q.n[0] && k.n[2] == q.n[2])) &&
+              heads(v[0], 0, q.n, 1 << q.type, &o, &hdo) && two_weights(v[4], v[5], q.n[2], q.type, &wq, &wk) &&
+              rotation(v[6], v[7], q.n[0], &at, &f) && real(v[8], &eps) && heads(v[10], 1, q.n, 1 << q.type, &dq, &hdq) &&
+              vector(v[12], 1, q.n[2], 1 << REFT_F32, &gq) && vector(v[13], 1, q.n[2], 1 << REFT_F32, &gk) && scratch(v[14], &room));
+    if (k.type < 0) {
+        dk.type = -1;
+        OTHERWISE(v[1] == Py_None && v[11] == Py_None && v[13] == Py_None);
+    } else {
+        OTHERWISE(heads(v[1], 0, k.n, 1 << q.type, &o, &hdko) && heads(v[11], 1, k.n, 1 << q.type, &dk, &hdk));
+    }
+    const int adjacent = PyObject_IsTrue(v[9]);
+    PyErr_Clear();
+    OTHERWISE(adjacent >= 0 && stream_of(v[15], &stream));
+    CALL(reft_heads_backward(&hdo, k.type < 0 ? NULL : &hdko, &hq, q.n[1], k.type < 0 ? NULL : &hk, k.type < 0 ? 0 : k.n[1], wq.p, wk.p, at.p,
+                             f.p, f.n[0], adjacent, q.n[0], q.n[2], q.type, wq.type >= 0 ? wq.type : wk.type >= 0 ? wk.type : q.type, eps,
+                             dq.type < 0 ? NULL : &hdq, dk.type < 0 ? NULL : &hdk, gq.p, gk.p, room.p, room.n[0], stream));
+}
+
+static PyObject *py_gate_forward(PyObject *self, PyObject *const *v, Py_ssize_t n)
+{
+    operand g, u, y;
+    reft_eight y8, g8, u8;
+    int fy, fg, fu;
+    uint64_t act;
+    void *stream;
+    OTHERWISE(begin(n, 8) && matrix(v[0], 0, NULL, FLOATS, &g));
+    OTHERWISE(matrix(v[1], 1, g.n, 1 << g.type, &u) && whole(v[2], &act) && act < 256 && matrix(v[3], 1, g.n, 1 << g.type, &y) &&
+              eight(v[4], g.n[0], g.n[1], EIGHTS, &fy, &y8) && eight(v[5], g.n[0], g.n[1], EIGHTS, &fg, &g8) &&
+              eight(v[6], g.n[0], g.n[1], fg < 0 ? EIGHTS : 1 << fg, &fu, &u8) && stream_of(v[7], &stream));
+    CALL(reft_gate_forward(g.p, g.ld, u.p, u.ld, g.n[0], g.n[1], g.type, (int)act, y.p, y.ld, &y8, fy, &g8, &u8, fg >= 0 ? fg : fu, stream));
+}
+
+static PyObject *py_gate_backward(PyObject *self, PyObject *const *v, Py_ssize_t n)
+{
+    operand dy, dg, du;
+    reft_eight g8, u8, grads[4], y8_t;
+    int kept, f, fmt = -1, fy;
+    uint64_t act;
+    void *stream;
+    OTHERWISE(begin(n, 12) && matrix(v[0], 0, NULL, FLOATS, &dy));
+    const uint64_t rows = dy.n[0], cols = dy.n[1];
+    OTHERWISE(eight(v[1], rows, cols, EIGHTS, &kept, &g8) && kept >= 0 && eight(v[2], rows, cols, 1 << kept, &f, &u8) && whole(v[3], &act) &&
+              act < 256 && matrix(v[4], 1, dy.n, 1 << dy.type, &dg) && matrix(v[5], 1, dy.n, 1 << dy.type, &du));
+    for (int i = 0; i < 4; ++i) {
+        OTHERWISE(eight(v[6 + i], i < 2 ? rows : cols, i < 2 ? cols : rows, fmt < 0 ? EIGHTS : 1 << fmt, &f, &grads[i]));
+        if (fmt < 0) fmt = f;
+    }
+    OTHERWISE(eight(v[10], cols, rows, EIGHTS, &fy, &y8_t) && stream_of(v[11], &stream));
+    CALL(reft_gate_backward(dy.p, dy.ld, &g8, &u8, kept, rows, cols, dy.type, (int)act, dg.p, dg.ld, du.p, du.ld, &grads[0], &grads[1], &grads[2],
+                            &grads[3], fmt, &y8_t, fy, stream));
+}
+
+static PyObject *py_transpose(PyObject *self, PyObject *const *v, Py_ssize_t n)
+{
+    operand q, s, t, st;
+    void *stream;
+    OTHERWISE(begin(n, 5) && matrix(v[0], 0, NULL, EIGHTS, &q));
+    const uint64_t turned[2] = {q.n[1], q.n[0]};
+    OTHERWISE(scales(v[1], 0, q.n[0], q.n[1], &s) && matrix(v[2], 0, turned, EIGHTS, &t) && scales(v[3], 0, q.n[1], q.n[0], &st) &&
+              stream_of(v[4], &stream));
+    const reft_eight a = {q.p, q.ld, s.p, s.ld}, b = {t.p, t.ld, st.p, st.ld};
+    CALL(reft_transpose(&a, q.type, q.n[0], q.n[1], &b, t.type, stream));
+}
+
 /* know(dtype, number) */
 static PyObject *py_know(PyObject *self, PyObject *const *v, Py_ssize_t n)
 {
     const long i = n == 2 ? PyLong_AsLong(v[1]) : -1;
     if (PyErr_Occurred()) return NULL;
-    if (i < 0 || i >= 5) {
+    if (i < 0 || i >= KNOWN) {
         PyErr_SetString(PyExc_ValueError, "know(dtype, number of a type)");
         return NULL;
     }
@@ -255,7 +385,8 @@ static PyObject *py_know(PyObject *self, PyObject *const *v, Py_ssize_t n)
 
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(dropout), METHOD(norm_forward), METHOD(norm_backward), METHOD(quantize),
-                                METHOD(product), METHOD(know), {NULL, NULL, 0, NULL}};
+                                METHOD(product), METHOD(heads_forward), METHOD(heads_backward),
+                                METHOD(gate_forward), METHOD(gate_backward), METHOD(transpose), METHOD(know), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__marshal(void)

@@ -1,6 +1,6 @@
 // Operators of a training step that read and write each value once: dropout, root-mean-square norm with the
 // residual's addition (forward, backward), quantization to 8 bits.  Kernels and their entry points (see include/reft.h).
-#include "reft_step.hpp"
+#include "reft_calls.hpp"
 
 #include <algorithm>
 #include <cmath>
@@ -371,15 +371,6 @@ template <typename T> __global__ __launch_bounds__(256) void k_quantize_rows(Qua
     if ((lane & 15) == 0) a.scales[((uint64_t)blockIdx.y * a.ld_s + row) * 4 + lane / 16] = n ? (uint8_t)e : 127;
 }
 
-// The scale byte of block b of a row, and ones in the rest of its word behind the last of the `blocks` blocks.
-__device__ __forceinline__ void store_scale(uint8_t *scales, uint64_t ld, uint64_t row, uint64_t b, uint64_t blocks, uint32_t e)
-{
-    uint8_t *word = scales + ((b / 4) * ld + row) * 4;
-    word[b % 4] = (uint8_t)e;
-    if (b + 1 == blocks)
-        for (int i = (int)(b % 4) + 1; i < 4; ++i) word[i] = 127;
-}
-
 // A tile of 128 x 128 values, in registers: a thread holds 8 rows of 8 columns, so that each of its columns is 8 bytes of
 // the transpose, which leaves through LDS in whole rows.  BLOCKS: one scale for the tile, else one for each row and, in the
 // transpose, for each column.  LINES: the results' rows lie on cache lines, which a tile then writes whole.  Bound by HBM where large:
@@ -490,10 +481,8 @@ template <typename T, bool BLOCKS, bool LINES> __global__ __launch_bounds__(256)
 // ------------------------------------------------------------------------------------------------
 // which kernel
 // ------------------------------------------------------------------------------------------------
-// Rows on cache lines are read past the L2.  (Gradient of 16384 x 8192 in bf16: 241 us kept, 227 not; dropout of 16384 x 11008: 120
+// Rows on cache lines (on_lines) are read past the L2.  (Gradient of 16384 x 8192 in bf16: 241 us kept, 227 not; dropout of 16384 x 11008: 120
 // and 115.  Of other rows each line is read twice: dropout of 4096 x 5003 in fp32 31 and 38, of 16384 x 1155 16.8 and 19.7.)
-static bool on_lines(const void *p, uint64_t row_bytes) { return ((uintptr_t)p | row_bytes) % 128 == 0; }
-
 template <typename T> static void launch_dropout(const DropoutArgs &a, bool lines, uint32_t blocks, hipStream_t s)
 {
     if (lines) k_dropout<T, true><<<blocks, 256, 0, s>>>(a);
@@ -559,14 +548,6 @@ template <typename T, typename R> static hipError_t launch_backward(const NormBa
     return hipGetLastError();
 }
 
-constexpr uint64_t kMaxBlocks256 = 0xffffff;            // a grid has less than 2^32 threads: blocks of 256
-
-static bool is_float_type(int t) { return t == REFT_F32 || t == REFT_BF16 || t == REFT_F16; }
-static bool is_eight(int t) { return t == REFT_E4M3 || t == REFT_E5M2; }
-static size_t size_of(int t) { return t == REFT_F32 ? 4 : 2; }
-// Arrays of elements lie on multiples of an element.
-static bool lies(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
-
 // p in [0, 1] as a threshold of 65536; false if it is none.
 static bool make_dropout(double p, uint64_t seed, uint64_t offset, Dropout *d)
 {
@@ -584,17 +565,6 @@ static bool make_dropout(double p, uint64_t seed, uint64_t offset, Dropout *d)
 }  // namespace reft
 
 using namespace reft;
-
-#define NEED(cond, code, ...)                                                                     \
-    do {                                                                                          \
-        if (!(cond)) return fail(code, __VA_ARGS__);                                              \
-    } while (0)
-
-static int launched(const char *who, hipError_t e)
-{
-    if (e != hipSuccess) return fail(REFT_EHIP, "%s: %s", who, hipGetErrorString(e));
-    return REFT_OK;
-}
 
 extern "C" int reft_dropout(const void *x, uint64_t ld_x, void *y, uint64_t ld_y, uint64_t rows, uint64_t cols, int dtype,
                             double p, uint64_t seed, uint64_t offset, reft_stream stream)

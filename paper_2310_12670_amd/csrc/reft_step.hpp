@@ -199,6 +199,15 @@ template <bool STREAM> __device__ __forceinline__ void store8_bytes(uint8_t *p, 
     }
 }
 
+// The scale byte of block b of a row, and ones in the rest of its word behind the last of the `blocks` blocks.
+__device__ __forceinline__ void store_scale(uint8_t *scales, uint64_t ld, uint64_t row, uint64_t b, uint64_t blocks, uint32_t e)
+{
+    uint8_t *word = scales + ((b / 4) * ld + row) * 4;
+    word[b % 4] = (uint8_t)e;
+    if (b + 1 == blocks)
+        for (int i = (int)(b % 4) + 1; i < 4; ++i) word[i] = 127;
+}
+
 __device__ __forceinline__ int top_of(bool e5m2) { return e5m2 ? 15 : 8; }
 
 }  // namespace reft
