@@ -20,8 +20,11 @@ struct HeadsArgs {
     const float *freqs;
     uint64_t rows;
     uint32_t cols, pairs;
-    float eps;
+    float eps, inverse_cols;
     float *part;                   // [blocks][2][cols], of the backward pass
+    uint64_t units;                // of wave_rows rows and one of `parts` parts of their heads
+    uint32_t parts;
+    uint32_t wave_rows, row_groups;        // rows that a wave works on at once, groups of lanes for each of them
     uint8_t adjacent, weight_f32;
 };
 
@@ -39,15 +42,6 @@ __device__ __forceinline__ void sine_cosine(int64_t position, float freq, float 
     *cosine = (quarter + 1) & 2 ? -b : b;
 }
 
-// The column that column c turns with, and which pair that is; c itself and none (-1) behind the pairs.
-__device__ __forceinline__ int partner_of(int c, int pairs, bool adjacent, int *pair)
-{
-    *pair = -1;
-    if (c >= 2 * pairs) return c;
-    *pair = adjacent ? c / 2 : c < pairs ? c : c - pairs;
-    return adjacent ? c ^ 1 : c < pairs ? c + pairs : c - pairs;
-}
-
 // The sum over G neighbouring lanes.
 template <int G> __device__ __forceinline__ float sum_of(float v)
 {
@@ -60,93 +54,228 @@ template <int G> __device__ __forceinline__ float sum_of(float v)
     return v;
 }
 
-template <typename T> __device__ __forceinline__ float weight_at(const HeadsArgs &a, const Side &s, int c)
+// To a step of fp32; the hardware's takes numbers below 2^-126, which eps == 0 leaves room for, for zero.
+__device__ __forceinline__ float inverse_root(float v)
 {
-    return !s.weight ? 1.f : a.weight_f32 ? ((const float *)s.weight)[c] : widen(((const T *)s.weight)[c]);
+    return v < 1.17549435e-38f ? 1.f / sqrtf(v) : __builtin_amdgcn_rsqf(v);
 }
 
-// A head belongs to G lanes with eight columns each.
-template <typename T, int G> __global__ __launch_bounds__(256) void k_heads_forward(HeadsArgs a)
+// How a lane comes to the values that its eight columns turn with: they are its own neighbours, all another lane's, or anyone's.
+enum { kAdjacent, kLane, kAny };
+
+// A wave works on `rows` rows at once, each with 64 / G / rows of its groups of G lanes; a group's lanes hold eight columns of a head each.
+// Sines and cosines are computed once a row, one pair a lane and turn, and pass through the wave's own part of LDS, as do the partners of kAny.
+template <typename T, int G, int MODE> struct Wave {
+    static constexpr int kGroups = 64 / G;
+    struct Room {
+        float2 turn[4 * 64];                               // rows x pairs <= 64 / G x 4 G
+        float values[MODE == kAny ? 64 * 8 : 1];
+    };
+    Room &room;
+    int c0, n, first;                                       // the lane's columns, the partner lane or where its group's values lie
+    int pair[8];
+    float cosine[8], sine[8];                               // of its columns; the sine with the partner's sign
+
+    __device__ __forceinline__ Wave(Room &room, const HeadsArgs &a) : room(room)
+    {
+        const int lane = threadIdx.x & 63, pairs = (int)a.pairs;
+        c0 = lane % G * 8;
+        n = (int)a.cols - c0;
+        if (MODE == kLane) first = c0 >= 2 * pairs ? lane : c0 < pairs ? lane + pairs / 8 : lane - pairs / 8;
+        if (MODE == kAny) first = lane / G * G * 8;
+    }
+    // The wave's other lanes see what this one has written; nothing moves across.
+    __device__ __forceinline__ static void settle() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
+    __device__ __forceinline__ void turn(const HeadsArgs &a, uint64_t row0, int rows, int row)
+    {
+        const int lane = threadIdx.x & 63, pairs = (int)a.pairs;
+        settle();
+        for (int at = lane; at < rows * pairs; at += 64) {
+            const int r = rows == 1 ? 0 : at / pairs;
+            if (row0 + r < a.rows) sine_cosine(a.positions[row0 + r], a.freqs[at - r * pairs], &room.turn[at].y, &room.turn[at].x);
+        }
+        settle();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = c0 + i;
+            const bool turns = c < 2 * pairs, lower = MODE == kAdjacent ? !(i & 1) : c < pairs;
+            const float2 t = turns ? room.turn[row * pairs + (MODE == kAdjacent ? c / 2 : lower ? c : c - pairs)] : float2{1.f, 0.f};
+            cosine[i] = t.x;
+            sine[i] = lower ? -t.y : t.y;
+        }
+    }
+    // The values of the partners' columns.
+    template <typename E> __device__ __forceinline__ void partners(const Eight<E> &x, float v[8], int pairs)
+    {
+        if constexpr (MODE == kAdjacent) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = x[i ^ 1];
+        } else if constexpr (MODE == kLane) {
+            Eight<E> y;
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(E) / 2; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) y.w[i][k] = (uint32_t)__shfl((int)x.w[i][k], first);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = y[i];
+        } else {
+            settle();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) room.values[first + c0 + i] = x[i];
+            settle();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = c0 + i;
+                v[i] = room.values[first + (c >= 2 * pairs ? c : c < pairs ? c + pairs : c - pairs)];
+            }
+        }
+    }
+    __device__ __forceinline__ Eight<float> weight(const HeadsArgs &a, const Side &s)
+    {
+        Eight<float> w;
+        float v[8];
+        load8_of<T>(s.weight, a.weight_f32, c0, s.weight ? n : 0, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w.t[i] = s.weight ? v[i] : 1.f;
+        return w;
+    }
+};
+
+// One of the units that the waves share: `rows` rows from row0 on, and a part of their heads.
+struct Unit {
+    uint64_t row0, row;
+    uint32_t slot;                                          // the group's among its row's
+    uint32_t part;
+};
+__device__ __forceinline__ Unit unit_of(const HeadsArgs &a, uint64_t number, int group)
 {
-    const int cols = (int)a.cols, c0 = (threadIdx.x % G) * 8, n = cols - c0;
-    const uint64_t all = a.side[0].heads + a.side[1].heads, total = a.rows * all;
-    for (uint64_t unit = (uint64_t)blockIdx.x * (256 / G) + threadIdx.x / G; unit < total; unit += (uint64_t)gridDim.x * (256 / G)) {
-        const uint64_t row = unit / all;
-        const uint32_t number = (uint32_t)(unit % all);
-        const Side &s = a.side[number >= a.side[0].heads];
-        const uint32_t head = number >= a.side[0].heads ? number - a.side[0].heads : number;
-        const T *x = (const T *)s.x + row * s.row_x + head * s.head_x;
-        float v[8], other[8], sum = 0;
-        load8<false>(x + c0, n, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            int pair;
-            const int c = min(c0 + i, cols - 1), p = partner_of(c, a.pairs, a.adjacent, &pair);
-            other[i] = widen(x[p]);
-            sum += v[i] * v[i];
+    Unit u;
+    u.part = (uint32_t)(number % a.parts);
+    u.row0 = number / a.parts * a.wave_rows;
+    u.row = u.row0 + group / a.row_groups;
+    u.slot = group % a.row_groups;
+    return u;
+}
+
+constexpr int kAhead = 2;                                   // heads of a group in flight
+
+template <typename T, int G, int MODE> __global__ __launch_bounds__(256) void k_heads_forward(HeadsArgs a)
+{
+    __shared__ typename Wave<T, G, MODE>::Room room[4];
+    const int wave = threadIdx.x >> 6, group = (threadIdx.x & 63) / G, pairs = (int)a.pairs;
+    Wave<T, G, MODE> w(room[wave], a);
+    const uint32_t step = a.row_groups * a.parts;
+    for (uint64_t number = (uint64_t)blockIdx.x * 4 + wave; number < a.units; number += (uint64_t)gridDim.x * 4) {
+        const Unit u = unit_of(a, number, group);
+        w.turn(a, u.row0, a.wave_rows, group / a.row_groups);
+    #pragma unroll 1
+        for (int kind = 0; kind < 2; ++kind) {
+            const Side &s = a.side[kind];
+            if (!s.heads) continue;
+            float other[8], by_own[8], by_other[8];
+            const Eight<float> weight = w.weight(a, s);
+            w.partners(weight, other, pairs);
+    #pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                by_own[i] = weight.t[i] * w.cosine[i];
+                by_other[i] = other[i] * w.sine[i];
+            }
+            const T *from = (const T *)s.x + u.row * s.row_x + w.c0;
+            T *to = (T *)s.out + u.row * s.row_out + w.c0;
+            // heads part, part + parts, ... of as many as the row has groups for; all lanes of the wave go round as often
+            for (uint32_t head0 = u.part * a.row_groups; head0 < s.heads; head0 += step * kAhead) {
+                Eight<T> x[kAhead];
+    #pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    const uint32_t head = head0 + k * step + u.slot;
+                    x[k].template load<false>(from + head * s.head_x, head < s.heads && u.row < a.rows ? w.n : 0);
+                }
+    #pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    const uint32_t head = head0 + k * step + u.slot;
+                    float v[8], sum = 0;
+                    w.partners(x[k], other, pairs);
+    #pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        v[i] = x[k][i];
+                        sum += v[i] * v[i];
+                    }
+                    const float r = inverse_root(sum_of<G>(sum) * a.inverse_cols + a.eps);
+    #pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = r * (v[i] * by_own[i] + other[i] * by_other[i]);
+                    store8(to + head * s.head_out, head < s.heads && u.row < a.rows ? w.n : 0, v);
+                }
+            }
         }
-        const float r = 1.f / sqrtf(sum_of<G>(sum) / (float)cols + a.eps);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            int pair;
-            const int c = min(c0 + i, cols - 1), p = partner_of(c, a.pairs, a.adjacent, &pair);
-            float sine = 0, cosine = 1;
-            if (pair >= 0) sine_cosine(a.positions[row], a.freqs[pair], &sine, &cosine);
-            v[i] = v[i] * r * weight_at<T>(a, s, c) * cosine + (p > c ? -sine : sine) * (other[i] * r * weight_at<T>(a, s, p));
-        }
-        store8((T *)s.out + row * s.row_out + head * s.head_out + c0, n, v);
     }
 }
 
-// The same for the gradients; a group of lanes sums its heads' part of the weights' gradients, the block adds its groups' in their order.
-template <typename T, int G> __global__ __launch_bounds__(256) void k_heads_backward(HeadsArgs a)
+// The gradients; a lane sums its heads' part of the weights' gradients, the block adds its groups' in their order.
+template <typename T, int G, int MODE> __global__ __launch_bounds__(256) void k_heads_backward(HeadsArgs a)
 {
+    __shared__ typename Wave<T, G, MODE>::Room room[4];
     __shared__ float fold[256 / G][G * 8];
-    const int cols = (int)a.cols, c0 = (threadIdx.x % G) * 8, n = cols - c0, group = threadIdx.x / G;
-    const uint64_t all = a.side[0].heads + a.side[1].heads, total = a.rows * all;
+    const int wave = threadIdx.x >> 6, group = (threadIdx.x & 63) / G, pairs = (int)a.pairs;
+    Wave<T, G, MODE> w(room[wave], a);
     float dw[2][8] = {};
-    for (uint64_t unit = (uint64_t)blockIdx.x * (256 / G) + group; unit < total; unit += (uint64_t)gridDim.x * (256 / G)) {
-        const uint64_t row = unit / all;
-        const uint32_t number = (uint32_t)(unit % all);
-        const bool key = number >= a.side[0].heads;
-        const Side &s = a.side[key];
-        const uint32_t head = key ? number - a.side[0].heads : number;
-        const T *dy = (const T *)s.dy + row * s.row_dy + head * s.head_dy;
-        float x[8], t[8], w[8], sum = 0, dot = 0;
-        load8<false>((const T *)s.x + row * s.row_x + head * s.head_x + c0, n, x);
-        load8<false>(dy + c0, n, t);
+    const uint32_t step = a.row_groups * a.parts;
+    for (uint64_t number = (uint64_t)blockIdx.x * 4 + wave; number < a.units; number += (uint64_t)gridDim.x * 4) {
+        const Unit u = unit_of(a, number, group);
+        w.turn(a, u.row0, a.wave_rows, group / a.row_groups);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            int pair;
-            const int c = min(c0 + i, cols - 1), p = partner_of(c, a.pairs, a.adjacent, &pair);
-            float sine = 0, cosine = 1;
-            if (pair >= 0) sine_cosine(a.positions[row], a.freqs[pair], &sine, &cosine);
-            t[i] = t[i] * cosine + (p > c ? sine : -sine) * widen(dy[p]);
-            w[i] = weight_at<T>(a, s, c);
-            sum += x[i] * x[i];
-            dot += x[i] * (t[i] * w[i]);
-        }
-        const float r = 1.f / sqrtf(sum_of<G>(sum) / (float)cols + a.eps);
-        dot = r * (sum_of<G>(dot) / (float)cols);
+        for (int kind = 0; kind < 2; ++kind) {
+            const Side &s = a.side[kind];
+            if (!s.heads) continue;
+            const Eight<float> weight = w.weight(a, s);
+            const T *from = (const T *)s.x + u.row * s.row_x + w.c0, *from_dy = (const T *)s.dy + u.row * s.row_dy + w.c0;
+            T *to = (T *)s.out + u.row * s.row_out + w.c0;
+            for (uint32_t head0 = u.part * a.row_groups; head0 < s.heads; head0 += step * kAhead) {
+                Eight<T> x[kAhead], dy[kAhead];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float xhat = x[i] * r;
-            if (key) dw[1][i] += i < n ? t[i] * xhat : 0.f;
-            else dw[0][i] += i < n ? t[i] * xhat : 0.f;
-            t[i] = r * (t[i] * w[i] - xhat * dot);
+                for (int k = 0; k < kAhead; ++k) {
+                    const uint32_t head = head0 + k * step + u.slot;
+                    const int n = head < s.heads && u.row < a.rows ? w.n : 0;
+                    x[k].template load<false>(from + head * s.head_x, n);
+                    dy[k].template load<false>(from_dy + head * s.head_dy, n);
+                }
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    const uint32_t head = head0 + k * step + u.slot;
+                    const int n = head < s.heads && u.row < a.rows ? w.n : 0;
+                    float other[8], t[8], sum = 0, dot = 0;
+                    w.partners(dy[k], other, pairs);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float v = x[k][i];
+                        t[i] = dy[k][i] * w.cosine[i] - other[i] * w.sine[i];
+                        sum += v * v;
+                        dot += v * (t[i] * weight.t[i]);
+                    }
+                    const float r = inverse_root(sum_of<G>(sum) * a.inverse_cols + a.eps);
+                    dot = r * (sum_of<G>(dot) * a.inverse_cols);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float xhat = x[k][i] * r;
+                        dw[kind][i] += i < n ? t[i] * xhat : 0.f;
+                        t[i] = r * (t[i] * weight.t[i] - xhat * dot);
+                    }
+                    if (s.out) store8(to + head * s.head_out, n, t);
+                }
+            }
         }
-        if (s.out) store8((T *)s.out + row * s.row_out + head * s.head_out + c0, n, t);
     }
     if (!a.part) return;
+#pragma unroll
     for (int kind = 0; kind < 2; ++kind) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) fold[group][c0 + i] = dw[kind][i];
+        for (int i = 0; i < 8; ++i) fold[threadIdx.x / G][w.c0 + i] = dw[kind][i];
         __syncthreads();
-        for (int c = threadIdx.x; c < cols; c += 256) {
+        for (int c = threadIdx.x; c < (int)a.cols; c += 256) {
             float s = 0;
             for (int g = 0; g < 256 / G; ++g) s += fold[g][c];
-            a.part[((uint64_t)blockIdx.x * 2 + kind) * cols + c] = s;
+            a.part[((uint64_t)blockIdx.x * 2 + kind) * a.cols + c] = s;
         }
     }
 }
@@ -173,35 +302,57 @@ __global__ __launch_bounds__(256) void k_heads_weights(const float *part, uint32
 constexpr uint64_t kMaxHeadCols = 512;
 static int lanes_of(uint64_t cols) { return cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : 64; }
 
-// As many blocks as the chip holds at once.
-static uint32_t heads_blocks(uint64_t rows, uint64_t heads, uint64_t cols)
+// How the waves share the work; of the sizes alone, as sums are taken in this order.
+struct Shares {
+    uint64_t units;
+    uint32_t parts, wave_rows, row_groups;
+};
+static Shares shares_of(uint64_t rows, uint64_t q_heads, uint64_t k_heads, uint64_t cols)
 {
-    const uint64_t groups = 256 / lanes_of(cols);
-    return (uint32_t)std::min<uint64_t>((rows * heads + groups - 1) / groups, 2048);
+    const uint64_t groups = 64 / lanes_of(cols), most = std::max(q_heads, k_heads);
+    Shares s;
+    s.row_groups = (uint32_t)groups;
+    while (s.row_groups > 1 && s.row_groups / 2 >= most) s.row_groups /= 2;
+    s.wave_rows = (uint32_t)(groups / s.row_groups);
+    const uint64_t bunches = (rows + s.wave_rows - 1) / s.wave_rows, turns = (most + s.row_groups - 1) / s.row_groups;
+    s.parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(turns, 4096 / std::max<uint64_t>(1, bunches)));
+    s.units = bunches * s.parts;
+    return s;
 }
 
-template <typename T> static hipError_t launch_forward(const HeadsArgs &a, hipStream_t s)
+// The gradients' blocks: as many as the chip holds at once.
+static uint32_t backward_blocks(const Shares &s) { return (uint32_t)std::min<uint64_t>((s.units + 3) / 4, 1024); }
+
+template <typename T, int G> static hipError_t launch(const HeadsArgs &a, uint32_t grid, bool back, hipStream_t s)
 {
-    const uint64_t heads = a.side[0].heads + a.side[1].heads;
-    const uint32_t grid = heads_blocks(a.rows, heads, a.cols);
-    switch (lanes_of(a.cols)) {
-    case 8: k_heads_forward<T, 8><<<grid, 256, 0, s>>>(a); break;
-    case 16: k_heads_forward<T, 16><<<grid, 256, 0, s>>>(a); break;
-    case 32: k_heads_forward<T, 32><<<grid, 256, 0, s>>>(a); break;
-    default: k_heads_forward<T, 64><<<grid, 256, 0, s>>>(a);
-    }
+    const int mode = a.adjacent ? kAdjacent : a.pairs % 8 ? kAny : kLane;
+    if (!back && mode == kAdjacent) k_heads_forward<T, G, kAdjacent><<<grid, 256, 0, s>>>(a);
+    else if (!back && mode == kLane) k_heads_forward<T, G, kLane><<<grid, 256, 0, s>>>(a);
+    else if (!back) k_heads_forward<T, G, kAny><<<grid, 256, 0, s>>>(a);
+    else if (mode == kAdjacent) k_heads_backward<T, G, kAdjacent><<<grid, 256, 0, s>>>(a);
+    else if (mode == kLane) k_heads_backward<T, G, kLane><<<grid, 256, 0, s>>>(a);
+    else k_heads_backward<T, G, kAny><<<grid, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
-template <typename T> static hipError_t launch_backward(const HeadsArgs &a, uint32_t grid, hipStream_t s)
+template <typename T> static hipError_t launch(HeadsArgs a, const Shares &share, bool back, hipStream_t s)
 {
+    a.units = share.units;
+    a.parts = share.parts;
+    a.wave_rows = share.wave_rows;
+    a.row_groups = share.row_groups;
+    const uint32_t grid = back ? backward_blocks(share) : (uint32_t)std::min<uint64_t>((share.units + 3) / 4, kMaxBlocks256);
     switch (lanes_of(a.cols)) {
-    case 8: k_heads_backward<T, 8><<<grid, 256, 0, s>>>(a); break;
-    case 16: k_heads_backward<T, 16><<<grid, 256, 0, s>>>(a); break;
-    case 32: k_heads_backward<T, 32><<<grid, 256, 0, s>>>(a); break;
-    default: k_heads_backward<T, 64><<<grid, 256, 0, s>>>(a);
+    case 8: return launch<T, 8>(a, grid, back, s);
+    case 16: return launch<T, 16>(a, grid, back, s);
+    case 32: return launch<T, 32>(a, grid, back, s);
+    default: return launch<T, 64>(a, grid, back, s);
     }
-    return hipGetLastError();
+}
+
+static hipError_t launch(const HeadsArgs &a, const Shares &share, int dtype, bool back, hipStream_t s)
+{
+    return dtype == REFT_F32 ? launch<float>(a, share, back, s) : dtype == REFT_BF16 ? launch<bf16>(a, share, back, s) : launch<f16>(a, share, back, s);
 }
 
 // Elements in places of their own: a row's heads one behind the other, or a head's rows.
@@ -239,6 +390,7 @@ static HeadsArgs heads_args(const int64_t *positions, const float *freqs, uint64
     a.cols = (uint32_t)cols;
     a.pairs = (uint32_t)pairs;
     a.eps = (float)eps;
+    a.inverse_cols = 1.f / (float)cols;
     a.adjacent = adjacent != 0;
     a.weight_f32 = weight_dtype == REFT_F32;
     return a;
@@ -280,16 +432,13 @@ extern "C" int reft_heads_forward(const reft_heads *q, uint64_t q_heads, const r
     HeadsArgs a = heads_args(positions, freqs, pairs, adjacent, rows, cols, weight_dtype, eps);
     a.side[0] = side_of(q, q_heads, q_weight, nullptr, q_out);
     if (k) a.side[1] = side_of(k, k_heads, k_weight, nullptr, k_out);
-    hipStream_t s = (hipStream_t)stream;
-    return launched(who, dtype == REFT_F32    ? launch_forward<float>(a, s)
-                         : dtype == REFT_BF16 ? launch_forward<bf16>(a, s)
-                                              : launch_forward<f16>(a, s));
+    return launched(who, launch(a, shares_of(rows, q_heads, k ? k_heads : 0, cols), dtype, false, (hipStream_t)stream));
 }
 
 extern "C" uint64_t reft_heads_backward_workspace(uint64_t rows, uint64_t q_heads, uint64_t k_heads, uint64_t cols)
 {
     if (!rows || !cols || cols > kMaxHeadCols || rows > 0x7fffffff || q_heads > 65535 || k_heads > 65535) return 0;
-    return (uint64_t)heads_blocks(rows, q_heads + k_heads, cols) * 2 * cols * sizeof(float);
+    return (uint64_t)backward_blocks(shares_of(rows, q_heads, k_heads, cols)) * 2 * cols * sizeof(float);
 }
 
 extern "C" int reft_heads_backward(const reft_heads *dq_out, const reft_heads *dk_out, const reft_heads *q, uint64_t q_heads,
@@ -306,7 +455,8 @@ extern "C" int reft_heads_backward(const reft_heads *dq_out, const reft_heads *d
     NEED(dq || dk || sums || !rows, REFT_EINVAL, "%s: no output", who);
     NEED(lies(dq_weight, 4) && lies(dk_weight, 4), REFT_EINVAL, "%s: misaligned pointer", who);
     hipStream_t s = (hipStream_t)stream;
-    const uint32_t grid = rows ? heads_blocks(rows, q_heads + (k ? k_heads : 0), cols) : 0;
+    const Shares share = shares_of(rows, q_heads, k ? k_heads : 0, cols);
+    const uint32_t grid = backward_blocks(share);
     if (rows) {
         NEED(q->p && dq_out->p && (!k || (k->p && dk_out->p)) && (!dq || dq->p) && (!dk || dk->p), REFT_EINVAL, "%s: null pointer", who);
         NEED((!dq || apart(dq, rows, q_heads, cols)) && (!dk || apart(dk, rows, k_heads, cols)), REFT_ESIZE, "%s: heads overlap", who);
@@ -326,9 +476,7 @@ extern "C" int reft_heads_backward(const reft_heads *dq_out, const reft_heads *d
         a.side[0] = side_of(q, q_heads, q_weight, dq_out, dq);
         if (k) a.side[1] = side_of(k, k_heads, k_weight, dk_out, dk);
         a.part = sums ? (float *)workspace : nullptr;
-        e = dtype == REFT_F32    ? launch_backward<float>(a, grid, s)
-            : dtype == REFT_BF16 ? launch_backward<bf16>(a, grid, s)
-                                 : launch_backward<f16>(a, grid, s);
+        e = launch(a, share, dtype, true, s);
     }
     if (e == hipSuccess && sums) {
         k_heads_weights<<<(uint32_t)((2 * cols + 15) / 16), 256, 0, s>>>((const float *)workspace, grid, (uint32_t)cols, dq_weight, dk_weight);
