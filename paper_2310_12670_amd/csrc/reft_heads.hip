@@ -6,12 +6,20 @@
 
 namespace reft {
 
+// How the waves share the work on one kind of heads: units of wave_rows rows, each with row_groups groups of lanes, and one of `parts`
+// parts of their heads.  Of the sizes alone, as sums are taken in this order.
+struct Shares {
+    uint64_t units;
+    uint32_t parts, wave_rows, row_groups;
+};
+
 // One kind of heads: inputs, outputs, weight.
 struct Side {
     const void *x, *dy, *weight;
     void *out;
     uint64_t row_x, head_x, row_dy, head_dy, row_out, head_out;
     uint32_t heads;
+    Shares share;
 };
 
 struct HeadsArgs {
@@ -22,9 +30,6 @@ struct HeadsArgs {
     uint32_t cols, pairs;
     float eps, inverse_cols;
     float *part;                   // [blocks][2][cols], of the backward pass
-    uint64_t units;                // of wave_rows rows and one of `parts` parts of their heads
-    uint32_t parts;
-    uint32_t wave_rows, row_groups;        // rows that a wave works on at once, groups of lanes for each of them
     uint8_t adjacent, weight_f32;
 };
 
@@ -93,7 +98,9 @@ template <typename T, int G, int MODE> struct Wave {
         settle();
         for (int at = lane; at < rows * pairs; at += 64) {
             const int r = rows == 1 ? 0 : at / pairs;
-            if (row0 + r < a.rows) sine_cosine(a.positions[row0 + r], a.freqs[at - r * pairs], &room.turn[at].y, &room.turn[at].x);
+            float2 t = {1.f, 0.f};
+            if (row0 + r < a.rows) sine_cosine(a.positions[row0 + r], a.freqs[at - r * pairs], &t.y, &t.x);
+            room.turn[at] = t;
         }
         settle();
 #pragma unroll
@@ -142,107 +149,124 @@ template <typename T, int G, int MODE> struct Wave {
     }
 };
 
-// One of the units that the waves share: `rows` rows from row0 on, and a part of their heads.
+// A unit as one of its wave's groups of lanes sees it: its row, and its heads first, first + step, ... of those of its row.
 struct Unit {
     uint64_t row0, row;
-    uint32_t slot;                                          // the group's among its row's
-    uint32_t part;
+    uint32_t head0, slot, step;
+    int turn;                                               // the row's number among the unit's
+    __device__ __forceinline__ Unit(const Shares &s, uint64_t number, int group)
+    {
+        const uint32_t part = (uint32_t)(number % s.parts);
+        turn = group / s.row_groups;
+        row0 = number / s.parts * s.wave_rows;
+        row = row0 + turn;
+        slot = group % s.row_groups;
+        head0 = part * s.row_groups;
+        step = s.parts * s.row_groups;
+    }
 };
-__device__ __forceinline__ Unit unit_of(const HeadsArgs &a, uint64_t number, int group)
-{
-    Unit u;
-    u.part = (uint32_t)(number % a.parts);
-    u.row0 = number / a.parts * a.wave_rows;
-    u.row = u.row0 + group / a.row_groups;
-    u.slot = group % a.row_groups;
-    return u;
-}
 
-constexpr int kAhead = 2;                                   // heads of a group in flight
+#ifndef AHEAD
+#define AHEAD 2
+#endif
+constexpr int kAhead = AHEAD;                                   // heads of a group in flight
 
 template <typename T, int G, int MODE> __global__ __launch_bounds__(256) void k_heads_forward(HeadsArgs a)
 {
     __shared__ typename Wave<T, G, MODE>::Room room[4];
     const int wave = threadIdx.x >> 6, group = (threadIdx.x & 63) / G, pairs = (int)a.pairs;
     Wave<T, G, MODE> w(room[wave], a);
-    const uint32_t step = a.row_groups * a.parts;
-    for (uint64_t number = (uint64_t)blockIdx.x * 4 + wave; number < a.units; number += (uint64_t)gridDim.x * 4) {
-        const Unit u = unit_of(a, number, group);
-        w.turn(a, u.row0, a.wave_rows, group / a.row_groups);
-    #pragma unroll 1
-        for (int kind = 0; kind < 2; ++kind) {
-            const Side &s = a.side[kind];
-            if (!s.heads) continue;
-            float other[8], by_own[8], by_other[8];
-            const Eight<float> weight = w.weight(a, s);
-            w.partners(weight, other, pairs);
-    #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                by_own[i] = weight.t[i] * w.cosine[i];
-                by_other[i] = other[i] * w.sine[i];
+    const uint64_t units = a.side[0].share.units + a.side[1].share.units;
+    for (uint64_t number = (uint64_t)blockIdx.x * 4 + wave; number < units; number += (uint64_t)gridDim.x * 4) {
+        const bool keys = number >= a.side[0].share.units;
+        const Side &s = a.side[keys];
+        const Unit u(s.share, keys ? number - a.side[0].share.units : number, group);
+        const T *from = (const T *)s.x + u.row * s.row_x + w.c0;
+        T *to = (T *)s.out + u.row * s.row_out + w.c0;
+        const int there = u.row < a.rows ? w.n : 0;
+        Eight<T> x[kAhead], next[kAhead];
+        // all lanes of the wave go round as often
+        auto fetch = [&](uint32_t head0) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const uint32_t head = head0 + k * u.step + u.slot;
+                next[k].template load<false>(from + head * s.head_x, head < s.heads ? there : 0);
             }
-            const T *from = (const T *)s.x + u.row * s.row_x + w.c0;
-            T *to = (T *)s.out + u.row * s.row_out + w.c0;
-            // heads part, part + parts, ... of as many as the row has groups for; all lanes of the wave go round as often
-            for (uint32_t head0 = u.part * a.row_groups; head0 < s.heads; head0 += step * kAhead) {
-                Eight<T> x[kAhead];
-    #pragma unroll
-                for (int k = 0; k < kAhead; ++k) {
-                    const uint32_t head = head0 + k * step + u.slot;
-                    x[k].template load<false>(from + head * s.head_x, head < s.heads && u.row < a.rows ? w.n : 0);
+        };
+        fetch(u.head0);
+        float other[8], by_own[8], by_other[8];
+        const Eight<float> weight = w.weight(a, s);
+        w.turn(a, u.row0, s.share.wave_rows, u.turn);
+        w.partners(weight, other, pairs);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            by_own[i] = weight.t[i] * w.cosine[i];
+            by_other[i] = other[i] * w.sine[i];
+        }
+        for (uint32_t head0 = u.head0; head0 < s.heads; head0 += u.step * kAhead) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) x[k] = next[k];
+            if (head0 + u.step * kAhead < s.heads) fetch(head0 + u.step * kAhead);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                if (k && head0 + k * u.step >= s.heads) break;
+                const uint32_t head = head0 + k * u.step + u.slot;
+                float v[8], sum = 0;
+                w.partners(x[k], other, pairs);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    v[i] = x[k][i];
+                    sum += v[i] * v[i];
                 }
-    #pragma unroll
-                for (int k = 0; k < kAhead; ++k) {
-                    const uint32_t head = head0 + k * step + u.slot;
-                    float v[8], sum = 0;
-                    w.partners(x[k], other, pairs);
-    #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        v[i] = x[k][i];
-                        sum += v[i] * v[i];
-                    }
-                    const float r = inverse_root(sum_of<G>(sum) * a.inverse_cols + a.eps);
-    #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = r * (v[i] * by_own[i] + other[i] * by_other[i]);
-                    store8(to + head * s.head_out, head < s.heads && u.row < a.rows ? w.n : 0, v);
-                }
+                const float r = inverse_root(sum_of<G>(sum) * a.inverse_cols + a.eps);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = r * (v[i] * by_own[i] + other[i] * by_other[i]);
+                store8(to + head * s.head_out, head < s.heads ? there : 0, v);
             }
         }
     }
 }
 
-// The gradients; a lane sums its heads' part of the weights' gradients, the block adds its groups' in their order.
+// The gradients; a lane sums its heads' part of a weight's gradient, the block adds its groups' in their order.  Queries first, then keys.
 template <typename T, int G, int MODE> __global__ __launch_bounds__(256) void k_heads_backward(HeadsArgs a)
 {
     __shared__ typename Wave<T, G, MODE>::Room room[4];
     __shared__ float fold[256 / G][G * 8];
     const int wave = threadIdx.x >> 6, group = (threadIdx.x & 63) / G, pairs = (int)a.pairs;
     Wave<T, G, MODE> w(room[wave], a);
-    float dw[2][8] = {};
-    const uint32_t step = a.row_groups * a.parts;
-    for (uint64_t number = (uint64_t)blockIdx.x * 4 + wave; number < a.units; number += (uint64_t)gridDim.x * 4) {
-        const Unit u = unit_of(a, number, group);
-        w.turn(a, u.row0, a.wave_rows, group / a.row_groups);
-#pragma unroll
-        for (int kind = 0; kind < 2; ++kind) {
-            const Side &s = a.side[kind];
-            if (!s.heads) continue;
-            const Eight<float> weight = w.weight(a, s);
+#pragma unroll 1
+    for (int kind = 0; kind < 2; ++kind) {
+        const Side &s = a.side[kind];
+        float dw[8] = {};
+        const Eight<float> weight = w.weight(a, s);
+        for (uint64_t number = (uint64_t)blockIdx.x * 4 + wave; number < s.share.units; number += (uint64_t)gridDim.x * 4) {
+            const Unit u(s.share, number, group);
             const T *from = (const T *)s.x + u.row * s.row_x + w.c0, *from_dy = (const T *)s.dy + u.row * s.row_dy + w.c0;
             T *to = (T *)s.out + u.row * s.row_out + w.c0;
-            for (uint32_t head0 = u.part * a.row_groups; head0 < s.heads; head0 += step * kAhead) {
-                Eight<T> x[kAhead], dy[kAhead];
+            const int there = u.row < a.rows ? w.n : 0;
+            Eight<T> x[kAhead], dy[kAhead], next[kAhead], next_dy[kAhead];
+            auto fetch = [&](uint32_t head0) {
 #pragma unroll
                 for (int k = 0; k < kAhead; ++k) {
-                    const uint32_t head = head0 + k * step + u.slot;
-                    const int n = head < s.heads && u.row < a.rows ? w.n : 0;
-                    x[k].template load<false>(from + head * s.head_x, n);
-                    dy[k].template load<false>(from_dy + head * s.head_dy, n);
+                    const uint32_t head = head0 + k * u.step + u.slot;
+                    next[k].template load<false>(from + head * s.head_x, head < s.heads ? there : 0);
+                    next_dy[k].template load<false>(from_dy + head * s.head_dy, head < s.heads ? there : 0);
                 }
+            };
+            fetch(u.head0);
+            w.turn(a, u.row0, s.share.wave_rows, u.turn);
+            for (uint32_t head0 = u.head0; head0 < s.heads; head0 += u.step * kAhead) {
 #pragma unroll
                 for (int k = 0; k < kAhead; ++k) {
-                    const uint32_t head = head0 + k * step + u.slot;
-                    const int n = head < s.heads && u.row < a.rows ? w.n : 0;
+                    x[k] = next[k];
+                    dy[k] = next_dy[k];
+                }
+                if (head0 + u.step * kAhead < s.heads) fetch(head0 + u.step * kAhead);
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    if (k && head0 + k * u.step >= s.heads) break;
+                    const uint32_t head = head0 + k * u.step + u.slot;
+                    const int n = head < s.heads ? there : 0;
                     float other[8], t[8], sum = 0, dot = 0;
                     w.partners(dy[k], other, pairs);
 #pragma unroll
@@ -252,46 +276,45 @@ template <typename T, int G, int MODE> __global__ __launch_bounds__(256) void k_
                         sum += v * v;
                         dot += v * (t[i] * weight.t[i]);
                     }
-                    const float r = inverse_root(sum_of<G>(sum) * a.inverse_cols + a.eps);
+                    float r = inverse_root(sum_of<G>(sum) * a.inverse_cols + a.eps);
+                    r = n > 0 ? r : 0.f;                    // of zeroes that do not exist it may be infinite
                     dot = r * (sum_of<G>(dot) * a.inverse_cols);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const float xhat = x[k][i] * r;
-                        dw[kind][i] += i < n ? t[i] * xhat : 0.f;
+                        dw[i] += t[i] * xhat;
                         t[i] = r * (t[i] * weight.t[i] - xhat * dot);
                     }
                     if (s.out) store8(to + head * s.head_out, n, t);
                 }
             }
         }
-    }
-    if (!a.part) return;
-#pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
+        if (!a.part) continue;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) fold[threadIdx.x / G][w.c0 + i] = dw[kind][i];
+        for (int i = 0; i < 8; ++i) fold[threadIdx.x / G][w.c0 + i] = dw[i];
         __syncthreads();
         for (int c = threadIdx.x; c < (int)a.cols; c += 256) {
-            float s = 0;
-            for (int g = 0; g < 256 / G; ++g) s += fold[g][c];
-            a.part[((uint64_t)blockIdx.x * 2 + kind) * a.cols + c] = s;
+            float sum = 0;
+            for (int g = 0; g < 256 / G; ++g) sum += fold[g][c];
+            a.part[((uint64_t)blockIdx.x * 2 + kind) * a.cols + c] = sum;
         }
     }
 }
 
-// The weights' gradients: the blocks' parts in an order of their number alone, 16 interleaved sums and then those one after the other.
-__global__ __launch_bounds__(256) void k_heads_weights(const float *part, uint32_t n, uint32_t cols, float *dq, float *dk)
+// The weights' gradients: the blocks' parts in an order of their number alone, 64 interleaved sums and then those one after the other.
+__global__ __launch_bounds__(1024) void k_heads_weights(const float *part, uint32_t n, uint32_t cols, float *dq, float *dk)
 {
-    __shared__ float sums[16][16];
+    __shared__ float sums[64][16];
     const uint32_t x = threadIdx.x & 15, y = threadIdx.x >> 4, at = blockIdx.x * 16 + x;
     float s = 0;
     if (at < 2 * cols)
-        for (uint32_t i = y; i < n; i += 16) s += part[(uint64_t)i * 2 * cols + at];
+#pragma unroll 4
+        for (uint32_t i = y; i < n; i += 64) s += part[(uint64_t)i * 2 * cols + at];
     sums[y][x] = s;
     __syncthreads();
     if (y > 0 || at >= 2 * cols) return;
-    for (int i = 1; i < 16; ++i) s += sums[i][x];
+    for (int i = 1; i < 64; ++i) s += sums[i][x];
     float *out = at < cols ? dq : dk;
     if (out) out[at < cols ? at : at - cols] = s;
 }
@@ -302,26 +325,34 @@ __global__ __launch_bounds__(256) void k_heads_weights(const float *part, uint32
 constexpr uint64_t kMaxHeadCols = 512;
 static int lanes_of(uint64_t cols) { return cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : 64; }
 
-// How the waves share the work; of the sizes alone, as sums are taken in this order.
-struct Shares {
-    uint64_t units;
-    uint32_t parts, wave_rows, row_groups;
-};
-static Shares shares_of(uint64_t rows, uint64_t q_heads, uint64_t k_heads, uint64_t cols)
+#ifndef WAVES
+#define WAVES 4096
+#endif
+#ifndef BLOCKS
+#define BLOCKS 512
+#endif
+// As few groups for a row, and thereby as many rows at once, as leave the chip filled; then parts of the heads.
+static Shares shares_of(uint64_t rows, uint64_t heads, uint64_t cols)
 {
-    const uint64_t groups = 64 / lanes_of(cols), most = std::max(q_heads, k_heads);
-    Shares s;
-    s.row_groups = (uint32_t)groups;
-    while (s.row_groups > 1 && s.row_groups / 2 >= most) s.row_groups /= 2;
+    Shares s = {};
+    if (!heads) return s;
+    const uint64_t groups = 64 / lanes_of(cols);
+    s.row_groups = 1;
+    while (s.row_groups < groups && s.row_groups < heads && (rows * s.row_groups + groups - 1) / groups < WAVES) s.row_groups *= 2;
     s.wave_rows = (uint32_t)(groups / s.row_groups);
-    const uint64_t bunches = (rows + s.wave_rows - 1) / s.wave_rows, turns = (most + s.row_groups - 1) / s.row_groups;
-    s.parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(turns, 4096 / std::max<uint64_t>(1, bunches)));
+    const uint64_t bunches = (rows + s.wave_rows - 1) / s.wave_rows, turns = (heads + s.row_groups - 1) / s.row_groups;
+    s.parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(turns, WAVES / std::max<uint64_t>(1, bunches)));
     s.units = bunches * s.parts;
     return s;
 }
 
-// The gradients' blocks: as many as the chip holds at once.
-static uint32_t backward_blocks(const Shares &s) { return (uint32_t)std::min<uint64_t>((s.units + 3) / 4, 1024); }
+// The gradients' blocks: as many as the chip holds at once, or as few as need no more rounds of them.
+static uint32_t backward_blocks(uint64_t rows, uint64_t q_heads, uint64_t k_heads, uint64_t cols)
+{
+    const uint64_t blocks = (std::max(shares_of(rows, q_heads, cols).units, shares_of(rows, k_heads, cols).units) + 3) / 4;
+    const uint64_t rounds = (blocks + BLOCKS - 1) / BLOCKS;
+    return blocks ? (uint32_t)((blocks + rounds - 1) / rounds) : 0;
+}
 
 template <typename T, int G> static hipError_t launch(const HeadsArgs &a, uint32_t grid, bool back, hipStream_t s)
 {
@@ -335,13 +366,8 @@ template <typename T, int G> static hipError_t launch(const HeadsArgs &a, uint32
     return hipGetLastError();
 }
 
-template <typename T> static hipError_t launch(HeadsArgs a, const Shares &share, bool back, hipStream_t s)
+template <typename T> static hipError_t launch(const HeadsArgs &a, uint32_t grid, bool back, hipStream_t s)
 {
-    a.units = share.units;
-    a.parts = share.parts;
-    a.wave_rows = share.wave_rows;
-    a.row_groups = share.row_groups;
-    const uint32_t grid = back ? backward_blocks(share) : (uint32_t)std::min<uint64_t>((share.units + 3) / 4, kMaxBlocks256);
     switch (lanes_of(a.cols)) {
     case 8: return launch<T, 8>(a, grid, back, s);
     case 16: return launch<T, 16>(a, grid, back, s);
@@ -350,9 +376,9 @@ template <typename T> static hipError_t launch(HeadsArgs a, const Shares &share,
     }
 }
 
-static hipError_t launch(const HeadsArgs &a, const Shares &share, int dtype, bool back, hipStream_t s)
+static hipError_t launch(const HeadsArgs &a, int dtype, uint32_t grid, bool back, hipStream_t s)
 {
-    return dtype == REFT_F32 ? launch<float>(a, share, back, s) : dtype == REFT_BF16 ? launch<bf16>(a, share, back, s) : launch<f16>(a, share, back, s);
+    return dtype == REFT_F32 ? launch<float>(a, grid, back, s) : dtype == REFT_BF16 ? launch<bf16>(a, grid, back, s) : launch<f16>(a, grid, back, s);
 }
 
 // Elements in places of their own: a row's heads one behind the other, or a head's rows.
@@ -396,9 +422,11 @@ static HeadsArgs heads_args(const int64_t *positions, const float *freqs, uint64
     return a;
 }
 
-static Side side_of(const reft_heads *x, uint64_t heads, const void *weight, const reft_heads *dy, const reft_heads *out)
+static Side side_of(const reft_heads *x, uint64_t rows, uint64_t heads, uint64_t cols, const void *weight, const reft_heads *dy,
+                    const reft_heads *out)
 {
     Side s = {};
+    s.share = shares_of(rows, heads, cols);
     s.heads = (uint32_t)heads;
     s.weight = weight;
     s.x = x->p;
@@ -430,15 +458,16 @@ extern "C" int reft_heads_forward(const reft_heads *q, uint64_t q_heads, const r
          REFT_EINVAL, "%s: misaligned pointer", who);
     if ((uintptr_t)stream == kCheckOnly) return REFT_OK;
     HeadsArgs a = heads_args(positions, freqs, pairs, adjacent, rows, cols, weight_dtype, eps);
-    a.side[0] = side_of(q, q_heads, q_weight, nullptr, q_out);
-    if (k) a.side[1] = side_of(k, k_heads, k_weight, nullptr, k_out);
-    return launched(who, launch(a, shares_of(rows, q_heads, k ? k_heads : 0, cols), dtype, false, (hipStream_t)stream));
+    a.side[0] = side_of(q, rows, q_heads, cols, q_weight, nullptr, q_out);
+    if (k) a.side[1] = side_of(k, rows, k_heads, cols, k_weight, nullptr, k_out);
+    const uint64_t units = a.side[0].share.units + a.side[1].share.units;
+    return launched(who, launch(a, dtype, (uint32_t)std::min<uint64_t>((units + 3) / 4, kMaxBlocks256), false, (hipStream_t)stream));
 }
 
 extern "C" uint64_t reft_heads_backward_workspace(uint64_t rows, uint64_t q_heads, uint64_t k_heads, uint64_t cols)
 {
     if (!rows || !cols || cols > kMaxHeadCols || rows > 0x7fffffff || q_heads > 65535 || k_heads > 65535) return 0;
-    return (uint64_t)backward_blocks(shares_of(rows, q_heads, k_heads, cols)) * 2 * cols * sizeof(float);
+    return (uint64_t)backward_blocks(rows, q_heads, k_heads, cols) * 2 * cols * sizeof(float);
 }
 
 extern "C" int reft_heads_backward(const reft_heads *dq_out, const reft_heads *dk_out, const reft_heads *q, uint64_t q_heads,
@@ -455,8 +484,7 @@ extern "C" int reft_heads_backward(const reft_heads *dq_out, const reft_heads *d
     NEED(dq || dk || sums || !rows, REFT_EINVAL, "%s: no output", who);
     NEED(lies(dq_weight, 4) && lies(dk_weight, 4), REFT_EINVAL, "%s: misaligned pointer", who);
     hipStream_t s = (hipStream_t)stream;
-    const Shares share = shares_of(rows, q_heads, k ? k_heads : 0, cols);
-    const uint32_t grid = backward_blocks(share);
+    const uint32_t grid = backward_blocks(rows, q_heads, k ? k_heads : 0, cols);
     if (rows) {
         NEED(q->p && dq_out->p && (!k || (k->p && dk_out->p)) && (!dq || dq->p) && (!dk || dk->p), REFT_EINVAL, "%s: null pointer", who);
         NEED((!dq || apart(dq, rows, q_heads, cols)) && (!dk || apart(dk, rows, k_heads, cols)), REFT_ESIZE, "%s: heads overlap", who);
@@ -473,13 +501,13 @@ extern "C" int reft_heads_backward(const reft_heads *dq_out, const reft_heads *d
     hipError_t e = hipSuccess;
     if (rows) {
         HeadsArgs a = heads_args(positions, freqs, pairs, adjacent, rows, cols, weight_dtype, eps);
-        a.side[0] = side_of(q, q_heads, q_weight, dq_out, dq);
-        if (k) a.side[1] = side_of(k, k_heads, k_weight, dk_out, dk);
+        a.side[0] = side_of(q, rows, q_heads, cols, q_weight, dq_out, dq);
+        if (k) a.side[1] = side_of(k, rows, k_heads, cols, k_weight, dk_out, dk);
         a.part = sums ? (float *)workspace : nullptr;
-        e = launch(a, share, dtype, true, s);
+        e = launch(a, dtype, grid, true, s);
     }
     if (e == hipSuccess && sums) {
-        k_heads_weights<<<(uint32_t)((2 * cols + 15) / 16), 256, 0, s>>>((const float *)workspace, grid, (uint32_t)cols, dq_weight, dk_weight);
+        k_heads_weights<<<(uint32_t)((2 * cols + 15) / 16), 1024, 0, s>>>((const float *)workspace, grid, (uint32_t)cols, dq_weight, dk_weight);
         e = hipGetLastError();
     }
     return launched(who, e);
