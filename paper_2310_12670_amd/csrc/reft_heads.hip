@@ -10,7 +10,7 @@ namespace reft {
 // parts of their heads.  Of the sizes alone, as sums are taken in this order.
 struct Shares {
     uint64_t units;
-    uint32_t parts, wave_rows, row_groups;
+    uint32_t parts, wave_rows, row_groups;                  // the last two powers of two
 };
 
 // One kind of heads: inputs, outputs, weight.
@@ -30,7 +30,7 @@ struct HeadsArgs {
     uint32_t cols, pairs;
     float eps, inverse_cols;
     float *part;                   // [blocks][2][cols], of the backward pass
-    uint8_t adjacent, weight_f32;
+    uint8_t adjacent, weight_f32, lines;    // lines: heads lie on cache lines
 };
 
 // Sine and cosine of position * frequency.  The angle is a product in 64 bits; the multiple of pi / 2 next to it leaves in two parts (Cody
@@ -68,52 +68,78 @@ __device__ __forceinline__ float inverse_root(float v)
 // How a lane comes to the values that its eight columns turn with: they are its own neighbours, all another lane's, or anyone's.
 enum { kAdjacent, kLane, kAny };
 
-// A wave works on `rows` rows at once, each with 64 / G / rows of its groups of G lanes; a group's lanes hold eight columns of a head each.
+// A pointer to memory of the GPU, for the compiler to know: one that was chosen among others it would take for any.
+template <typename T> __device__ __forceinline__ T *global(T *p) { return (T *)(__attribute__((address_space(1))) T *)p; }
+
+// The side with everything the same in all lanes.
+__device__ __forceinline__ Side side_at(const HeadsArgs &a, bool keys)
+{
+    Side s = keys ? a.side[1] : a.side[0];
+    s.x = global(s.x);
+    s.dy = global(s.dy);
+    s.weight = global(s.weight);
+    s.out = global(s.out);
+    return s;
+}
+
+// Eight values of a head, or none; WHOLE: there are no heads' ends between; past: not kept in the caches.
+template <bool WHOLE, typename T> __device__ __forceinline__ void load_part(Eight<T> &e, const T *p, int n, bool past = false)
+{
+    if (past) e.template load<true>(p, WHOLE ? n > 0 ? 8 : 0 : n);
+    else e.template load<false>(p, WHOLE ? n > 0 ? 8 : 0 : n);
+}
+template <bool WHOLE, typename T> __device__ __forceinline__ void store_part(T *p, int n, const float v[8])
+{
+    if (!WHOLE) store8(p, n, v);
+    else if (n > 0) store8(p, 8, v);
+}
+
+// A wave works on several rows at once, each with some of its 64 / G groups of G lanes; a group's lanes hold eight columns of a head each.
 // Sines and cosines are computed once a row, one pair a lane and turn, and pass through the wave's own part of LDS, as do the partners of kAny.
-template <typename T, int G, int MODE> struct Wave {
-    static constexpr int kGroups = 64 / G;
+template <typename T, int G, int MODE, bool WHOLE> struct Wave {
     struct Room {
-        float2 turn[4 * 64];                               // rows x pairs <= 64 / G x 4 G
+        float2 turn[4 * 64];                               // of a row 4 G pairs, those that do not turn with one and zero
         float values[MODE == kAny ? 64 * 8 : 1];
     };
     Room &room;
-    int c0, n, first;                                       // the lane's columns, the partner lane or where its group's values lie
-    int pair[8];
+    const int lane, pairs;
+    int c0, n, partner, pair0;                              // the lane's columns, their partners' lane (kAny: its group's place), the first one's pair
+    bool lower;                                             // kLane: its columns come first in their pairs
     float cosine[8], sine[8];                               // of its columns; the sine with the partner's sign
 
-    __device__ __forceinline__ Wave(Room &room, const HeadsArgs &a) : room(room)
+    __device__ __forceinline__ Wave(Room &room, const HeadsArgs &a) : room(room), lane(threadIdx.x & 63), pairs((int)a.pairs)
     {
-        const int lane = threadIdx.x & 63, pairs = (int)a.pairs;
         c0 = lane % G * 8;
         n = (int)a.cols - c0;
-        if (MODE == kLane) first = c0 >= 2 * pairs ? lane : c0 < pairs ? lane + pairs / 8 : lane - pairs / 8;
-        if (MODE == kAny) first = lane / G * G * 8;
+        lower = c0 < pairs;
+        const bool turns = c0 < 2 * pairs;
+        partner = MODE == kAny ? lane / G * G * 8 : !turns ? lane : lower ? lane + pairs / 8 : lane - pairs / 8;
+        pair0 = MODE == kAdjacent ? c0 / 2 : !turns ? pairs : lower ? c0 : c0 - pairs;
     }
     // The wave's other lanes see what this one has written; nothing moves across.
     __device__ __forceinline__ static void settle() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
     __device__ __forceinline__ void turn(const HeadsArgs &a, uint64_t row0, int rows, int row)
     {
-        const int lane = threadIdx.x & 63, pairs = (int)a.pairs;
         settle();
-        for (int at = lane; at < rows * pairs; at += 64) {
-            const int r = rows == 1 ? 0 : at / pairs;
+        for (int at = lane; at < rows * 4 * G; at += 64) {
+            const int r = at / (4 * G), pair = at % (4 * G);
             float2 t = {1.f, 0.f};
-            if (row0 + r < a.rows) sine_cosine(a.positions[row0 + r], a.freqs[at - r * pairs], &t.y, &t.x);
+            if (pair < pairs && row0 + r < a.rows) sine_cosine(a.positions[row0 + r], a.freqs[pair], &t.y, &t.x);
             room.turn[at] = t;
         }
         settle();
+        const float2 *from = room.turn + row * 4 * G;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int c = c0 + i;
-            const bool turns = c < 2 * pairs, lower = MODE == kAdjacent ? !(i & 1) : c < pairs;
-            const float2 t = turns ? room.turn[row * pairs + (MODE == kAdjacent ? c / 2 : lower ? c : c - pairs)] : float2{1.f, 0.f};
+            const float2 t = from[MODE == kAdjacent ? pair0 + i / 2 : MODE == kLane ? pair0 + i : c >= 2 * pairs ? pairs : c < pairs ? c : c - pairs];
             cosine[i] = t.x;
-            sine[i] = lower ? -t.y : t.y;
+            sine[i] = (MODE == kAdjacent ? !(i & 1) : MODE == kLane ? lower : c < pairs) ? -t.y : t.y;
         }
     }
     // The values of the partners' columns.
-    template <typename E> __device__ __forceinline__ void partners(const Eight<E> &x, float v[8], int pairs)
+    template <typename E> __device__ __forceinline__ void partners(const Eight<E> &x, float v[8])
     {
         if constexpr (MODE == kAdjacent) {
 #pragma unroll
@@ -123,96 +149,98 @@ template <typename T, int G, int MODE> struct Wave {
 #pragma unroll
             for (int i = 0; i < (int)sizeof(E) / 2; ++i)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) y.w[i][k] = (uint32_t)__shfl((int)x.w[i][k], first);
+                for (int k = 0; k < 4; ++k) y.w[i][k] = (uint32_t)__shfl((int)x.w[i][k], partner);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = y[i];
         } else {
             settle();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) room.values[first + c0 + i] = x[i];
+            for (int i = 0; i < 8; ++i) room.values[partner + c0 + i] = x[i];
             settle();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int c = c0 + i;
-                v[i] = room.values[first + (c >= 2 * pairs ? c : c < pairs ? c + pairs : c - pairs)];
+                v[i] = room.values[partner + (c >= 2 * pairs ? c : c < pairs ? c + pairs : c - pairs)];
             }
         }
     }
     __device__ __forceinline__ Eight<float> weight(const HeadsArgs &a, const Side &s)
     {
         Eight<float> w;
-        float v[8];
-        load8_of<T>(s.weight, a.weight_f32, c0, s.weight ? n : 0, v);
+        if (!s.weight) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w.t[i] = s.weight ? v[i] : 1.f;
+            for (int i = 0; i < 8; ++i) w.t[i] = 1.f;
+        } else if (a.weight_f32) {
+            load_part<WHOLE>(w, (const float *)s.weight + c0, n);
+        } else {
+            Eight<T> e;
+            load_part<WHOLE>(e, (const T *)s.weight + c0, n);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w.t[i] = e[i];
+        }
         return w;
     }
 };
 
-// A unit as one of its wave's groups of lanes sees it: its row, and its heads first, first + step, ... of those of its row.
+// A unit as one of its wave's groups of lanes sees it: its row, and its heads head0 + slot, head0 + slot + step, ... of those of its row.
 struct Unit {
     uint64_t row0, row;
     uint32_t head0, slot, step;
     int turn;                                               // the row's number among the unit's
-    __device__ __forceinline__ Unit(const Shares &s, uint64_t number, int group)
+    __device__ __forceinline__ Unit(const Shares &s, uint32_t number, int group)
     {
-        const uint32_t part = (uint32_t)(number % s.parts);
-        turn = group / s.row_groups;
-        row0 = number / s.parts * s.wave_rows;
+        const uint32_t bunch = s.parts == 1 ? number : number / s.parts;
+        slot = group & (s.row_groups - 1);
+        turn = (group - (int)slot) >> __builtin_ctz(s.row_groups);
+        row0 = (uint64_t)bunch * s.wave_rows;
         row = row0 + turn;
-        slot = group % s.row_groups;
-        head0 = part * s.row_groups;
+        head0 = (number - bunch * s.parts) * s.row_groups;
         step = s.parts * s.row_groups;
     }
 };
 
-#ifndef AHEAD
-#define AHEAD 2
-#endif
-constexpr int kAhead = AHEAD;                                   // heads of a group in flight
-
-template <typename T, int G, int MODE> __global__ __launch_bounds__(256) void k_heads_forward(HeadsArgs a)
+template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(256) void k_heads_forward(HeadsArgs a)
 {
-    __shared__ typename Wave<T, G, MODE>::Room room[4];
-    const int wave = threadIdx.x >> 6, group = (threadIdx.x & 63) / G, pairs = (int)a.pairs;
-    Wave<T, G, MODE> w(room[wave], a);
+    typedef Wave<T, G, MODE, WHOLE> W;
+    __shared__ typename W::Room room[4];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = (threadIdx.x & 63) / G;
+    constexpr int kAhead = 8 / sizeof(T);                   // heads of a group in flight
+    W w(room[wave], a);
     const uint64_t units = a.side[0].share.units + a.side[1].share.units;
     for (uint64_t number = (uint64_t)blockIdx.x * 4 + wave; number < units; number += (uint64_t)gridDim.x * 4) {
         const bool keys = number >= a.side[0].share.units;
-        const Side &s = a.side[keys];
-        const Unit u(s.share, keys ? number - a.side[0].share.units : number, group);
-        const T *from = (const T *)s.x + u.row * s.row_x + w.c0;
-        T *to = (T *)s.out + u.row * s.row_out + w.c0;
+        const Side s = side_at(a, keys);
+        const Unit u(s.share, (uint32_t)(keys ? number - a.side[0].share.units : number), group);
+        const T *from = (const T *)s.x + u.row * s.row_x + (uint64_t)(u.head0 + u.slot) * s.head_x + w.c0;
+        T *to = (T *)s.out + u.row * s.row_out + (uint64_t)(u.head0 + u.slot) * s.head_out + w.c0;
+        const uint64_t step_x = u.step * s.head_x, step_out = u.step * s.head_out;
         const int there = u.row < a.rows ? w.n : 0;
         Eight<T> x[kAhead], next[kAhead];
         // all lanes of the wave go round as often
         auto fetch = [&](uint32_t head0) {
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                const uint32_t head = head0 + k * u.step + u.slot;
-                next[k].template load<false>(from + head * s.head_x, head < s.heads ? there : 0);
-            }
+            for (int k = 0; k < kAhead; ++k) load_part<WHOLE>(next[k], from + k * step_x, head0 + k * u.step + u.slot < s.heads ? there : 0, a.lines);
+            from += kAhead * step_x;
         };
         fetch(u.head0);
         float other[8], by_own[8], by_other[8];
         const Eight<float> weight = w.weight(a, s);
         w.turn(a, u.row0, s.share.wave_rows, u.turn);
-        w.partners(weight, other, pairs);
+        w.partners(weight, other);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             by_own[i] = weight.t[i] * w.cosine[i];
             by_other[i] = other[i] * w.sine[i];
         }
-        for (uint32_t head0 = u.head0; head0 < s.heads; head0 += u.step * kAhead) {
+        for (uint32_t head0 = u.head0; head0 < s.heads; head0 += u.step * kAhead, to += kAhead * step_out) {
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) x[k] = next[k];
             if (head0 + u.step * kAhead < s.heads) fetch(head0 + u.step * kAhead);
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
                 if (k && head0 + k * u.step >= s.heads) break;
-                const uint32_t head = head0 + k * u.step + u.slot;
                 float v[8], sum = 0;
-                w.partners(x[k], other, pairs);
+                w.partners(x[k], other);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     v[i] = x[k][i];
@@ -221,41 +249,47 @@ template <typename T, int G, int MODE> __global__ __launch_bounds__(256) void k_
                 const float r = inverse_root(sum_of<G>(sum) * a.inverse_cols + a.eps);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = r * (v[i] * by_own[i] + other[i] * by_other[i]);
-                store8(to + head * s.head_out, head < s.heads ? there : 0, v);
+                store_part<WHOLE>(to + k * step_out, head0 + k * u.step + u.slot < s.heads ? there : 0, v);
             }
         }
     }
 }
 
 // The gradients; a lane sums its heads' part of a weight's gradient, the block adds its groups' in their order.  Queries first, then keys.
-template <typename T, int G, int MODE> __global__ __launch_bounds__(256) void k_heads_backward(HeadsArgs a)
+template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(256) void k_heads_backward(HeadsArgs a)
 {
-    __shared__ typename Wave<T, G, MODE>::Room room[4];
+    typedef Wave<T, G, MODE, WHOLE> W;
+    __shared__ typename W::Room room[4];
     __shared__ float fold[256 / G][G * 8];
-    const int wave = threadIdx.x >> 6, group = (threadIdx.x & 63) / G, pairs = (int)a.pairs;
-    Wave<T, G, MODE> w(room[wave], a);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = (threadIdx.x & 63) / G;
+    constexpr int kAhead = 8 / sizeof(T);                   // heads of a group in flight
+    W w(room[wave], a);
 #pragma unroll 1
     for (int kind = 0; kind < 2; ++kind) {
-        const Side &s = a.side[kind];
+        const Side s = side_at(a, kind);
         float dw[8] = {};
         const Eight<float> weight = w.weight(a, s);
         for (uint64_t number = (uint64_t)blockIdx.x * 4 + wave; number < s.share.units; number += (uint64_t)gridDim.x * 4) {
-            const Unit u(s.share, number, group);
-            const T *from = (const T *)s.x + u.row * s.row_x + w.c0, *from_dy = (const T *)s.dy + u.row * s.row_dy + w.c0;
-            T *to = (T *)s.out + u.row * s.row_out + w.c0;
+            const Unit u(s.share, (uint32_t)number, group);
+            const T *from = (const T *)s.x + u.row * s.row_x + (uint64_t)(u.head0 + u.slot) * s.head_x + w.c0;
+            const T *from_dy = (const T *)s.dy + u.row * s.row_dy + (uint64_t)(u.head0 + u.slot) * s.head_dy + w.c0;
+            T *to = (T *)s.out + u.row * s.row_out + (uint64_t)(u.head0 + u.slot) * s.head_out + w.c0;
+            const uint64_t step_x = u.step * s.head_x, step_dy = u.step * s.head_dy, step_out = u.step * s.head_out;
             const int there = u.row < a.rows ? w.n : 0;
             Eight<T> x[kAhead], dy[kAhead], next[kAhead], next_dy[kAhead];
             auto fetch = [&](uint32_t head0) {
 #pragma unroll
                 for (int k = 0; k < kAhead; ++k) {
-                    const uint32_t head = head0 + k * u.step + u.slot;
-                    next[k].template load<false>(from + head * s.head_x, head < s.heads ? there : 0);
-                    next_dy[k].template load<false>(from_dy + head * s.head_dy, head < s.heads ? there : 0);
+                    const int n = head0 + k * u.step + u.slot < s.heads ? there : 0;
+                    load_part<WHOLE>(next[k], from + k * step_x, n, a.lines);
+                    load_part<WHOLE>(next_dy[k], from_dy + k * step_dy, n, a.lines);
                 }
+                from += kAhead * step_x;
+                from_dy += kAhead * step_dy;
             };
             fetch(u.head0);
             w.turn(a, u.row0, s.share.wave_rows, u.turn);
-            for (uint32_t head0 = u.head0; head0 < s.heads; head0 += u.step * kAhead) {
+            for (uint32_t head0 = u.head0; head0 < s.heads; head0 += u.step * kAhead, to += kAhead * step_out) {
 #pragma unroll
                 for (int k = 0; k < kAhead; ++k) {
                     x[k] = next[k];
@@ -265,10 +299,9 @@ template <typename T, int G, int MODE> __global__ __launch_bounds__(256) void k_
 #pragma unroll
                 for (int k = 0; k < kAhead; ++k) {
                     if (k && head0 + k * u.step >= s.heads) break;
-                    const uint32_t head = head0 + k * u.step + u.slot;
-                    const int n = head < s.heads ? there : 0;
+                    const int n = head0 + k * u.step + u.slot < s.heads ? there : 0;
                     float other[8], t[8], sum = 0, dot = 0;
-                    w.partners(dy[k], other, pairs);
+                    w.partners(dy[k], other);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const float v = x[k][i];
@@ -285,7 +318,7 @@ template <typename T, int G, int MODE> __global__ __launch_bounds__(256) void k_
                         dw[i] += t[i] * xhat;
                         t[i] = r * (t[i] * weight.t[i] - xhat * dot);
                     }
-                    if (s.out) store8(to + head * s.head_out, n, t);
+                    if (s.out) store_part<WHOLE>(to + k * step_out, n, t);
                 }
             }
         }
@@ -325,23 +358,20 @@ __global__ __launch_bounds__(1024) void k_heads_weights(const float *part, uint3
 constexpr uint64_t kMaxHeadCols = 512;
 static int lanes_of(uint64_t cols) { return cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : 64; }
 
-#ifndef WAVES
-#define WAVES 4096
-#endif
-#ifndef BLOCKS
-#define BLOCKS 512
-#endif
-// As few groups for a row, and thereby as many rows at once, as leave the chip filled; then parts of the heads.
+constexpr uint64_t kWaves = 4096, kTurns = 4, kBackwardBlocks = 512;
+// Groups of lanes for a row: as many as leave each kTurns heads (a row's heads lie together more often than a head's rows), more
+// where that fills the chip; then parts of the heads, for the same.
 static Shares shares_of(uint64_t rows, uint64_t heads, uint64_t cols)
 {
     Shares s = {};
     if (!heads) return s;
     const uint64_t groups = 64 / lanes_of(cols);
     s.row_groups = 1;
-    while (s.row_groups < groups && s.row_groups < heads && (rows * s.row_groups + groups - 1) / groups < WAVES) s.row_groups *= 2;
+    while (s.row_groups < groups && (s.row_groups * 2 * kTurns <= heads || (s.row_groups < heads && (rows * s.row_groups + groups - 1) / groups < kWaves)))
+        s.row_groups *= 2;
     s.wave_rows = (uint32_t)(groups / s.row_groups);
     const uint64_t bunches = (rows + s.wave_rows - 1) / s.wave_rows, turns = (heads + s.row_groups - 1) / s.row_groups;
-    s.parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(turns, WAVES / std::max<uint64_t>(1, bunches)));
+    s.parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(turns, kWaves / std::max<uint64_t>(1, bunches)));
     s.units = bunches * s.parts;
     return s;
 }
@@ -350,19 +380,23 @@ static Shares shares_of(uint64_t rows, uint64_t heads, uint64_t cols)
 static uint32_t backward_blocks(uint64_t rows, uint64_t q_heads, uint64_t k_heads, uint64_t cols)
 {
     const uint64_t blocks = (std::max(shares_of(rows, q_heads, cols).units, shares_of(rows, k_heads, cols).units) + 3) / 4;
-    const uint64_t rounds = (blocks + BLOCKS - 1) / BLOCKS;
+    const uint64_t rounds = (blocks + kBackwardBlocks - 1) / kBackwardBlocks;
     return blocks ? (uint32_t)((blocks + rounds - 1) / rounds) : 0;
+}
+
+template <typename T, int G, int MODE, bool WHOLE> static void launch(const HeadsArgs &a, uint32_t grid, bool back, hipStream_t s)
+{
+    if (back) k_heads_backward<T, G, MODE, WHOLE><<<grid, 256, 0, s>>>(a);
+    else k_heads_forward<T, G, MODE, WHOLE><<<grid, 256, 0, s>>>(a);
 }
 
 template <typename T, int G> static hipError_t launch(const HeadsArgs &a, uint32_t grid, bool back, hipStream_t s)
 {
-    const int mode = a.adjacent ? kAdjacent : a.pairs % 8 ? kAny : kLane;
-    if (!back && mode == kAdjacent) k_heads_forward<T, G, kAdjacent><<<grid, 256, 0, s>>>(a);
-    else if (!back && mode == kLane) k_heads_forward<T, G, kLane><<<grid, 256, 0, s>>>(a);
-    else if (!back) k_heads_forward<T, G, kAny><<<grid, 256, 0, s>>>(a);
-    else if (mode == kAdjacent) k_heads_backward<T, G, kAdjacent><<<grid, 256, 0, s>>>(a);
-    else if (mode == kLane) k_heads_backward<T, G, kLane><<<grid, 256, 0, s>>>(a);
-    else k_heads_backward<T, G, kAny><<<grid, 256, 0, s>>>(a);
+    const bool whole = a.cols % 8 == 0;
+    if (a.adjacent && whole) launch<T, G, kAdjacent, true>(a, grid, back, s);
+    else if (a.adjacent) launch<T, G, kAdjacent, false>(a, grid, back, s);
+    else if (a.pairs % 8 == 0 && whole) launch<T, G, kLane, true>(a, grid, back, s);
+    else launch<T, G, kAny, false>(a, grid, back, s);
     return hipGetLastError();
 }
 
@@ -404,6 +438,13 @@ static int check_heads(const char *who, uint64_t q_heads, const reft_heads *k, u
     NEED(!rows || !pairs || (positions && freqs), REFT_EINVAL, "%s: pairs without positions or freqs", who);
     NEED(lies(positions, 8) && lies(freqs, 4), REFT_EINVAL, "%s: misaligned pointer", who);
     return REFT_OK;
+}
+
+// Heads on cache lines, which no two of them share, are read past the L2.
+static bool heads_on_lines(const reft_heads *x, uint64_t cols, int dtype)
+{
+    const uint64_t size = size_of(dtype);
+    return !x || (on_lines(x->p, x->row * size) && x->head * size % 128 == 0 && cols * size % 128 == 0);
 }
 
 static HeadsArgs heads_args(const int64_t *positions, const float *freqs, uint64_t pairs, int adjacent, uint64_t rows, uint64_t cols,
@@ -460,6 +501,7 @@ extern "C" int reft_heads_forward(const reft_heads *q, uint64_t q_heads, const r
     HeadsArgs a = heads_args(positions, freqs, pairs, adjacent, rows, cols, weight_dtype, eps);
     a.side[0] = side_of(q, rows, q_heads, cols, q_weight, nullptr, q_out);
     if (k) a.side[1] = side_of(k, rows, k_heads, cols, k_weight, nullptr, k_out);
+    a.lines = heads_on_lines(q, cols, dtype) && heads_on_lines(k, cols, dtype);
     const uint64_t units = a.side[0].share.units + a.side[1].share.units;
     return launched(who, launch(a, dtype, (uint32_t)std::min<uint64_t>((units + 3) / 4, kMaxBlocks256), false, (hipStream_t)stream));
 }
@@ -504,6 +546,8 @@ extern "C" int reft_heads_backward(const reft_heads *dq_out, const reft_heads *d
         a.side[0] = side_of(q, rows, q_heads, cols, q_weight, dq_out, dq);
         if (k) a.side[1] = side_of(k, rows, k_heads, cols, k_weight, dk_out, dk);
         a.part = sums ? (float *)workspace : nullptr;
+        a.lines = heads_on_lines(q, cols, dtype) && heads_on_lines(k, cols, dtype) && heads_on_lines(dq_out, cols, dtype) &&
+                  heads_on_lines(dk_out, cols, dtype);
         e = launch(a, dtype, grid, true, s);
     }
     if (e == hipSuccess && sums) {
