@@ -630,7 +630,7 @@ int reft_gate_forward(const void *g, uint64_t ld_g, const void *u, uint64_t ld_u
  * as dg and du in dtype; in 8 bits (grad_format) as dg8 and du8, for the product that gives the gradient of the products' inputs, and transposed, as
  * dg8_t and du8_t ([cols][rows], scales per 128 rows), for that of their weights; and y = act(g) u, transposed, as y8_t in y_format, for the gradient
  * of the weights that y is multiplied by.  Outputs are each left out where NULL.  dg or du may be dy (with the same ld).
- * rows, cols < 2^31, ceil(rows / 128) ceil(cols / 128) < 2^23.
+ * rows, cols < 2^31, ceil(rows / 128) ceil(cols / 128) < 2^22.
  */
 int reft_gate_backward(const void *dy, uint64_t ld_dy, const reft_eight *g8, const reft_eight *u8, int kept_format,
                        uint64_t rows, uint64_t cols, int dtype, int act, void *dg, uint64_t ld_dg, void *du, uint64_t ld_du,

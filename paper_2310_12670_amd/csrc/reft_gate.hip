@@ -2,6 +2,8 @@
 // transpose of what is kept.  Kernels and their entry points (see include/reft.h).
 #include "reft_calls.hpp"
 
+#include <algorithm>
+
 namespace reft {
 
 struct EightIn {
@@ -58,6 +60,73 @@ template <int ACT> __device__ __forceinline__ void act(float g, float *a, float 
 }
 
 // ------------------------------------------------------------------------------------------------
+// 8 bits
+// ------------------------------------------------------------------------------------------------
+// The conversions of fp32 from and to 8 bits take a power of two along, as a float of its exponent: 2^(e - 127) is e << 23, and with 255 all
+// values are NaN.  To nearest even, as by a product with the power and a conversion (both compared over all bytes and powers).
+__device__ __forceinline__ float power_of(uint32_t e) { return __uint_as_float(e << 23); }
+
+// Eight neighbouring 8-bit values; those that do not exist are zeroes.
+__device__ __forceinline__ w32x2 load8_bytes(const uint8_t *p, int n)
+{
+    w32x2 w = {0, 0};
+    if (n >= 8) return *(const w32x2_any *)p;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) {
+            if (i < 4) w.x |= (uint32_t)p[i] << (8 * i);
+            else w.y |= (uint32_t)p[i] << (8 * (i - 4));
+        }
+    return w;
+}
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
+template <bool HIGH> __device__ __forceinline__ f32x2 widen2(uint32_t w, bool e5m2, float power)
+{
+    return e5m2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_bf8(w, power, HIGH) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, power, HIGH);
+}
+
+__device__ __forceinline__ void widen4(uint32_t w, bool e5m2, float power, float v[4])
+{
+    const f32x2 lo = widen2<false>(w, e5m2, power), hi = widen2<true>(w, e5m2, power);
+    v[0] = lo.x, v[1] = lo.y, v[2] = hi.x, v[3] = hi.y;
+}
+
+// Four values in 8 bits.
+__device__ __forceinline__ uint32_t to_four(float v0, float v1, float v2, float v3, float power, bool e5m2)
+{
+    s16x2 w = {0, 0};
+    if (e5m2) {
+        w = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(w, v0, v1, power, false);
+        w = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(w, v2, v3, power, true);
+    } else {
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v0, v1, power, false);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v2, v3, power, true);
+    }
+    return __builtin_bit_cast(uint32_t, w);
+}
+
+__device__ __forceinline__ w32x2 to_eight_scaled(const float v[8], float power, bool e5m2)
+{
+    w32x2 w;
+    w.x = to_four(v[0], v[1], v[2], v[3], power, e5m2);
+    w.y = to_four(v[4], v[5], v[6], v[7], power, e5m2);
+    return w;
+}
+
+// The larger of a magnitude and two values'; a NaN stays one, as bits larger than all numbers.
+__device__ __forceinline__ float larger(float most, float a, float b)
+{
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(most, fabsf(a)), fabsf(b));
+}
+__device__ __forceinline__ uint32_t largest_of(const float v[8])
+{
+    return magnitude(larger(larger(larger(larger(0.f, v[0], v[1]), v[2], v[3]), v[4], v[5]), v[6], v[7]));
+}
+
+// ------------------------------------------------------------------------------------------------
 // forward
 // ------------------------------------------------------------------------------------------------
 struct GateForward {
@@ -72,11 +141,8 @@ struct GateForward {
 // Eight of a row's values in 8 bits with the power of two of the 16 lanes' 128.
 __device__ __forceinline__ void leave_row(const EightOut &o, const float v[8], uint64_t row, uint64_t c, int n, bool e5m2)
 {
-    uint32_t most = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[i]));
-    const uint32_t e = scale_of(max_of_16(most), top_of(e5m2));
-    store8_bytes<true>(o.q + row * o.ld + c, n, to_eight(v, inverse_of(e), e5m2));
+    const uint32_t e = scale_of(max_of_16(largest_of(v)), top_of(e5m2));
+    store8_bytes<true>(o.q + row * o.ld + c, n, to_eight_scaled(v, power_of(e), e5m2));
     if ((threadIdx.x & 15) == 0) o.scales[(c / 512 * o.ld_s + row) * 4 + c / 128 % 4] = n ? (uint8_t)e : 127;
 }
 
@@ -123,135 +189,125 @@ __device__ __forceinline__ Tile tile_of(uint32_t number, uint64_t rows, uint64_t
     return t;
 }
 
-// The factor that a scale byte stands for: 2^(e - 127), and a NaN for 255.
-__device__ __forceinline__ float factor_of(uint32_t e)
-{
-    return __uint_as_float(e == 255 ? 0x7fc00000u : e ? e << 23 : 0x00400000u);
-}
+constexpr int kTileThreads = 512, kRows = 4;               // and rows of a thread
 
-// Eight neighbouring 8-bit values; those that do not exist are zeroes.
-__device__ __forceinline__ w32x2 load8_bytes(const uint8_t *p, int n)
-{
-    w32x2 w = {0, 0};
-    if (n >= 8) return *(const w32x2_any *)p;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < n) {
-            if (i < 4) w.x |= (uint32_t)p[i] << (8 * i);
-            else w.y |= (uint32_t)p[i] << (8 * (i - 4));
-        }
-    return w;
-}
-
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ void widen8(w32x2 w, bool e5m2, float factor, float v[8])
-{
-    f32x2 p[4];
-    if (e5m2) {
-        p[0] = __builtin_amdgcn_cvt_pk_f32_bf8((int)w.x, false);
-        p[1] = __builtin_amdgcn_cvt_pk_f32_bf8((int)w.x, true);
-        p[2] = __builtin_amdgcn_cvt_pk_f32_bf8((int)w.y, false);
-        p[3] = __builtin_amdgcn_cvt_pk_f32_bf8((int)w.y, true);
-    } else {
-        p[0] = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.x, false);
-        p[1] = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.x, true);
-        p[2] = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.y, false);
-        p[3] = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.y, true);
+// A thread's place in the tile: eight columns of kRows rows, of which its wave, which is the same in all lanes, has 4 kRows.  An element's
+// address is one of the wave's and an offset of O bits in it.
+template <typename O> struct Place {
+    int lane, wave, c, r;
+    __device__ __forceinline__ Place()
+    {
+        lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));                      // what follows from it is computed anew for each tile, and not held
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        c = (lane & 15) * 8;
+        r = wave * 4 * kRows + (lane >> 4) * kRows;
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = p[i].x * factor;
-        v[2 * i + 1] = p[i].y * factor;
+    // Row i of the thread's in a matrix of rows (x), scales of rows (s: words).
+    template <typename E> __device__ __forceinline__ E *in(E *x, uint64_t ld, const Tile &t, int i) const
+    {
+        return x + (t.row0 + wave * 4 * kRows + i) * ld + t.col0 + ((O)(lane >> 4) * kRows * (O)ld + c);
     }
-}
-
-// Four values in 8 bits, to nearest even.
-__device__ __forceinline__ uint32_t to_four(const float v[4], float inv, bool e5m2)
-{
-    int w = 0;
-    if (e5m2) {
-        w = __builtin_amdgcn_cvt_pk_bf8_f32(v[0] * inv, v[1] * inv, w, false);
-        w = __builtin_amdgcn_cvt_pk_bf8_f32(v[2] * inv, v[3] * inv, w, true);
-    } else {
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inv, v[1] * inv, w, false);
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inv, v[3] * inv, w, true);
+    template <typename E> __device__ __forceinline__ E *scale(E *s, uint64_t ld_s, const Tile &t, int i) const
+    {
+        return s + ((t.along / 4 * ld_s + t.row0 + wave * 4 * kRows + i) * 4 + t.along % 4) + (lane >> 4) * kRows * 4u;
     }
-    return (uint32_t)w;
-}
-
-constexpr int kTileThreads = 512;
-
-// A thread's place in the tile.
-struct Place {
-    int c, r;                                               // its first column and row
-    __device__ __forceinline__ Place() : c((threadIdx.x & 15) * 8), r((threadIdx.x >> 4) * 4) {}
 };
 
-struct Turn {
-    // LDS bytes of eight columns of 128 rows, and four banks more: no two of a wave's words, eight columns and four rows apart, meet.
+// Transposes of N tiles of values on their way out, each in 8 bits with a power of two for each of its columns.
+template <int N, typename O> struct Turn {
+    // Bytes of eight columns of 128 rows, and four banks more: no two of a wave's words, eight columns and four rows apart, meet.
     static constexpr int kPitch = 1024 + 16;
-    __align__(16) uint8_t tile[16 * kPitch];
-    uint32_t most[kTileThreads / 64][128];
+    __align__(16) uint8_t tile[N][16 * kPitch];
+    uint32_t most[N][kTileThreads / 64][128];
+    __align__(16) float power[N][128];
+
+    // First the columns' largest magnitudes in each wave.  A step halves the lanes that hold a column and joins two columns, in
+    // the halves of the wave and then in their halves; the wave's four rows of lanes end with columns 0, 2, 1, 3 and the same and four.
+    __device__ __forceinline__ void look(int which, const float (&v)[kRows][8], const Place<O> &at)
+    {
+        uint32_t m[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m[j] = magnitude(larger(larger(0.f, v[0][j], v[1][j]), v[2][j], v[3][j]));
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            const auto r = __builtin_amdgcn_permlane32_swap(m[j], m[j + 1], false, false);
+            m[j] = max(r[0], r[1]);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j += 4) {
+            const auto r = __builtin_amdgcn_permlane16_swap(m[j], m[j + 2], false, false);
+            most[which][at.wave][at.c + j + (at.lane >> 5) + 2 * (at.lane >> 4 & 1)] = max(r[0], r[1]);
+        }
+    }
+    // Then, behind a barrier, their powers of two.
+    __device__ __forceinline__ void decide(int which, int c, const EightOut &o, const Tile &t, bool e5m2)
+    {
+        uint32_t m = 0;
+#pragma unroll
+        for (int w = 0; w < kTileThreads / 64; ++w) m = max(m, most[which][w][c]);
+        const uint32_t e = scale_of(m, top_of(e5m2));
+        if (c < t.cols) store_scale(o.scales, o.ld_s, t.col0 + c, t.down, t.high, e);
+        power[which][c] = power_of(e);
+    }
+    // Behind another, the bytes.
+    __device__ __forceinline__ void put(int which, const float (&v)[kRows][8], bool e5m2, const Place<O> &at)
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            *(uint32_t *)(tile[which] + at.c / 8 * kPitch + j * 128 + at.r) = to_four(v[0][j], v[1][j], v[2][j], v[3][j], power[which][at.c + j], e5m2);
+    }
+    // And behind a last one whole rows of the transpose.
+    template <bool FULL, bool LINES> __device__ __forceinline__ void leave(int which, const EightOut &o, const Tile &t, const Place<O> &at)
+    {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int c0 = at.wave * 16 + k * 8, c = c0 + (at.lane >> 3), r = (at.lane & 7) * 16;
+            if (!FULL && (c >= t.cols || r >= t.rows)) continue;
+            const uint8_t *from = tile[which] + c0 / 8 * kPitch + (at.lane >> 3) * 128 + r;
+            uint8_t *to = o.q + (t.col0 + c0) * o.ld + t.row0 + ((O)(at.lane >> 3) * (O)o.ld + r);
+            if (FULL || r + 16 <= t.rows) {
+                if constexpr (LINES) __builtin_nontemporal_store(*(const w32x4 *)from, (w32x4_any *)to);
+                else *(w32x4_any *)to = *(const w32x4 *)from;
+            } else {
+                for (int i = 0; i < t.rows - r; ++i) to[i] = from[i];
+            }
+        }
+    }
 };
 
-// The tile's transpose in 8 bits with a power of two for each of its columns, through LDS, in whole rows.
-__device__ __forceinline__ void leave_turned(const EightOut &o, const float (&v)[4][8], const Tile &t, bool e5m2, Turn &lds)
+// Eight of a tile's row in 8 bits with the power of two of the row's 128.
+template <bool FULL, bool LINES, typename O>
+__device__ __forceinline__ void leave_part(const EightOut &o, const float (&v)[8], const Tile &t, const Place<O> &at, int i, bool e5m2)
 {
-    const Place at;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    __syncthreads();                                        // what was here before has been read
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        uint32_t m = max(max(magnitude(v[0][j]), magnitude(v[1][j])), max(magnitude(v[2][j]), magnitude(v[3][j])));
-        m = max(m, (uint32_t)__shfl_xor((int)m, 16));
-        m = max(m, (uint32_t)__shfl_xor((int)m, 32));
-        if (lane < 16) lds.most[wave][at.c + j] = m;
+    const uint32_t e = scale_of(max_of_16(largest_of(v)), top_of(e5m2));
+    if (!FULL && at.r + i >= t.rows) return;
+    if (at.c == 0) {
+        uint8_t *byte = at.scale(o.scales, o.ld_s, t, i);
+        *byte = (uint8_t)e;
+        if (t.along + 1 == t.wide)                          // ones in the rest of the row's last word
+            for (int k = 1; k < 4 - (int)(t.along % 4); ++k) byte[k] = 127;
     }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int w = 0; w < kTileThreads / 64; ++w) m = max(m, lds.most[w][at.c + j]);
-        const uint32_t e = scale_of(m, top_of(e5m2));
-        if (at.r == 0 && at.c + j < t.cols) store_scale(o.scales, o.ld_s, t.col0 + at.c + j, t.down, t.high, e);
-        const float four[4] = {v[0][j], v[1][j], v[2][j], v[3][j]};
-        *(uint32_t *)(lds.tile + at.c / 8 * Turn::kPitch + j * 128 + at.r) = to_four(four, inverse_of(e), e5m2);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int c = (threadIdx.x >> 3) + 64 * k, r = (threadIdx.x & 7) * 16;
-        if (c >= t.cols || r >= t.rows) continue;
-        const uint8_t *from = lds.tile + c / 8 * Turn::kPitch + c % 8 * 128 + r;
-        uint8_t *to = o.q + (t.col0 + c) * o.ld + t.row0 + r;
-        if (r + 16 <= t.rows) *(w32x4_any *)to = *(const w32x4 *)from;
-        else
-            for (int i = 0; i < t.rows - r; ++i) to[i] = from[i];
-    }
+    store8_bytes<LINES>(at.in(o.q, o.ld, t, i), FULL ? 8 : t.cols - at.c, to_eight_scaled(v, power_of(e), e5m2));
 }
 
-// A thread's rows in 8 bits with a power of two for each row of the tile.
-__device__ __forceinline__ void leave_rows(const EightOut &o, const float (&v)[4][8], const Tile &t, bool e5m2)
-{
-    const Place at;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = max(m, magnitude(v[i][j]));
-        const uint32_t e = scale_of(max_of_16(m), top_of(e5m2));
-        if (at.r + i >= t.rows) continue;
-        if (at.c == 0) store_scale(o.scales, o.ld_s, t.row0 + at.r + i, t.along, t.wide, e);
-        store8_bytes<false>(o.q + (t.row0 + at.r + i) * o.ld + t.col0 + at.c, t.cols - at.c, to_eight(v[i], inverse_of(e), e5m2));
-    }
-}
+// A thread's rows of 8-bit values, and their powers of two.
+struct Rows {
+    w32x2 q[kRows];
+    uint32_t e[kRows];
 
-__device__ __forceinline__ float factor_at(const EightIn &x, const Tile &t, int r)
-{
-    return factor_of(x.scales[(t.along / 4 * x.ld_s + t.row0 + r) * 4 + t.along % 4]);
-}
+    template <bool FULL, typename O> __device__ __forceinline__ void load(const EightIn &x, const Tile &t, const Place<O> &at)
+    {
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int n = FULL ? 8 : at.r + i < t.rows ? t.cols - at.c : 0;
+            q[i] = load8_bytes(at.in(x.q, x.ld, t, i), n);
+            e[i] = FULL || n > 0 ? *at.scale(x.scales, x.ld_s, t, i) : 0;
+        }
+    }
+    // Four of row i, the first or the last.
+    __device__ __forceinline__ void widen(int i, int half, bool e5m2, float v[4]) const { widen4(q[i][half], e5m2, power_of(e[i]), v); }
+};
 
 struct GateBackward {
     const void *dy;
@@ -260,40 +316,110 @@ struct GateBackward {
     void *dg, *du;
     uint64_t ld_dg, ld_du;
     EightOut dg8, du8, dg8_t, du8_t, y8_t;
+    uint32_t tiles;
+    uint8_t turns;                                          // which of the last three there are
     uint8_t kept_e5m2, grad_e5m2, y_e5m2;
 };
 
-template <typename T, int ACT> __global__ __launch_bounds__(kTileThreads) void k_gate_backward(GateBackward a)
+// The kernel's arguments as they lie in memory: more than the scalar registers hold, so that each is read where it is used (what is
+// said here keeps the compiler from reading all of them first and holding them in vector registers).
+typedef const __attribute__((address_space(4))) GateBackward *GateArgs;
+__device__ __forceinline__ GateArgs gate_args()
 {
-    __shared__ Turn lds;
-    const Tile t = tile_of(blockIdx.x, a.rows, a.cols);
-    const Place at;
-    float dg[4][8], du[4][8], y[4][8];
+    GateArgs a = (GateArgs)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(a));
+    return a;
+}
+template <typename T> __device__ __forceinline__ T *global(T *p) { return (T *)(__attribute__((address_space(1))) T *)p; }
+__device__ __forceinline__ EightIn read(const __attribute__((address_space(4))) EightIn &x)
+{
+    return EightIn{global(x.q), global(x.scales), x.ld, x.ld_s};
+}
+__device__ __forceinline__ EightOut read(const __attribute__((address_space(4))) EightOut &x)
+{
+    return EightOut{global(x.q), global(x.scales), x.ld, x.ld_s};
+}
+
+// The rows' results leave first, then the columns' (three tiles of fp32 in registers) through LDS.  FULL: the tile lies within the matrix.
+template <typename T, int ACT, bool FULL, bool LINES, typename O> __device__ __forceinline__ void gate_tile(const Tile &t, Turn<3, O> &turn)
+{
+    const Place<O> at;
+    const bool gated = gate_args()->u8.q;
+    float dg[kRows][8], du[kRows][8], y[kRows][8];
+    {
+        Eight<T> dy[kRows];
+        Rows g8, u8 = {};
+        const GateArgs a = gate_args();
+        const T *from = global((const T *)a->dy);
+        const bool e5m2 = a->kept_e5m2;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = at.r + i, n = r < t.rows ? t.cols - at.c : 0;
-        const uint64_t row = t.row0 + r, col = t.col0 + at.c;
-        float dy[8], g[8], u[8];
-        load8<false>((const T *)a.dy + row * a.ld_dy + col, n, dy);
-        widen8(load8_bytes(a.g8.q + row * a.g8.ld + col, n), a.kept_e5m2, n > 0 ? factor_at(a.g8, t, r) : 0.f, g);
-        if (a.u8.q) widen8(load8_bytes(a.u8.q + row * a.u8.ld + col, n), a.kept_e5m2, n > 0 ? factor_at(a.u8, t, r) : 0.f, u);
+        for (int i = 0; i < kRows; ++i)
+            dy[i].template load<false>(at.in(from, a->ld_dy, t, i), FULL ? 8 : at.r + i < t.rows ? t.cols - at.c : 0);
+        g8.load<FULL>(read(a->g8), t, at);
+        if (gated) u8.load<FULL>(read(gate_args()->u8), t, at);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float v, slope;
-            act<ACT>(g[j], &v, &slope);
-            const float by_u = a.u8.q ? u[j] : 1.f;
-            dg[i][j] = dy[j] * by_u * slope;
-            du[i][j] = dy[j] * v;
-            y[i][j] = v * by_u;
-        }
-        if (a.dg) store8((T *)a.dg + row * a.ld_dg + col, n, dg[i]);
-        if (a.du) store8((T *)a.du + row * a.ld_du + col, n, du[i]);
+        for (int i = 0; i < kRows; ++i)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                float g[4], u[4] = {1.f, 1.f, 1.f, 1.f};
+                g8.widen(i, half, e5m2, g);
+                if (gated) u8.widen(i, half, e5m2, u);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int j = half * 4 + k;
+                    float v, slope;
+                    act<ACT>(g[k], &v, &slope);
+                    const float d = dy[i][j];
+                    dg[i][j] = d * u[k] * slope;
+                    du[i][j] = d * v;
+                    y[i][j] = v * u[k];
+                    // here and not where they are used, behind branches, with all that they are made of held until then
+                    asm volatile("" : "+v"(dg[i][j]), "+v"(du[i][j]), "+v"(y[i][j]));
+                }
+                __builtin_amdgcn_sched_barrier(0);          // more values under way than four would not fit the registers
+            }
     }
-    if (a.dg8.q) leave_rows(a.dg8, dg, t, a.grad_e5m2);
-    if (a.du8.q) leave_rows(a.du8, du, t, a.grad_e5m2);
-    if (a.dg8_t.q) leave_turned(a.dg8_t, dg, t, a.grad_e5m2, lds);
-    if (a.du8_t.q) leave_turned(a.du8_t, du, t, a.grad_e5m2, lds);
-    if (a.y8_t.q) leave_turned(a.y8_t, y, t, a.y_e5m2, lds);
+    auto wide = [&](T *out, uint64_t ld, const float (&v)[kRows][8]) {
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) store8(at.in(global(out), ld, t, i), FULL ? 8 : at.r + i < t.rows ? t.cols - at.c : 0, v[i]);
+    };
+    auto rows = [&](const EightOut &o, bool e5m2, const float (&v)[kRows][8]) {
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) leave_part<FULL, LINES>(o, v[i], t, at, i, e5m2);
+    };
+    if (const GateArgs a = gate_args(); a->dg) wide((T *)a->dg, a->ld_dg, dg);
+    if (const GateArgs a = gate_args(); a->du) wide((T *)a->du, a->ld_du, du);
+    if (const GateArgs a = gate_args(); a->dg8.q) rows(read(a->dg8), a->grad_e5m2, dg);
+    if (const GateArgs a = gate_args(); a->du8.q) rows(read(a->du8), a->grad_e5m2, du);
+    if (gate_args()->turns == 0) return;
+    turn.look(0, dg, at);
+    turn.look(1, du, at);
+    turn.look(2, y, at);
+    __syncthreads();
+    // two waves for each of the three
+    if (const GateArgs a = gate_args(); at.wave < 6 && (a->turns >> at.wave / 2 & 1)) {
+        const int which = at.wave / 2;
+        turn.decide(which, at.wave % 2 * 64 + at.lane, read(which == 0 ? a->dg8_t : which == 1 ? a->du8_t : a->y8_t), t,
+                    which == 2 ? a->y_e5m2 : a->grad_e5m2);
+    }
+    __syncthreads();
+    if (const GateArgs a = gate_args(); a->turns & 1) turn.put(0, dg, a->grad_e5m2, at);
+    if (const GateArgs a = gate_args(); a->turns & 2) turn.put(1, du, a->grad_e5m2, at);
+    if (const GateArgs a = gate_args(); a->turns & 4) turn.put(2, y, a->y_e5m2, at);
+    __syncthreads();
+    if (const GateArgs a = gate_args(); a->turns & 1) turn.template leave<FULL, LINES>(0, read(a->dg8_t), t, at);
+    if (const GateArgs a = gate_args(); a->turns & 2) turn.template leave<FULL, LINES>(1, read(a->du8_t), t, at);
+    if (const GateArgs a = gate_args(); a->turns & 4) turn.template leave<FULL, LINES>(2, read(a->y8_t), t, at);
+}
+
+__device__ __forceinline__ bool full(const Tile &t) { return t.rows == 128 && t.cols == 128; }
+
+template <typename T, int ACT, bool LINES, typename O> __global__ __launch_bounds__(kTileThreads) void k_gate_backward(GateBackward a)
+{
+    __shared__ Turn<3, O> turn;
+    const Tile t = tile_of(blockIdx.x, a.rows, a.cols);
+    if (full(t)) gate_tile<T, ACT, true, LINES>(t, turn);
+    else gate_tile<T, ACT, false, LINES>(t, turn);
 }
 
 struct TransposeArgs {
@@ -303,18 +429,32 @@ struct TransposeArgs {
     uint8_t e5m2, e5m2_t;
 };
 
-__global__ __launch_bounds__(kTileThreads) void k_transpose(TransposeArgs a)
+template <bool FULL, bool LINES, typename O> __device__ __forceinline__ void transpose_tile(const TransposeArgs &a, const Tile &t, Turn<1, O> &turn)
 {
-    __shared__ Turn lds;
-    const Tile t = tile_of(blockIdx.x, a.rows, a.cols);
-    const Place at;
-    float v[4][8];
+    const Place<O> at;
+    Rows q;
+    q.load<FULL>(a.q, t, at);
+    float v[kRows][8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = at.r + i, n = r < t.rows ? t.cols - at.c : 0;
-        widen8(load8_bytes(a.q.q + (t.row0 + r) * a.q.ld + t.col0 + at.c, n), a.e5m2, n > 0 ? factor_at(a.q, t, r) : 0.f, v[i]);
+    for (int i = 0; i < kRows; ++i) {
+        q.widen(i, 0, a.e5m2, v[i]);
+        q.widen(i, 1, a.e5m2, v[i] + 4);
     }
-    leave_turned(a.q_t, v, t, a.e5m2_t, lds);
+    turn.look(0, v, at);
+    __syncthreads();
+    if (at.wave < 2) turn.decide(0, at.wave * 64 + at.lane, a.q_t, t, a.e5m2_t);
+    __syncthreads();
+    turn.put(0, v, a.e5m2_t, at);
+    __syncthreads();
+    turn.template leave<FULL, LINES>(0, a.q_t, t, at);
+}
+
+template <bool LINES, typename O> __global__ __launch_bounds__(kTileThreads) void k_transpose(TransposeArgs a)
+{
+    __shared__ Turn<1, O> turn;
+    const Tile t = tile_of(blockIdx.x, a.rows, a.cols);
+    if (full(t)) transpose_tile<true, LINES>(a, t, turn);
+    else transpose_tile<false, LINES>(a, t, turn);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -330,13 +470,28 @@ template <typename T> static hipError_t launch_forward(const GateForward &a, int
     return hipGetLastError();
 }
 
+// Results whose rows lie on cache lines, which tiles then do not share, are written past the L2.
+static bool lines_of(const EightOut &o) { return !o.q || on_lines(o.q, o.ld); }
+// Offsets of a wave's rows fit 32 bits.
+static bool near(uint64_t ld) { return ld < (1u << 26); }
+
+template <typename T, int ACT> static void launch_backward(const GateBackward &a, bool lines, bool far, uint32_t grid, hipStream_t s)
+{
+    if (far) k_gate_backward<T, ACT, false, uint64_t><<<grid, kTileThreads, 0, s>>>(a);
+    else if (lines) k_gate_backward<T, ACT, true, uint32_t><<<grid, kTileThreads, 0, s>>>(a);
+    else k_gate_backward<T, ACT, false, uint32_t><<<grid, kTileThreads, 0, s>>>(a);
+}
+
 template <typename T> static hipError_t launch_backward(const GateBackward &a, int kind, hipStream_t s)
 {
-    const uint32_t grid = (uint32_t)((a.rows + 127) / 128 * ((a.cols + 127) / 128));
-    if (kind == REFT_SILU) k_gate_backward<T, REFT_SILU><<<grid, kTileThreads, 0, s>>>(a);
-    else if (kind == REFT_GELU) k_gate_backward<T, REFT_GELU><<<grid, kTileThreads, 0, s>>>(a);
-    else if (kind == REFT_GELU_TANH) k_gate_backward<T, REFT_GELU_TANH><<<grid, kTileThreads, 0, s>>>(a);
-    else k_gate_backward<T, REFT_RELU2><<<grid, kTileThreads, 0, s>>>(a);
+    const uint32_t grid = a.tiles;
+    const bool lines = lines_of(a.dg8) && lines_of(a.du8) && lines_of(a.dg8_t) && lines_of(a.du8_t) && lines_of(a.y8_t);
+    const bool far = !(near(a.ld_dy) && near(a.ld_dg) && near(a.ld_du) && near(a.g8.ld) && near(a.u8.ld) && near(a.dg8.ld) && near(a.du8.ld) &&
+                       near(a.dg8_t.ld) && near(a.du8_t.ld) && near(a.y8_t.ld));
+    if (kind == REFT_SILU) launch_backward<T, REFT_SILU>(a, lines, far, grid, s);
+    else if (kind == REFT_GELU) launch_backward<T, REFT_GELU>(a, lines, far, grid, s);
+    else if (kind == REFT_GELU_TANH) launch_backward<T, REFT_GELU_TANH>(a, lines, far, grid, s);
+    else launch_backward<T, REFT_RELU2>(a, lines, far, grid, s);
     return hipGetLastError();
 }
 
@@ -459,13 +614,15 @@ extern "C" int reft_gate_backward(const void *dy, uint64_t ld_dy, const reft_eig
     a.u8 = in_of(u8);
     a.dg = dg;
     a.du = du;
-    a.ld_dg = ld_dg;
-    a.ld_du = ld_du;
+    a.ld_dg = dg ? ld_dg : 0;
+    a.ld_du = du ? ld_du : 0;
     a.dg8 = out_of(dg8);
     a.du8 = out_of(du8);
     a.dg8_t = out_of(dg8_t);
     a.du8_t = out_of(du8_t);
     a.y8_t = out_of(y8_t);
+    a.turns = (a.dg8_t.q ? 1 : 0) | (a.du8_t.q ? 2 : 0) | (a.y8_t.q ? 4 : 0);
+    a.tiles = (uint32_t)((rows + 127) / 128 * ((cols + 127) / 128));
     a.kept_e5m2 = kept_format == REFT_E5M2;
     a.grad_e5m2 = grad_format == REFT_E5M2;
     a.y_e5m2 = y_format == REFT_E5M2;
@@ -494,6 +651,10 @@ extern "C" int reft_transpose(const reft_eight *q, int format, uint64_t rows, ui
     a.cols = cols;
     a.e5m2 = format == REFT_E5M2;
     a.e5m2_t = format_t == REFT_E5M2;
-    k_transpose<<<(uint32_t)((rows + 127) / 128 * ((cols + 127) / 128)), kTileThreads, 0, (hipStream_t)stream>>>(a);
+    const uint32_t grid = (uint32_t)((rows + 127) / 128 * ((cols + 127) / 128));
+    hipStream_t s = (hipStream_t)stream;
+    if (!near(q->ld) || !near(q_t->ld)) k_transpose<false, uint64_t><<<grid, kTileThreads, 0, s>>>(a);
+    else if (lines_of(a.q_t)) k_transpose<true, uint32_t><<<grid, kTileThreads, 0, s>>>(a);
+    else k_transpose<false, uint32_t><<<grid, kTileThreads, 0, s>>>(a);
     return launched(who, hipGetLastError());
 }
