@@ -615,7 +615,7 @@ int reft_heads_backward(const reft_heads *dq_out, const reft_heads *dk_out, cons
  *   REFT_GELU_TANH  g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2
  *   REFT_RELU2      max(g, 0)^2
  * Outputs are each left out where NULL.  y may be g or u (with the same ld).  Where a block of 128 values of g8, u8 or y8 holds an infinity or
- * a NaN, all of it is NaN.  rows < 2^31, cols <= 128 * 65535, ceil(rows / 4) ceil(cols / 512) < 2^24.
+ * a NaN, all of it is NaN.  rows, cols < 2^31, rows ceil(cols / 512) <= 2^26 - 4.
  */
 #define REFT_SILU      0
 #define REFT_GELU      1
@@ -630,7 +630,7 @@ int reft_gate_forward(const void *g, uint64_t ld_g, const void *u, uint64_t ld_u
  * as dg and du in dtype; in 8 bits (grad_format) as dg8 and du8, for the product that gives the gradient of the products' inputs, and transposed, as
  * dg8_t and du8_t ([cols][rows], scales per 128 rows), for that of their weights; and y = act(g) u, transposed, as y8_t in y_format, for the gradient
  * of the weights that y is multiplied by.  Outputs are each left out where NULL.  dg or du may be dy (with the same ld).
- * rows, cols < 2^31, ceil(rows / 128) ceil(cols / 128) < 2^22.
+ * rows, cols < 2^31, ceil(rows / 128) ceil(cols / 128) < 2^23.
  */
 int reft_gate_backward(const void *dy, uint64_t ld_dy, const reft_eight *g8, const reft_eight *u8, int kept_format,
                        uint64_t rows, uint64_t cols, int dtype, int act, void *dg, uint64_t ld_dg, void *du, uint64_t ld_du,

@@ -135,35 +135,52 @@ struct GateForward {
     void *y;
     uint64_t ld_y;
     EightOut y8, g8, u8;
+    uint32_t words;                                         // of 512 columns in a row
     uint8_t y_e5m2, kept_e5m2;
 };
 
-// Eight of a row's values in 8 bits with the power of two of the 16 lanes' 128.
-__device__ __forceinline__ void leave_row(const EightOut &o, const float v[8], uint64_t row, uint64_t c, int n, bool e5m2)
+// Eight of a row's values in 8 bits with the power of two of the 16 lanes' 128.  FULL: there are all of them.
+template <bool FULL> __device__ __forceinline__ void leave_row(const EightOut &o, const float v[8], uint64_t row, uint64_t c, int n, bool e5m2)
 {
     const uint32_t e = scale_of(max_of_16(largest_of(v)), top_of(e5m2));
-    store8_bytes<true>(o.q + row * o.ld + c, n, to_eight_scaled(v, power_of(e), e5m2));
-    if ((threadIdx.x & 15) == 0) o.scales[(c / 512 * o.ld_s + row) * 4 + c / 128 % 4] = n ? (uint8_t)e : 127;
+    store8_bytes<true>(o.q + row * o.ld + c, FULL ? 8 : n, to_eight_scaled(v, power_of(e), e5m2));
+    if ((threadIdx.x & 15) == 0) o.scales[(c / 512 * o.ld_s + row) * 4 + c / 128 % 4] = FULL || n > 0 ? (uint8_t)e : 127;
 }
 
-// A wave takes 512 columns of a row, 16 lanes each block of 128.
-template <typename T, int ACT> __global__ __launch_bounds__(256) void k_gate_forward(GateForward a)
+template <typename T, int ACT, bool FULL> __device__ __forceinline__ void gate_row(const GateForward &a, uint64_t row, uint64_t c)
 {
-    const uint64_t row = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6), c = (uint64_t)blockIdx.y * 512 + (threadIdx.x & 63) * 8;
-    if (row >= a.rows) return;
-    const int n = c >= a.cols ? 0 : (int)min(a.cols - c, (uint64_t)8);
-    float g[8], u[8], y[8], slope;
-    load8<false>((const T *)a.g + row * a.ld_g + c, n, g);
-    if (a.u) load8<false>((const T *)a.u + row * a.ld_u + c, n, u);
+    const int n = FULL ? 8 : c < a.cols ? (int)min(a.cols - c, (uint64_t)8) : 0;
+    Eight<T> g, u;
+    g.template load<false>((const T *)a.g + row * a.ld_g + c, n);
+    if (a.u) u.template load<false>((const T *)a.u + row * a.ld_u + c, n);
+    float v[8], y[8], slope;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         act<ACT>(g[i], &y[i], &slope);
         if (a.u) y[i] *= u[i];
     }
     if (a.y) store8((T *)a.y + row * a.ld_y + c, n, y);
-    if (a.y8.q) leave_row(a.y8, y, row, c, n, a.y_e5m2);
-    if (a.g8.q) leave_row(a.g8, g, row, c, n, a.kept_e5m2);
-    if (a.u8.q) leave_row(a.u8, u, row, c, n, a.kept_e5m2);
+    if (a.y8.q) leave_row<FULL>(a.y8, y, row, c, n, a.y_e5m2);
+    if (a.g8.q) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = g[i];
+        leave_row<FULL>(a.g8, v, row, c, n, a.kept_e5m2);
+    }
+    if (a.u8.q) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = u[i];
+        leave_row<FULL>(a.u8, v, row, c, n, a.kept_e5m2);
+    }
+}
+
+// A wave takes 512 columns of a row, 16 lanes each block of 128; waves follow each other along the rows.
+template <typename T, int ACT> __global__ __launch_bounds__(256) void k_gate_forward(GateForward a)
+{
+    const uint32_t number = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = number / a.words;
+    const uint64_t first = (uint64_t)(number - row * a.words) * 512, c = first + (threadIdx.x & 63) * 8;
+    if (row >= a.rows) return;
+    if (first + 512 <= a.cols) gate_row<T, ACT, true>(a, row, c);
+    else gate_row<T, ACT, false>(a, row, c);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -175,13 +192,15 @@ struct Tile {
     int rows, cols;                                         // of the matrix in it
 };
 
-__device__ __forceinline__ Tile tile_of(uint32_t number, uint64_t rows, uint64_t cols)
+// Tiles go down the columns of a band, `band` of them, along it, and then to the next band.
+__device__ __forceinline__ Tile tile_of(uint32_t number, uint64_t rows, uint64_t cols, uint32_t band)
 {
     Tile t;
     t.high = (uint32_t)((rows + 127) / 128);
     t.wide = (uint32_t)((cols + 127) / 128);
-    t.down = number / t.wide;
-    t.along = number % t.wide;
+    const uint32_t first = number / (band * t.wide) * band, in = number - first * t.wide, tall = min(t.high - first, band);
+    t.along = in / tall;
+    t.down = first + in - t.along * tall;
     t.row0 = (uint64_t)t.down * 128;
     t.col0 = (uint64_t)t.along * 128;
     t.rows = (int)min(rows - t.row0, (uint64_t)128);
@@ -316,7 +335,7 @@ struct GateBackward {
     void *dg, *du;
     uint64_t ld_dg, ld_du;
     EightOut dg8, du8, dg8_t, du8_t, y8_t;
-    uint32_t tiles;
+    uint32_t band;
     uint8_t turns;                                          // which of the last three there are
     uint8_t kept_e5m2, grad_e5m2, y_e5m2;
 };
@@ -340,7 +359,7 @@ __device__ __forceinline__ EightOut read(const __attribute__((address_space(4)))
     return EightOut{global(x.q), global(x.scales), x.ld, x.ld_s};
 }
 
-// The rows' results leave first, then the columns' (three tiles of fp32 in registers) through LDS.  FULL: the tile lies within the matrix.
+// The rows' results leave while the columns' powers of two are settled, then the columns' (three tiles of fp32 in registers) through LDS.  FULL: the tile lies within the matrix.
 template <typename T, int ACT, bool FULL, bool LINES, typename O> __device__ __forceinline__ void gate_tile(const Tile &t, Turn<3, O> &turn)
 {
     const Place<O> at;
@@ -387,11 +406,6 @@ template <typename T, int ACT, bool FULL, bool LINES, typename O> __device__ __f
 #pragma unroll
         for (int i = 0; i < kRows; ++i) leave_part<FULL, LINES>(o, v[i], t, at, i, e5m2);
     };
-    if (const GateArgs a = gate_args(); a->dg) wide((T *)a->dg, a->ld_dg, dg);
-    if (const GateArgs a = gate_args(); a->du) wide((T *)a->du, a->ld_du, du);
-    if (const GateArgs a = gate_args(); a->dg8.q) rows(read(a->dg8), a->grad_e5m2, dg);
-    if (const GateArgs a = gate_args(); a->du8.q) rows(read(a->du8), a->grad_e5m2, du);
-    if (gate_args()->turns == 0) return;
     turn.look(0, dg, at);
     turn.look(1, du, at);
     turn.look(2, y, at);
@@ -402,6 +416,11 @@ template <typename T, int ACT, bool FULL, bool LINES, typename O> __device__ __f
         turn.decide(which, at.wave % 2 * 64 + at.lane, read(which == 0 ? a->dg8_t : which == 1 ? a->du8_t : a->y8_t), t,
                     which == 2 ? a->y_e5m2 : a->grad_e5m2);
     }
+    if (const GateArgs a = gate_args(); a->dg) wide((T *)a->dg, a->ld_dg, dg);
+    if (const GateArgs a = gate_args(); a->du) wide((T *)a->du, a->ld_du, du);
+    if (const GateArgs a = gate_args(); a->dg8.q) rows(read(a->dg8), a->grad_e5m2, dg);
+    if (const GateArgs a = gate_args(); a->du8.q) rows(read(a->du8), a->grad_e5m2, du);
+    if (gate_args()->turns == 0) return;
     __syncthreads();
     if (const GateArgs a = gate_args(); a->turns & 1) turn.put(0, dg, a->grad_e5m2, at);
     if (const GateArgs a = gate_args(); a->turns & 2) turn.put(1, du, a->grad_e5m2, at);
@@ -417,7 +436,7 @@ __device__ __forceinline__ bool full(const Tile &t) { return t.rows == 128 && t.
 template <typename T, int ACT, bool LINES, typename O> __global__ __launch_bounds__(kTileThreads) void k_gate_backward(GateBackward a)
 {
     __shared__ Turn<3, O> turn;
-    const Tile t = tile_of(blockIdx.x, a.rows, a.cols);
+    const Tile t = tile_of(blockIdx.x, a.rows, a.cols, a.band);
     if (full(t)) gate_tile<T, ACT, true, LINES>(t, turn);
     else gate_tile<T, ACT, false, LINES>(t, turn);
 }
@@ -426,6 +445,7 @@ struct TransposeArgs {
     EightIn q;
     EightOut q_t;
     uint64_t rows, cols;
+    uint32_t band;
     uint8_t e5m2, e5m2_t;
 };
 
@@ -452,7 +472,7 @@ template <bool FULL, bool LINES, typename O> __device__ __forceinline__ void tra
 template <bool LINES, typename O> __global__ __launch_bounds__(kTileThreads) void k_transpose(TransposeArgs a)
 {
     __shared__ Turn<1, O> turn;
-    const Tile t = tile_of(blockIdx.x, a.rows, a.cols);
+    const Tile t = tile_of(blockIdx.x, a.rows, a.cols, a.band);
     if (full(t)) transpose_tile<true, LINES>(a, t, turn);
     else transpose_tile<false, LINES>(a, t, turn);
 }
@@ -462,13 +482,16 @@ template <bool LINES, typename O> __global__ __launch_bounds__(kTileThreads) voi
 // ------------------------------------------------------------------------------------------------
 template <typename T> static hipError_t launch_forward(const GateForward &a, int kind, hipStream_t s)
 {
-    const dim3 grid((uint32_t)((a.rows + 3) / 4), (uint32_t)((a.cols + 511) / 512));
+    const uint32_t grid = (uint32_t)((a.rows * a.words + 3) / 4);
     if (kind == REFT_SILU) k_gate_forward<T, REFT_SILU><<<grid, 256, 0, s>>>(a);
     else if (kind == REFT_GELU) k_gate_forward<T, REFT_GELU><<<grid, 256, 0, s>>>(a);
     else if (kind == REFT_GELU_TANH) k_gate_forward<T, REFT_GELU_TANH><<<grid, 256, 0, s>>>(a);
     else k_gate_forward<T, REFT_RELU2><<<grid, 256, 0, s>>>(a);
     return hipGetLastError();
 }
+
+// Tiles of a band: a result's neighbours in the transpose are written soon after each other.
+constexpr uint32_t kGateBand = 8, kTransposeBand = 32;
 
 // Results whose rows lie on cache lines, which tiles then do not share, are written past the L2.
 static bool lines_of(const EightOut &o) { return !o.q || on_lines(o.q, o.ld); }
@@ -484,7 +507,7 @@ template <typename T, int ACT> static void launch_backward(const GateBackward &a
 
 template <typename T> static hipError_t launch_backward(const GateBackward &a, int kind, hipStream_t s)
 {
-    const uint32_t grid = a.tiles;
+    const uint32_t grid = (uint32_t)((a.rows + 127) / 128 * ((a.cols + 127) / 128));
     const bool lines = lines_of(a.dg8) && lines_of(a.du8) && lines_of(a.dg8_t) && lines_of(a.du8_t) && lines_of(a.y8_t);
     const bool far = !(near(a.ld_dy) && near(a.ld_dg) && near(a.ld_du) && near(a.g8.ld) && near(a.u8.ld) && near(a.dg8.ld) && near(a.du8.ld) &&
                        near(a.dg8_t.ld) && near(a.du8_t.ld) && near(a.y8_t.ld));
@@ -542,7 +565,7 @@ extern "C" int reft_gate_forward(const void *g, uint64_t ld_g, const void *u, ui
     const char *who = "reft_gate_forward";
     NEED(is_float_type(dtype), REFT_EINVAL, "%s: unknown type %d", who, dtype);
     NEED(is_act(act), REFT_EINVAL, "%s: unknown activation %d", who, act);
-    NEED(rows <= 0x7fffffff && cols <= 128 * 65535, REFT_ESIZE, "%s: too many rows or columns", who);
+    NEED(rows <= 0x7fffffff && cols <= 0x7fffffff, REFT_ESIZE, "%s: too many rows or columns", who);
     NEED(ld_g >= cols && (!u || ld_u >= cols) && (!y || ld_y >= cols), REFT_ESIZE, "%s: rows overlap", who);
     CHECK_EIGHT(who, y8, rows, cols);
     CHECK_EIGHT(who, g8, rows, cols);
@@ -553,7 +576,7 @@ extern "C" int reft_gate_forward(const void *g, uint64_t ld_g, const void *u, ui
     NEED(y || given(y8) || given(g8) || given(u8), REFT_EINVAL, "%s: no output", who);
     NEED(u || !given(u8), REFT_EINVAL, "%s: u8 without u", who);
     NEED(g, REFT_EINVAL, "%s: null pointer", who);
-    NEED((rows + 3) / 4 * ((cols + 511) / 512) <= kMaxBlocks256, REFT_ESIZE, "%s: too many values", who);
+    NEED((rows * ((cols + 511) / 512) + 3) / 4 <= kMaxBlocks256, REFT_ESIZE, "%s: too many values", who);
     NEED(lies(g, size_of(dtype)) && lies(u, size_of(dtype)) && lies(y, size_of(dtype)), REFT_EINVAL, "%s: misaligned pointer", who);
     if ((uintptr_t)stream == kCheckOnly) return REFT_OK;
     GateForward a;
@@ -565,6 +588,7 @@ extern "C" int reft_gate_forward(const void *g, uint64_t ld_g, const void *u, ui
     a.cols = cols;
     a.y = y;
     a.ld_y = ld_y;
+    a.words = (uint32_t)((cols + 511) / 512);
     a.y8 = out_of(y8);
     a.g8 = out_of(g8);
     a.u8 = out_of(u8);
@@ -622,7 +646,7 @@ extern "C" int reft_gate_backward(const void *dy, uint64_t ld_dy, const reft_eig
     a.du8_t = out_of(du8_t);
     a.y8_t = out_of(y8_t);
     a.turns = (a.dg8_t.q ? 1 : 0) | (a.du8_t.q ? 2 : 0) | (a.y8_t.q ? 4 : 0);
-    a.tiles = (uint32_t)((rows + 127) / 128 * ((cols + 127) / 128));
+    a.band = given(dg8) || given(du8) || given(dg8_t) || given(du8_t) ? kGateBand : 1;
     a.kept_e5m2 = kept_format == REFT_E5M2;
     a.grad_e5m2 = grad_format == REFT_E5M2;
     a.y_e5m2 = y_format == REFT_E5M2;
@@ -649,6 +673,7 @@ extern "C" int reft_transpose(const reft_eight *q, int format, uint64_t rows, ui
     a.q_t = out_of(q_t);
     a.rows = rows;
     a.cols = cols;
+    a.band = kTransposeBand;
     a.e5m2 = format == REFT_E5M2;
     a.e5m2_t = format_t == REFT_E5M2;
     const uint32_t grid = (uint32_t)((rows + 127) / 128 * ((cols + 127) / 128));
