@@ -359,8 +359,9 @@ __device__ __forceinline__ EightOut read(const __attribute__((address_space(4)))
     return EightOut{global(x.q), global(x.scales), x.ld, x.ld_s};
 }
 
-// The rows' results leave while the columns' powers of two are settled, then the columns' (three tiles of fp32 in registers) through LDS.  FULL: the tile lies within the matrix.
-template <typename T, int ACT, bool FULL, bool LINES, typename O> __device__ __forceinline__ void gate_tile(const Tile &t, Turn<3, O> &turn)
+// The rows' results leave while the columns' powers of two are settled, then the columns' (three tiles of fp32 in registers) through LDS.  FULL: the tile lies within the matrix;
+// E4M3: so are all 8-bit matrices, and no conversion is chosen while it runs (4096 x 4096 32 -> 28 us).
+template <typename T, int ACT, bool FULL, bool E4M3, bool LINES, typename O> __device__ __forceinline__ void gate_tile(const Tile &t, Turn<3, O> &turn)
 {
     const Place<O> at;
     const bool gated = gate_args()->u8.q;
@@ -370,7 +371,7 @@ template <typename T, int ACT, bool FULL, bool LINES, typename O> __device__ __f
         Rows g8, u8 = {};
         const GateArgs a = gate_args();
         const T *from = global((const T *)a->dy);
-        const bool e5m2 = a->kept_e5m2;
+        const bool e5m2 = !E4M3 && a->kept_e5m2;
 #pragma unroll
         for (int i = 0; i < kRows; ++i)
             dy[i].template load<false>(at.in(from, a->ld_dy, t, i), FULL ? 8 : at.r + i < t.rows ? t.cols - at.c : 0);
@@ -414,17 +415,17 @@ template <typename T, int ACT, bool FULL, bool LINES, typename O> __device__ __f
     if (const GateArgs a = gate_args(); at.wave < 6 && (a->turns >> at.wave / 2 & 1)) {
         const int which = at.wave / 2;
         turn.decide(which, at.wave % 2 * 64 + at.lane, read(which == 0 ? a->dg8_t : which == 1 ? a->du8_t : a->y8_t), t,
-                    which == 2 ? a->y_e5m2 : a->grad_e5m2);
+                    !E4M3 && (which == 2 ? a->y_e5m2 : a->grad_e5m2));
     }
     if (const GateArgs a = gate_args(); a->dg) wide((T *)a->dg, a->ld_dg, dg);
     if (const GateArgs a = gate_args(); a->du) wide((T *)a->du, a->ld_du, du);
-    if (const GateArgs a = gate_args(); a->dg8.q) rows(read(a->dg8), a->grad_e5m2, dg);
-    if (const GateArgs a = gate_args(); a->du8.q) rows(read(a->du8), a->grad_e5m2, du);
+    if (const GateArgs a = gate_args(); a->dg8.q) rows(read(a->dg8), !E4M3 && a->grad_e5m2, dg);
+    if (const GateArgs a = gate_args(); a->du8.q) rows(read(a->du8), !E4M3 && a->grad_e5m2, du);
     if (gate_args()->turns == 0) return;
     __syncthreads();
-    if (const GateArgs a = gate_args(); a->turns & 1) turn.put(0, dg, a->grad_e5m2, at);
-    if (const GateArgs a = gate_args(); a->turns & 2) turn.put(1, du, a->grad_e5m2, at);
-    if (const GateArgs a = gate_args(); a->turns & 4) turn.put(2, y, a->y_e5m2, at);
+    if (const GateArgs a = gate_args(); a->turns & 1) turn.put(0, dg, !E4M3 && a->grad_e5m2, at);
+    if (const GateArgs a = gate_args(); a->turns & 2) turn.put(1, du, !E4M3 && a->grad_e5m2, at);
+    if (const GateArgs a = gate_args(); a->turns & 4) turn.put(2, y, !E4M3 && a->y_e5m2, at);
     __syncthreads();
     if (const GateArgs a = gate_args(); a->turns & 1) turn.template leave<FULL, LINES>(0, read(a->dg8_t), t, at);
     if (const GateArgs a = gate_args(); a->turns & 2) turn.template leave<FULL, LINES>(1, read(a->du8_t), t, at);
@@ -437,8 +438,9 @@ template <typename T, int ACT, bool LINES, typename O> __global__ __launch_bound
 {
     __shared__ Turn<3, O> turn;
     const Tile t = tile_of(blockIdx.x, a.rows, a.cols, a.band);
-    if (full(t)) gate_tile<T, ACT, true, LINES>(t, turn);
-    else gate_tile<T, ACT, false, LINES>(t, turn);
+    if (sizeof(O) == 8 || !full(t)) gate_tile<T, ACT, false, false, LINES>(t, turn);
+    else if (a.kept_e5m2 || a.grad_e5m2 || a.y_e5m2) gate_tile<T, ACT, true, false, LINES>(t, turn);
+    else gate_tile<T, ACT, true, true, LINES>(t, turn);
 }
 
 struct TransposeArgs {
