@@ -587,6 +587,7 @@ typedef struct reft_eight {
  *   out[first] = z[first] cos t - z[second] sin t,  out[second] = z[second] cos t + z[first] sin t,  out[c] = z[c] behind the pairs.
  * Angles are products in 64 bits (exact for positions below 2^29; at most 2^50), sines and cosines of them err by less than 2^-22.  A weight is a
  * vector of cols values for all heads of its kind in weight_dtype (dtype or fp32), NULL: ones.  positions and freqs may be NULL with pairs == 0.
+ * Where a head holds an infinity or a NaN its results are zeroes and NaN; no other head's are touched by it.
  * An output may be its input (with the same strides).  rows < 2^31, 1 to 65535 heads of each kind, 1 <= cols <= 512, 2 pairs <= cols.
  */
 int reft_heads_forward(const reft_heads *q, uint64_t q_heads, const reft_heads *k, uint64_t k_heads, const void *q_weight,
@@ -639,7 +640,8 @@ int reft_gate_backward(const void *dy, uint64_t ld_dy, const reft_eight *g8, con
 
 /* q_t = the transpose of the 8-bit matrix q ([rows][cols]), with scales per 128 rows of q: what the norm or the gate has kept, for the product of the
  * weights' gradient.  A value keeps all its bits where its new block's power of two is not larger than its old one, or not by so much that it
- * becomes subnormal, and the formats are the same.  Limits as for reft_gate_backward.
+ * becomes subnormal, and the formats are the same.  Values are fp32 between: what lies beyond its range is an infinity, and its block NaN.  Limits as
+ * for reft_gate_backward.
  */
 int reft_transpose(const reft_eight *q, int format, uint64_t rows, uint64_t cols, const reft_eight *q_t, int format_t,
                    reft_stream stream);

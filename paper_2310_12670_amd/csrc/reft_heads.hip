@@ -59,7 +59,7 @@ template <int G> __device__ __forceinline__ float sum_of(float v)
     return v;
 }
 
-// To a step of fp32; the hardware's takes numbers below 2^-126, which eps == 0 leaves room for, for zero.
+// To a step of fp32.  The hardware's takes numbers below 2^-126, which eps == 0 leaves room for, for zeroes.
 __device__ __forceinline__ float inverse_root(float v)
 {
     return v < 1.17549435e-38f ? 1.f / sqrtf(v) : __builtin_amdgcn_rsqf(v);
@@ -199,6 +199,10 @@ struct Unit {
     }
 };
 
+// out = rho (x (w cos) + x_partner (w_partner +- sin)), with rho = 1 / rms: the weights and angles are joined once a unit, so that a value takes a
+// square, two products and rho.  Everything is read once and written once, all of a unit's next heads on their way.  Bound by HBM: 16384 rows of
+// 64 + 8 heads of 128 in bf16 115 us, 5.3 TB/s (vector units busy 40 %; a lane a head's eight columns with its own sines 656 us, sines once
+// a row 122, no element-wise ends 117; 2 and 1 heads in flight instead of 4: 116, 117; four times as many waves: 125); one row of them 3.3 us.
 template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(256) void k_heads_forward(HeadsArgs a)
 {
     typedef Wave<T, G, MODE, WHOLE> W;
@@ -255,6 +259,9 @@ template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(
     }
 }
 
+// With u = dout turned back, xhat = x rho: dx = rho (u w - xhat mean(u w xhat)), dweight = sum of u xhat; both means of a head in one go over its lanes,
+// of x^2 and of u w x.  Bound by HBM: 16384 rows of 64 + 8 heads of 128 in bf16 182 us, 5.0 TB/s (queries' and keys' weights summed at once,
+// which takes 16 registers more: 228; at 128 registers with four waves a SIMD: 411, spilled).
 // The gradients; a lane sums its heads' part of a weight's gradient, the block adds its groups' in their order.  Queries first, then keys.
 template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(256) void k_heads_backward(HeadsArgs a)
 {
@@ -342,7 +349,7 @@ __global__ __launch_bounds__(1024) void k_heads_weights(const float *part, uint3
     const uint32_t x = threadIdx.x & 15, y = threadIdx.x >> 4, at = blockIdx.x * 16 + x;
     float s = 0;
     if (at < 2 * cols)
-#pragma unroll 4
+#pragma unroll 8
         for (uint32_t i = y; i < n; i += 64) s += part[(uint64_t)i * 2 * cols + at];
     sums[y][x] = s;
     __syncthreads();
@@ -358,28 +365,30 @@ __global__ __launch_bounds__(1024) void k_heads_weights(const float *part, uint3
 constexpr uint64_t kMaxHeadCols = 512;
 static int lanes_of(uint64_t cols) { return cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : 64; }
 
-constexpr uint64_t kWaves = 4096, kTurns = 4, kBackwardBlocks = 512;
-// Groups of lanes for a row: as many as leave each kTurns heads (a row's heads lie together more often than a head's rows), more
-// where that fills the chip; then parts of the heads, for the same.
-static Shares shares_of(uint64_t rows, uint64_t heads, uint64_t cols)
+constexpr uint64_t kWaves = 4096, kBackwardWaves = 2048, kTurns = 4, kBackwardBlocks = 512;
+// Groups of lanes for a row: as many as leave each kTurns heads (16384 rows of 32 + 32 heads of 64, us with a row on a whole wave and on an
+// eighth: 50 and 64; of 4 + 1 heads of 128 17 and 12), more where that fills the chip with `waves` units; then parts of the heads, for the same
+// (1024 rows of 72 heads of 128, us with 4096 and 16384: 10.5 and 15; their gradient with 2048 and 4096: 17.5 and 18.7).
+static Shares shares_of(uint64_t rows, uint64_t heads, uint64_t cols, uint64_t waves)
 {
     Shares s = {};
     if (!heads) return s;
     const uint64_t groups = 64 / lanes_of(cols);
     s.row_groups = 1;
-    while (s.row_groups < groups && (s.row_groups * 2 * kTurns <= heads || (s.row_groups < heads && (rows * s.row_groups + groups - 1) / groups < kWaves)))
+    while (s.row_groups < groups && (s.row_groups * 2 * kTurns <= heads || (s.row_groups < heads && (rows * s.row_groups + groups - 1) / groups < waves)))
         s.row_groups *= 2;
     s.wave_rows = (uint32_t)(groups / s.row_groups);
     const uint64_t bunches = (rows + s.wave_rows - 1) / s.wave_rows, turns = (heads + s.row_groups - 1) / s.row_groups;
-    s.parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(turns, kWaves / std::max<uint64_t>(1, bunches)));
+    s.parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(turns, waves / std::max<uint64_t>(1, bunches)));
     s.units = bunches * s.parts;
     return s;
 }
 
-// The gradients' blocks: as many as the chip holds at once, or as few as need no more rounds of them.
+// The gradients' blocks: what the chip holds at once at 176 registers (two waves a SIMD: 16384 rows of 72 heads of 128, us with 256, 512 and
+// 1024 blocks 200, 178 and 185), or as few as need no more rounds of their waves.
 static uint32_t backward_blocks(uint64_t rows, uint64_t q_heads, uint64_t k_heads, uint64_t cols)
 {
-    const uint64_t blocks = (std::max(shares_of(rows, q_heads, cols).units, shares_of(rows, k_heads, cols).units) + 3) / 4;
+    const uint64_t blocks = (std::max(shares_of(rows, q_heads, cols, kBackwardWaves).units, shares_of(rows, k_heads, cols, kBackwardWaves).units) + 3) / 4;
     const uint64_t rounds = (blocks + kBackwardBlocks - 1) / kBackwardBlocks;
     return blocks ? (uint32_t)((blocks + rounds - 1) / rounds) : 0;
 }
@@ -467,7 +476,7 @@ static Side side_of(const reft_heads *x, uint64_t rows, uint64_t heads, uint64_t
                     const reft_heads *out)
 {
     Side s = {};
-    s.share = shares_of(rows, heads, cols);
+    s.share = shares_of(rows, heads, cols, dy ? kBackwardWaves : kWaves);
     s.heads = (uint32_t)heads;
     s.weight = weight;
     s.x = x->p;
