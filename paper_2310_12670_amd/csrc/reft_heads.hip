@@ -201,7 +201,7 @@ struct Unit {
 
 // out = rho (x (w cos) + x_partner (w_partner +- sin)), with rho = 1 / rms: the weights and angles are joined once a unit, so that a value takes a
 // square, two products and rho.  Everything is read once and written once, all of a unit's next heads on their way.  Bound by HBM: 16384 rows of
-// 64 + 8 heads of 128 in bf16 115 us, 5.3 TB/s (vector units busy 40 %; a lane a head's eight columns with its own sines 656 us, sines once
+// 64 + 8 heads of 128 in bf16 115 us, 5.3 TB/s (vector units busy 46 %; a lane a head's eight columns with its own sines 656 us, sines once
 // a row 122, no element-wise ends 117; 2 and 1 heads in flight instead of 4: 116, 117; four times as many waves: 125); one row of them 3.3 us.
 template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(256) void k_heads_forward(HeadsArgs a)
 {

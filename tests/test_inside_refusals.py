@@ -256,3 +256,21 @@ def test_limits_of_the_gate(inside):
         assert f(128, 128 * 0x7FFFFF) == reft.REFT_OK and f(129, 128 * 0x7FFFFF) == ESIZE and f(128, 128 * 0x7FFFFF + 1) == ESIZE
         assert f(128 * 0x7FFFFF, 128) == reft.REFT_OK and f(128 * 0x7FFFFF + 1, 128) == ESIZE
         assert f(1 << 31, 1) == ESIZE and f(1, 1 << 31) == ESIZE
+
+
+# ---- memory that the current GPU does not see -------------------------------------------------------------------------------
+def test_another_gpus_memory_is_refused():
+    from test_step_operands import Elsewhere
+    far = lambda t: Elsewhere(t)                                                         # noqa: E731
+    x, w, e = torch.zeros(4, 3, 16), torch.ones(16), pair(4, 48)
+    at, f = torch.zeros(4, dtype=torch.int64), torch.ones(8)
+    flat = torch.zeros(4, 48)
+    away = lambda p: (far(p[0]), far(p[1]))                                                # noqa: E731
+    calls = [lambda: reft.reft_heads_forward(far(x), None, far(w), None, far(at), far(f), 1e-5, far(x)),
+             lambda: reft.reft_heads_backward(far(x), None, far(x), None, None, None, far(at), far(f), 1e-5, dq=far(x)),
+             lambda: reft.reft_gate_forward(far(flat), None, "silu", y8=away(e)),
+             lambda: reft.reft_gate_backward(far(flat), away(e), None, "silu", dg=far(flat)),
+             lambda: reft.reft_transpose(*away(e), *away(pair(48, 4)))]
+    for call in calls:
+        for _ in range(2):
+            assert "cuda:77" in refused(EINVAL, call)
