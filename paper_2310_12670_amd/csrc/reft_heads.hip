@@ -30,7 +30,7 @@ struct HeadsArgs {
     uint32_t cols, pairs;
     float eps, inverse_cols;
     float *part;                   // [blocks][2][cols], of the backward pass
-    uint8_t adjacent, weight_f32, lines;    // lines: heads lie on cache lines
+    uint8_t adjacent, weight_f32;
 };
 
 // Sine and cosine of position * frequency.  The angle is a product in 64 bits; the multiple of pi / 2 next to it leaves in two parts (Cody
@@ -82,11 +82,10 @@ __device__ __forceinline__ Side side_at(const HeadsArgs &a, bool keys)
     return s;
 }
 
-// Eight values of a head, or none; WHOLE: there are no heads' ends between; past: not kept in the caches.
-template <bool WHOLE, typename T> __device__ __forceinline__ void load_part(Eight<T> &e, const T *p, int n, bool past = false)
+// Eight values of a head, or none; WHOLE: there are no heads' ends between.
+template <bool WHOLE, typename T> __device__ __forceinline__ void load_part(Eight<T> &e, const T *p, int n)
 {
-    if (past) e.template load<true>(p, WHOLE ? n > 0 ? 8 : 0 : n);
-    else e.template load<false>(p, WHOLE ? n > 0 ? 8 : 0 : n);
+    e.template load<false>(p, WHOLE ? n > 0 ? 8 : 0 : n);
 }
 template <bool WHOLE, typename T> __device__ __forceinline__ void store_part(T *p, int n, const float v[8])
 {
@@ -201,14 +200,15 @@ struct Unit {
 
 // out = rho (x (w cos) + x_partner (w_partner +- sin)), with rho = 1 / rms: the weights and angles are joined once a unit, so that a value takes a
 // square, two products and rho.  Everything is read once and written once, all of a unit's next heads on their way.  Bound by HBM: 16384 rows of
-// 64 + 8 heads of 128 in bf16 115 us, 5.3 TB/s (vector units busy 46 %; a lane a head's eight columns with its own sines 656 us, sines once
-// a row 122, no element-wise ends 117; 2 and 1 heads in flight instead of 4: 116, 117; four times as many waves: 125); one row of them 3.3 us.
-template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(256) void k_heads_forward(HeadsArgs a)
+// 64 + 8 heads of 128 in bf16 118 us, 5.1 TB/s (vector units busy 46 %; a lane a head's eight columns with its own sines 656 us, sines once
+// a row 122, no element-wise ends 117; results through the L2 122; loads past it no different); 1024 of them 8.3 us, one 3.2.  Four heads at once in more
+// registers, four waves a SIMD instead of five: 116, 10.5 and 3.3; three: 115, 9.9 and 3.3.
+template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 5) void k_heads_forward(HeadsArgs a)
 {
     typedef Wave<T, G, MODE, WHOLE> W;
     __shared__ typename W::Room room[4];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = (threadIdx.x & 63) / G;
-    constexpr int kAhead = 8 / sizeof(T);                   // heads of a group in flight
+    constexpr int kAhead = 2;                               // heads of a group worked on at once, and as many on their way
     W w(room[wave], a);
     const uint64_t units = a.side[0].share.units + a.side[1].share.units;
     for (uint64_t number = (uint64_t)blockIdx.x * 4 + wave; number < units; number += (uint64_t)gridDim.x * 4) {
@@ -223,7 +223,7 @@ template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(
         // all lanes of the wave go round as often
         auto fetch = [&](uint32_t head0) {
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) load_part<WHOLE>(next[k], from + k * step_x, head0 + k * u.step + u.slot < s.heads ? there : 0, a.lines);
+            for (int k = 0; k < kAhead; ++k) load_part<WHOLE>(next[k], from + k * step_x, head0 + k * u.step + u.slot < s.heads ? there : 0);
             from += kAhead * step_x;
         };
         fetch(u.head0);
@@ -288,8 +288,8 @@ template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(
 #pragma unroll
                 for (int k = 0; k < kAhead; ++k) {
                     const int n = head0 + k * u.step + u.slot < s.heads ? there : 0;
-                    load_part<WHOLE>(next[k], from + k * step_x, n, a.lines);
-                    load_part<WHOLE>(next_dy[k], from_dy + k * step_dy, n, a.lines);
+                    load_part<WHOLE>(next[k], from + k * step_x, n);
+                    load_part<WHOLE>(next_dy[k], from_dy + k * step_dy, n);
                 }
                 from += kAhead * step_x;
                 from_dy += kAhead * step_dy;
@@ -449,13 +449,6 @@ static int check_heads(const char *who, uint64_t q_heads, const reft_heads *k, u
     return REFT_OK;
 }
 
-// Heads on cache lines, which no two of them share, are read past the L2.
-static bool heads_on_lines(const reft_heads *x, uint64_t cols, int dtype)
-{
-    const uint64_t size = size_of(dtype);
-    return !x || (on_lines(x->p, x->row * size) && x->head * size % 128 == 0 && cols * size % 128 == 0);
-}
-
 static HeadsArgs heads_args(const int64_t *positions, const float *freqs, uint64_t pairs, int adjacent, uint64_t rows, uint64_t cols,
                             int weight_dtype, double eps)
 {
@@ -510,7 +503,6 @@ extern "C" int reft_heads_forward(const reft_heads *q, uint64_t q_heads, const r
     HeadsArgs a = heads_args(positions, freqs, pairs, adjacent, rows, cols, weight_dtype, eps);
     a.side[0] = side_of(q, rows, q_heads, cols, q_weight, nullptr, q_out);
     if (k) a.side[1] = side_of(k, rows, k_heads, cols, k_weight, nullptr, k_out);
-    a.lines = heads_on_lines(q, cols, dtype) && heads_on_lines(k, cols, dtype);
     const uint64_t units = a.side[0].share.units + a.side[1].share.units;
     return launched(who, launch(a, dtype, (uint32_t)std::min<uint64_t>((units + 3) / 4, kMaxBlocks256), false, (hipStream_t)stream));
 }
@@ -555,8 +547,6 @@ extern "C" int reft_heads_backward(const reft_heads *dq_out, const reft_heads *d
         a.side[0] = side_of(q, rows, q_heads, cols, q_weight, dq_out, dq);
         if (k) a.side[1] = side_of(k, rows, k_heads, cols, k_weight, dk_out, dk);
         a.part = sums ? (float *)workspace : nullptr;
-        a.lines = heads_on_lines(q, cols, dtype) && heads_on_lines(k, cols, dtype) && heads_on_lines(dq_out, cols, dtype) &&
-                  heads_on_lines(dk_out, cols, dtype);
         e = launch(a, dtype, grid, true, s);
     }
     if (e == hipSuccess && sums) {
