@@ -1,0 +1,155 @@
+"""GPU tests of the ways that the operators inside the sublayers take: the same bits wherever rows lie (on cache lines, off them, further
+apart than 32 bits count), whatever else is asked for, and in whichever formats."""
+import pytest
+import torch
+
+import paper_2310_12670_amd as reft
+from oracle import step
+from test_gpu_inside import EPS, angles, check_forward, exactly
+from test_gpu_step import F8, dev, f64, normal  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def matrix(dev, rows, cols, dtype, ld, lead=0):  # noqa: F811
+    size = torch.empty((), dtype=dtype).element_size()
+    raw = torch.empty((lead + (rows - 1) * ld + cols) * size, dtype=torch.uint8, device=dev)
+    return torch.as_strided(raw.view(dtype), (rows, cols), (ld, 1), lead)
+
+
+def pair(dev, rows, cols, fmt, ld, lead=0):  # noqa: F811
+    return matrix(dev, rows, cols, F8[fmt], ld, lead), torch.full((-(-cols // 512), rows, 4), 0x5A, dtype=torch.uint8, device=dev)
+
+
+def up(n, m):
+    return -(-n // m) * m
+
+
+def same(a, b):
+    if isinstance(a, tuple):
+        return same(a[0], b[0]) and same(a[1], b[1])
+    return torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+
+LIES = {"lines": lambda n: (up(n, 128), 0), "off": lambda n: (n + 5, 3), "apart": lambda n: ((1 << 26) + 128, 0)}
+
+
+def gradients(dev, dy, g8, u8, fmt, y_fmt, lie, wide=True, kind="silu"):  # noqa: F811
+    rows, cols = dy.shape
+    outs = {}
+    for name in ("dg", "du") if u8 else ("dg",):
+        if wide:
+            outs[name] = matrix(dev, rows, cols, dy.dtype, *lie(cols))
+        outs[name + "8"], outs[name + "8_t"] = pair(dev, rows, cols, fmt, *lie(cols)), pair(dev, cols, rows, fmt, *lie(rows))
+    outs["y8_t"] = pair(dev, cols, rows, y_fmt, *lie(rows))
+    reft.reft_gate_backward(dy, g8, u8, kind, **outs)
+    return outs
+
+
+@pytest.mark.parametrize("rows,cols", [(128, 128), (384, 512), (300, 700), (1024, 256), (16, 2048)])
+@pytest.mark.parametrize("kind,gated", [("silu", True), ("gelu", False)])
+def test_gate_gradients_wherever_rows_lie(dev, rows, cols, kind, gated):  # noqa: F811
+    dy = normal(dev, 1, rows, cols, dtype=torch.bfloat16)
+    kept = []
+    for seed in (2, 3):
+        kept.append(pair(dev, rows, cols, "e4m3", up(cols, 16)))
+        reft.reft_quantize(normal(dev, seed, rows, cols, std=2.0), *kept[-1])
+    g8, u8 = kept[0], kept[1] if gated else None
+    want = gradients(dev, dy, g8, u8, "e4m3", "e4m3", LIES["lines"], kind=kind)
+    a, slope = step.act(step.scaled(f64(g8[0].float()), g8[1].cpu().numpy(), False), kind)
+    assert abs(f64(want["y8_t"][0].float())).max() > 100 and torch.isfinite(want["dg"]).all()       # 8 bits are used to their top
+    off = gradients(dev, dy, g8, u8, "e4m3", "e4m3", LIES["off"], kind=kind)
+    assert all(same(want[name], off[name]) for name in want)
+    # without the wide results tiles go in another order
+    bare = gradients(dev, dy, g8, u8, "e4m3", "e4m3", LIES["lines"], wide=False, kind=kind)
+    assert all(same(want[name], bare[name]) for name in bare)
+    # another format for y: the gradients' conversions are then chosen while the kernel runs
+    mixed = gradients(dev, dy, g8, u8, "e4m3", "e5m2", LIES["lines"], kind=kind)
+    assert all(same(want[name], mixed[name]) for name in want if name != "y8_t")
+    # y's transpose is what the forward pass says of y at the kept values, quantized
+    g, u = (step.scaled(f64(p[0].float()), p[1].cpu().numpy(), False) for p in kept)
+    y = matrix(dev, rows, cols, torch.float32, cols)
+    reft.reft_gate_forward(torch.from_numpy(g).float().to(dev), torch.from_numpy(u).float().to(dev) if gated else None, kind, y=y)
+    assert exactly(want["y8_t"], f64(y).T, "e4m3") and exactly(mixed["y8_t"], f64(y).T, "e5m2")
+
+
+def test_gate_gradients_of_rows_far_apart(dev):  # noqa: F811
+    """Rows 2^26 elements apart and more, whose offsets need 64 bits, in tiles that are whole and not."""
+    rows, cols = 140, 300
+    dy = normal(dev, 1, rows, cols, dtype=torch.bfloat16)
+    kept = [pair(dev, rows, cols, "e4m3", up(cols, 16)) for _ in range(2)]
+    for seed, p in enumerate(kept):
+        reft.reft_quantize(normal(dev, seed, rows, cols, std=2.0), *p)
+    want = gradients(dev, dy, *kept, "e4m3", "e4m3", LIES["lines"])
+    far = pair(dev, rows, cols, "e4m3", (1 << 26) + 128)
+    far[0].view(torch.uint8).copy_(kept[0][0].view(torch.uint8))
+    far[1].copy_(kept[0][1])
+    got = gradients(dev, dy, far, kept[1], "e4m3", "e4m3", LIES["off"])
+    assert all(same(want[name], got[name]) for name in want)
+    turned, near = pair(dev, cols, rows, "e4m3", up(rows, 128)), pair(dev, cols, rows, "e4m3", rows)
+    reft.reft_transpose(*far, *turned)
+    reft.reft_transpose(*kept[0], *near)
+    assert same(turned, near)
+    y, z = pair(dev, rows, cols, "e4m3", (1 << 26) + 128), pair(dev, rows, cols, "e4m3", cols)
+    reft.reft_gate_forward(dy, None, "relu2", g8=y)
+    reft.reft_gate_forward(dy, None, "relu2", g8=z)
+    assert same(y, z)
+
+
+@pytest.mark.parametrize("rows,cols", [(128, 128), (512, 640), (300, 700), (8, 4096)])
+@pytest.mark.parametrize("fmt,to", [("e4m3", "e4m3"), ("e5m2", "e4m3")])
+def test_transposes_wherever_rows_lie(dev, rows, cols, fmt, to):  # noqa: F811
+    got = []
+    for lie in ("lines", "off"):
+        x8, t8 = pair(dev, rows, cols, fmt, *LIES[lie](cols)), pair(dev, cols, rows, to, *LIES[lie](rows))
+        reft.reft_quantize(normal(dev, 5, rows, cols) * torch.exp2(normal(dev, 6, rows, 1) * 4), *x8)
+        reft.reft_transpose(*x8, *t8)
+        got.append(t8)
+    assert same(*got)
+    # there and back: values that kept their bits are as they were
+    back = pair(dev, rows, cols, fmt, cols)
+    reft.reft_transpose(*got[0], *back)
+    want, e = step.transpose(f64(got[0][0].float()), got[0][1].cpu().numpy(), fmt)
+    assert exactly(back, step.scaled(f64(got[0][0].float()), got[0][1].cpu().numpy(), False).T, fmt)
+
+
+@pytest.mark.parametrize("cols,pairs", [(128, 64), (80, 16), (64, 32), (256, 128), (72, 20)])
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_heads_whatever_else_is_in_the_call(dev, cols, pairs, adjacent):  # noqa: F811
+    """A head's result depends on that head, its weight and its row's position alone: not on how many rows and heads there are, how they are
+    shared out, or where they lie."""
+    rows, heads = 600, 12
+    x = normal(dev, 1, rows, heads, cols, dtype=torch.bfloat16)
+    w = (1 + normal(dev, 2, cols, std=0.2)).to(torch.bfloat16)
+    positions, freqs = angles(dev, rows, pairs)
+    out, dx, dout = torch.empty_like(x), torch.empty_like(x), normal(dev, 3, rows, heads, cols, dtype=torch.bfloat16)
+    reft.reft_heads_forward(x, None, w, None, positions, freqs, EPS, out, adjacent=adjacent)
+    reft.reft_heads_backward(dout, None, x, None, w, None, positions, freqs, EPS, adjacent=adjacent, dq=dx)
+    check_forward(out, x, w, positions, freqs, adjacent, "bf16")
+    for r, h in ((slice(0, 1), slice(0, 12)), (slice(5, 6), slice(3, 4)), (slice(17, 300), slice(2, 5)), (slice(0, 600), slice(7, 8))):
+        k, other = x[:, :1][r], torch.empty_like(x[r, h])
+        also = torch.empty_like(k)
+        reft.reft_heads_forward(x[r, h], k, w, None, positions[r], freqs, EPS, other, also, adjacent=adjacent)
+        assert torch.equal(other, out[r, h])
+        reft.reft_heads_backward(dout[r, h], k, x[r, h], k, w, None, positions[r], freqs, EPS, adjacent=adjacent, dq=other)
+        assert torch.equal(other, dx[r, h])
+
+
+def test_operands_in_pinned_host_memory(dev):  # noqa: F811
+    x = normal(dev, 1, 40, 2, 64)
+    positions, freqs = angles(dev, 40, 32)
+    want, got = torch.empty_like(x), torch.empty_like(x)
+    reft.reft_heads_forward(x, None, None, None, positions, freqs, EPS, want)
+    host = torch.empty(40, 2, 64, pin_memory=True)
+    host.copy_(x.cpu())
+    at = torch.empty(40, dtype=torch.int64, pin_memory=True)
+    at.copy_(positions.cpu())
+    reft.reft_heads_forward(host, None, None, None, at, freqs, EPS, got)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    flat = host.view(40, 128)
+    a, b = pair(dev, 40, 128, "e4m3", 128), pair(dev, 40, 128, "e4m3", 128)
+    reft.reft_gate_forward(flat, flat, "silu", y8=a)
+    reft.reft_gate_forward(x.view(40, 128), x.view(40, 128), "silu", y8=b)
+    torch.cuda.synchronize()
+    assert same(a, b)
