@@ -219,7 +219,6 @@ template <typename O> struct Place {
     __device__ __forceinline__ Place()
     {
         lane = threadIdx.x & 63;
-        asm volatile("" : "+v"(lane));                      // what follows from it is computed anew for each tile, and not held
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         c = (lane & 15) * 8;
         r = wave * 4 * kRows + (lane >> 4) * kRows;
