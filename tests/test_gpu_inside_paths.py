@@ -153,3 +153,57 @@ def test_operands_in_pinned_host_memory(dev):  # noqa: F811
     reft.reft_gate_forward(x.view(40, 128), x.view(40, 128), "silu", y8=b)
     torch.cuda.synchronize()
     assert same(a, b)
+
+
+def test_more_than_two_to_the_31_values(dev):  # noqa: F811
+    """The last rows of matrices whose elements and bytes do not count in 32 bits are as those rows alone."""
+    rows, cols, tail = 36000, 65536, 36000 - 281 * 128                       # the last tile of rows begins at 281 * 128
+    free, _ = torch.cuda.mem_get_info()
+    if free < 40 << 30:
+        pytest.skip("needs 40 GB")
+    g = torch.empty(rows, cols, dtype=torch.bfloat16, device=dev)
+    g.view(torch.int16).fill_(0x3F80)
+    g[-tail:].copy_(normal(dev, 1, tail, cols))
+    small = g[-tail:].clone()
+    g8, one = pair(dev, rows, cols, "e4m3", cols), pair(dev, tail, cols, "e4m3", cols)
+    reft.reft_gate_forward(g, None, "silu", y8=g8)
+    reft.reft_gate_forward(small, None, "silu", y8=one)
+    assert same(g8[0][-tail:], one[0]) and torch.equal(g8[1][:, -tail:], one[1])
+    t8, t1 = pair(dev, cols, rows, "e4m3", rows), pair(dev, cols, tail, "e4m3", tail)
+    reft.reft_transpose(*g8, *t8)
+    reft.reft_transpose(*one, *t1)
+    assert same(t8[0][:, -tail:], t1[0]) and torch.equal(t8[1][-1][:, 1], t1[1][0][:, 0])
+    reft.reft_gate_backward(g, g8, None, "gelu", dg=g, dg8_t=t8)
+    reft.reft_gate_backward(small, one, None, "gelu", dg=small, dg8_t=t1)
+    assert same(g[-tail:], small) and same(t8[0][:, -tail:], t1[0])
+    del g8, t8
+    n, heads, c = 128, 72, 128
+    x = g.view(-1)[:250000 * heads * c].view(250000, heads, c)
+    positions, freqs = angles(dev, 250000, 64)
+    x[-n:].copy_(normal(dev, 3, n, heads, c))
+    few = x[-n:].clone()
+    reft.reft_heads_forward(x, None, None, None, positions, freqs, EPS, x)
+    reft.reft_heads_forward(few, None, None, None, positions[-n:], freqs, EPS, few)
+    assert torch.equal(x[-n:], few)
+    reft.reft_heads_backward(x, None, x, None, None, None, positions, freqs, EPS, dq=x)
+    reft.reft_heads_backward(few, None, few, None, None, None, positions[-n:], freqs, EPS, dq=few)
+    assert torch.equal(x[-n:], few)
+
+
+@pytest.mark.parametrize("q_heads,k_heads", [(2, 9), (1, 40)])
+def test_more_keys_than_queries_and_results_over_inputs(dev, q_heads, k_heads):  # noqa: F811
+    rows, cols = 300, 96
+    q, k = normal(dev, 1, rows, q_heads, cols), normal(dev, 2, rows, k_heads, cols)
+    dq_out, dk_out = normal(dev, 3, rows, q_heads, cols), normal(dev, 4, rows, k_heads, cols)
+    w = 1 + normal(dev, 5, cols, std=0.2)
+    positions, freqs = angles(dev, rows, 48)
+    outs = torch.empty_like(q), torch.empty_like(k)
+    reft.reft_heads_forward(q, k, w, w, positions, freqs, EPS, *outs)
+    for x, out in ((q, outs[0]), (k, outs[1])):
+        check_forward(out, x, w, positions, freqs, False, "f32")
+    dw = torch.empty(4, cols, device=dev)
+    ws = torch.empty(reft.reft_heads_backward_workspace(rows, q_heads, k_heads, cols), dtype=torch.uint8, device=dev)
+    args = (dq_out, dk_out, q, k, w, w, positions, freqs, EPS)
+    reft.reft_heads_backward(*args, dq=outs[0], dk=outs[1], dq_weight=dw[0], dk_weight=dw[1], workspace=ws)
+    reft.reft_heads_backward(*args, dq=q, dk=k, dq_weight=dw[2], dk_weight=dw[3], workspace=ws)
+    assert torch.equal(q, outs[0]) and torch.equal(k, outs[1]) and torch.equal(dw[:2], dw[2:])
