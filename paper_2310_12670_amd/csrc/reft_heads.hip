@@ -405,6 +405,7 @@ template <typename T, int G> static hipError_t launch(const HeadsArgs &a, uint32
     if (a.adjacent && whole) launch<T, G, kAdjacent, true>(a, grid, back, s);
     else if (a.adjacent) launch<T, G, kAdjacent, false>(a, grid, back, s);
     else if (a.pairs % 8 == 0 && whole) launch<T, G, kLane, true>(a, grid, back, s);
+    else if (whole) launch<T, G, kAny, true>(a, grid, back, s);
     else launch<T, G, kAny, false>(a, grid, back, s);
     return hipGetLastError();
 }
