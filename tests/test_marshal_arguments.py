@@ -58,17 +58,18 @@ def both(tmp_path_factory):
     """(the C part on the stub, the stub)"""
     d = tmp_path_factory.mktemp("marshal")
     (d / "stub.c").write_text(stub(NAMES + REST))
-    subprocess.run(["gcc", "-O1", "-w", "-fPIC", "-shared", "-o", str(d / "libreft.so"), str(d / "stub.c")], check=True)
+    # a name of its own: one that is loaded already would stand for it
+    subprocess.run(["gcc", "-O1", "-w", "-fPIC", "-shared", "-o", str(d / "libstub.so"), str(d / "stub.c")], check=True)
     out = str(d / ("_marshal" + sysconfig.get_config_var("EXT_SUFFIX")))
     subprocess.run(["gcc", "-O2", "-std=c11", "-Wall", "-Wextra", "-Wno-unused-parameter", "-Wno-missing-field-initializers", "-Werror", "-fPIC",
                     "-shared", "-I", sysconfig.get_paths()["include"], "-o", out, os.path.join(build.CSRC, "reft_marshal.c"), "-L", str(d),
-                    "-l:libreft.so", "-Wl,-rpath,$ORIGIN"], check=True)
+                    "-l:libstub.so", "-Wl,-rpath,$ORIGIN"], check=True)
     spec = importlib.util.spec_from_file_location("_marshal", out)
     part = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(part)
     for t, code in ((torch.float32, 0), (torch.bfloat16, 1), (torch.float16, 2), (F8[0], 3), (F8[1], 4), (torch.int64, 5)):
         part.know(t, code)
-    lib = ctypes.CDLL(str(d / "libreft.so"))
+    lib = ctypes.CDLL(str(d / "libstub.so"))
     lib.stub_said.restype = ctypes.c_char_p
     real = reft.binding._load()
     for name in NAMES + REST:
