@@ -200,7 +200,7 @@ struct Unit {
 
 // out = rho (x (w cos) + x_partner (w_partner +- sin)), with rho = 1 / rms: the weights and angles are joined once a unit, so that a value takes a
 // square, two products and rho.  Everything is read once and written once, all of a unit's next heads on their way.  Bound by HBM: 16384 rows of
-// 64 + 8 heads of 128 in bf16 118 us, 5.1 TB/s (vector units busy 46 %; a lane a head's eight columns with its own sines 656 us, sines once
+// 64 + 8 heads of 128 in bf16 118 us, 5.1 TB/s (vector units busy 43 %; a lane a head's eight columns with its own sines 656 us, sines once
 // a row 122, no element-wise ends 117; results through the L2 122; loads past it no different); 1024 of them 8.3 us, one 3.2.  Four heads at once in more
 // registers, four waves a SIMD instead of five: 116, 10.5 and 3.3; three: 115, 9.9 and 3.3.
 template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 5) void k_heads_forward(HeadsArgs a)
