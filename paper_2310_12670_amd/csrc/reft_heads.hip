@@ -115,8 +115,14 @@ template <typename T, int G, int MODE, bool WHOLE> struct Wave {
         partner = MODE == kAny ? lane / G * G * 8 : !turns ? lane : lower ? lane + pairs / 8 : lane - pairs / 8;
         pair0 = MODE == kAdjacent ? c0 / 2 : !turns ? pairs : lower ? c0 : c0 - pairs;
     }
-    // The wave's other lanes see what this one has written; nothing moves across.
-    __device__ __forceinline__ static void settle() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+    // The wave's lanes come together and see what the others have written; nothing moves across.  The barrier in the middle is no instruction: it
+    // is what keeps the compiler from running some lanes ahead where only part of them has gone through a loop or branch before (a fence does not).
+    __device__ __forceinline__ static void settle()
+    {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
 
     __device__ __forceinline__ void turn(const HeadsArgs &a, uint64_t row0, int rows, int row)
     {
