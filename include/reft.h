@@ -587,7 +587,8 @@ typedef struct reft_eight {
  *   out[first] = z[first] cos t - z[second] sin t,  out[second] = z[second] cos t + z[first] sin t,  out[c] = z[c] behind the pairs.
  * Angles are products in 64 bits (exact for positions below 2^29; at most 2^50), sines and cosines of them err by less than 2^-22.  A weight is a
  * vector of cols values for all heads of its kind in weight_dtype (dtype or fp32), NULL: ones.  positions and freqs may be NULL with pairs == 0.
- * Where a head holds an infinity or a NaN its results are zeroes and NaN; no other head's are touched by it.
+ * Where a head holds an infinity or a NaN its results are zeroes and NaN; no other head's are touched by it.  Such a weight reaches its own column
+ * and, where that turns, its partner's.
  * An output may be its input (with the same strides).  rows < 2^31, 1 to 65535 heads of each kind, 1 <= cols <= 512, 2 pairs <= cols.
  */
 int reft_heads_forward(const reft_heads *q, uint64_t q_heads, const reft_heads *k, uint64_t k_heads, const void *q_weight,
@@ -598,6 +599,7 @@ int reft_heads_forward(const reft_heads *q, uint64_t q_heads, const reft_heads *
 /* The gradients of reft_heads_forward's inputs and weights, from those of its outputs (dq_out, dk_out) and its other arguments.  With u the
  * gradient of z (dout turned back) and x' = x / sqrt(mean(x^2) + eps):
  *   dx = (u weight - x' mean(u weight x')) / sqrt(mean(x^2) + eps),  dweight[c] = sum over rows and heads of u x'.
+ * An infinity or a NaN in a head of dout makes that head's dx infinities and NaN; of dweight it reaches its own column and its partner's.
  * dq, dk and the weights' gradients (fp32) are each left out where NULL; dq may be dq_out or q, dk dk_out or k (with the same strides).
  * rows == 0 gives dweight = 0.  workspace: on 16 bytes, of at least reft_heads_backward_workspace(rows, q_heads, k_heads, cols) bytes where a
  * weight's gradient is wanted; scratch, not shared with a call in flight.

@@ -96,9 +96,9 @@ template <bool WHOLE, typename T> __device__ __forceinline__ void store_part(T *
 // A wave works on several rows at once, each with some of its 64 / G groups of G lanes; a group's lanes hold eight columns of a head each.
 // Sines and cosines are computed once a row, one pair a lane and turn, and pass through the wave's own part of LDS, as do the partners of kAny.
 template <typename T, int G, int MODE, bool WHOLE> struct Wave {
-    struct Room {
+    struct __align__(16) Room {                             // so that a lane's eight values are two accesses
         float2 turn[4 * 64];                               // of a row 4 G pairs, those that do not turn with one and zero
-        float values[MODE == kAny ? 64 * 8 : 1];
+        float values[MODE == kAny ? 64 * 8 + 1 : 1];       // and a zero
     };
     Room &room;
     const int lane, pairs;
@@ -114,6 +114,7 @@ template <typename T, int G, int MODE, bool WHOLE> struct Wave {
         const bool turns = c0 < 2 * pairs;
         partner = MODE == kAny ? lane / G * G * 8 : !turns ? lane : lower ? lane + pairs / 8 : lane - pairs / 8;
         pair0 = MODE == kAdjacent ? c0 / 2 : !turns ? pairs : lower ? c0 : c0 - pairs;
+        if (MODE == kAny) room.values[64 * 8] = 0;
     }
     // The wave's lanes come together and see what the others have written; nothing moves across.  The barrier in the middle is no instruction: it
     // is what keeps the compiler from running some lanes ahead where only part of them has gone through a loop or branch before (a fence does not).
@@ -143,21 +144,14 @@ template <typename T, int G, int MODE, bool WHOLE> struct Wave {
             sine[i] = (MODE == kAdjacent ? !(i & 1) : MODE == kLane ? lower : c < pairs) ? -t.y : t.y;
         }
     }
-    // The values of the partners' columns.
-    template <typename E> __device__ __forceinline__ void partners(const Eight<E> &x, float v[8])
+    // All bits where column i of the lane's is one of a pair, none where it is not.
+    __device__ __forceinline__ uint32_t in_pair(int i) const { return (uint32_t)((c0 + (MODE == kLane ? 0 : i) - 2 * pairs) >> 31); }
+    // The values of the partners' columns.  A column that does not turn has a sine of zero; where what stands beside it or itself need be no number
+    // (APART), it gets a zero as well: zero times an infinity would be a NaN.
+    template <bool APART, typename E> __device__ __forceinline__ void partners(const Eight<E> &x, float v[8])
     {
-        if constexpr (MODE == kAdjacent) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = x[i ^ 1];
-        } else if constexpr (MODE == kLane) {
-            Eight<E> y;
-#pragma unroll
-            for (int i = 0; i < (int)sizeof(E) / 2; ++i)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) y.w[i][k] = (uint32_t)__shfl((int)x.w[i][k], partner);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = y[i];
-        } else {
+        constexpr int kWords = (int)sizeof(E) / 2;
+        if constexpr (MODE == kAny) {
             settle();
 #pragma unroll
             for (int i = 0; i < 8; ++i) room.values[partner + c0 + i] = x[i];
@@ -165,8 +159,19 @@ template <typename T, int G, int MODE, bool WHOLE> struct Wave {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int c = c0 + i;
-                v[i] = room.values[partner + (c >= 2 * pairs ? c : c < pairs ? c + pairs : c - pairs)];
+                v[i] = room.values[c >= 2 * pairs ? 64 * 8 : partner + (c < pairs ? c + pairs : c - pairs)];
             }
+        } else {
+            Eight<E> y;
+#pragma unroll
+            for (int i = 0; i < kWords; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    y.w[i][k] = MODE == kLane ? (uint32_t)__shfl((int)x.w[i][k], partner) : x.w[i][k];
+                    if (APART) y.w[i][k] &= in_pair(kWords == 1 ? 2 * k : (4 * i + k) & ~1);
+                }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = y[MODE == kLane ? i : i ^ 1];
         }
     }
     __device__ __forceinline__ Eight<float> weight(const HeadsArgs &a, const Side &s)
@@ -236,7 +241,7 @@ template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(
         float other[8], by_own[8], by_other[8];
         const Eight<float> weight = w.weight(a, s);
         w.turn(a, u.row0, s.share.wave_rows, u.turn);
-        w.partners(weight, other);
+        w.template partners<true>(weight, other);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             by_own[i] = weight.t[i] * w.cosine[i];
@@ -250,7 +255,7 @@ template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(
             for (int k = 0; k < kAhead; ++k) {
                 if (k && head0 + k * u.step >= s.heads) break;
                 float v[8], sum = 0;
-                w.partners(x[k], other);
+                w.template partners<false>(x[k], other);       // of a head with an infinity all is lost
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     v[i] = x[k][i];
@@ -314,7 +319,7 @@ template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(
                     if (k && head0 + k * u.step >= s.heads) break;
                     const int n = head0 + k * u.step + u.slot < s.heads ? there : 0;
                     float other[8], t[8], sum = 0, dot = 0;
-                    w.partners(dy[k], other);
+                    w.template partners<true>(dy[k], other);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const float v = x[k][i];
