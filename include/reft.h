@@ -602,7 +602,8 @@ int reft_heads_forward(const reft_heads *q, uint64_t q_heads, const reft_heads *
  * An infinity or a NaN in a head of dout makes that head's dx infinities and NaN; of dweight it reaches its own column and its partner's.
  * dq, dk and the weights' gradients (fp32) are each left out where NULL; dq may be dq_out or q, dk dk_out or k (with the same strides).
  * rows == 0 gives dweight = 0.  workspace: on 16 bytes, of at least reft_heads_backward_workspace(rows, q_heads, k_heads, cols) bytes where a
- * weight's gradient is wanted; scratch, not shared with a call in flight.
+ * weight's gradient is wanted; scratch, not shared with a call in flight.  More rows, heads or columns never need less, with keys or without (at most
+ * 4096 cols bytes), so that a workspace for the largest call serves all.
  */
 uint64_t reft_heads_backward_workspace(uint64_t rows, uint64_t q_heads, uint64_t k_heads, uint64_t cols);
 int reft_heads_backward(const reft_heads *dq_out, const reft_heads *dk_out, const reft_heads *q, uint64_t q_heads,
