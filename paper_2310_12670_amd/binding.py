@@ -808,7 +808,7 @@ _ACTS = {"silu": REFT_SILU, "gelu": REFT_GELU, "gelu_tanh": REFT_GELU_TANH, "rel
 def _act(who: str, act) -> int:
     """An activation by its name, or its number."""
     code = _ACTS.get(act, act) if isinstance(act, (str, int)) else None
-    if not isinstance(code, int):
+    if not isinstance(code, int) or not REFT_SILU <= code <= REFT_RELU2:
         _refuse(who, f"unknown activation {act!r}")
     return code
 
