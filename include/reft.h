@@ -589,6 +589,9 @@ typedef struct reft_eight {
  * vector of cols values for all heads of its kind in weight_dtype (dtype or fp32), NULL: ones.  positions and freqs may be NULL with pairs == 0.
  * Where a head holds an infinity or a NaN its results are zeroes and NaN; no other head's are touched by it.  Such a weight reaches its own column
  * and, where that turns, its partner's.
+ * Finite heads whose sum of squares reaches 2^128 (from 1.8e19 an element on) count as infinitely long, with results of zero.  With eps == 0 (eps
+ * counts in fp32) squares below 2^-126 lose their last bits, and heads whose squares vanish have infinities and NaN, as heads of zeroes have NaN.
+ * 1 / sqrt is the hardware's, to a step of fp32.
  * An output may be its input (with the same strides).  rows < 2^31, 1 to 65535 heads of each kind, 1 <= cols <= 512, 2 pairs <= cols.
  */
 int reft_heads_forward(const reft_heads *q, uint64_t q_heads, const reft_heads *k, uint64_t k_heads, const void *q_weight,
@@ -600,6 +603,7 @@ int reft_heads_forward(const reft_heads *q, uint64_t q_heads, const reft_heads *
  * gradient of z (dout turned back) and x' = x / sqrt(mean(x^2) + eps):
  *   dx = (u weight - x' mean(u weight x')) / sqrt(mean(x^2) + eps),  dweight[c] = sum over rows and heads of u x'.
  * An infinity or a NaN in a head of dout makes that head's dx infinities and NaN; of dweight it reaches its own column and its partner's.
+ * A head that is too long (see above) has dx = 0 and no part in dweight.
  * dq, dk and the weights' gradients (fp32) are each left out where NULL; dq may be dq_out or q, dk dk_out or k (with the same strides).
  * rows == 0 gives dweight = 0.  workspace: on 16 bytes, of at least reft_heads_backward_workspace(rows, q_heads, k_heads, cols) bytes where a
  * weight's gradient is wanted; scratch, not shared with a call in flight.  More rows, heads or columns never need less, with keys or without (at most
@@ -618,6 +622,9 @@ int reft_heads_backward(const reft_heads *dq_out, const reft_heads *dk_out, cons
  *   REFT_GELU       g (1 + erf(g / sqrt(2))) / 2
  *   REFT_GELU_TANH  g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2
  *   REFT_RELU2      max(g, 0)^2
+ * The exponentials' exponents v are rounded in fp32, so that small results err by more than a step, relative to their value by up to (in 2^-24)
+ * 1.25 |v| + 8 for silu (v = g), 2.25 |v| + 40 for gelu (v = g^2 / 2) and 6 |v| + 8 for gelu_tanh (v = sqrt(8 / pi) (g + 0.044715 g^3)); exponentials and
+ * reciprocals below 2^-126 are zero.  Slopes are of the same quality.
  * Outputs are each left out where NULL.  y may be g or u (with the same ld).  Where a block of 128 values of g8, u8 or y8 holds an infinity or
  * a NaN, all of it is NaN.  rows, cols < 2^31, rows ceil(cols / 512) <= 2^26 - 4.
  */

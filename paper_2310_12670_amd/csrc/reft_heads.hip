@@ -213,8 +213,9 @@ struct Unit {
 // square, two products and rho.  Everything is read once and written once, all of a unit's next heads on their way.  Bound by HBM: 16384 rows of
 // 64 + 8 heads of 128 in bf16 118 us, 5.1 TB/s (vector units busy 43 %; a lane a head's eight columns with its own sines 656 us, sines once
 // a row 122, no element-wise ends 117; results through the L2 122; loads past it no different); 1024 of them 8.3 us, one 3.2.  Four heads at once in more
-// registers, four waves a SIMD instead of five: 116, 10.5 and 3.3; three: 115, 9.9 and 3.3.
-template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 5) void k_heads_forward(HeadsArgs a)
+// registers, four waves a SIMD instead of five: 116, 10.5 and 3.3; three: 115, 9.9 and 3.3.  Five waves leave 96 registers, which all kernels keep to without a spill
+// but those of at most 64 columns, no multiple of 8, with halves as pairs: they take four (4000 rows of 24 heads of 60 in bf16 15.7 -> 14.9 us).
+template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : MODE == kAny && !WHOLE && G == 8 ? 4 : 5) void k_heads_forward(HeadsArgs a)
 {
     typedef Wave<T, G, MODE, WHOLE> W;
     __shared__ typename W::Room room[4];
@@ -261,7 +262,19 @@ template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(
                     v[i] = x[k][i];
                     sum += v[i] * v[i];
                 }
-                const float r = inverse_root(sum_of<G>(sum) * a.inverse_cols + a.eps);
+                sum = sum_of<G>(sum);
+                float r = inverse_root(sum * a.inverse_cols + a.eps);
+                const bool endless = !(sum < INFINITY);
+                if (__builtin_expect(__any(endless), 0)) {
+                    // a head that is too long: two of its values need not add up to a number, r times them are zeroes
+                    const float by = endless ? r : 1.f;
+                    r = endless ? 1.f : r;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        v[i] *= by;
+                        other[i] *= by;
+                    }
+                }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = r * (v[i] * by_own[i] + other[i] * by_other[i]);
                 store_part<WHOLE>(to + k * step_out, head0 + k * u.step + u.slot < s.heads ? there : 0, v);
@@ -329,7 +342,8 @@ template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(
                     }
                     float r = inverse_root(sum_of<G>(sum) * a.inverse_cols + a.eps);
                     r = n > 0 ? r : 0.f;                    // of zeroes that do not exist it may be infinite
-                    dot = r * (sum_of<G>(dot) * a.inverse_cols);
+                    dot = sum_of<G>(dot) * a.inverse_cols;
+                    dot = r == 0 ? 0.f : r * dot;           // of a head that is too long it may be infinite
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const float xhat = x[k][i] * r;
