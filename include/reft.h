@@ -563,7 +563,7 @@ int reft_product(const void *a, uint64_t ld_a, int a_format, const void *a_scale
 /* ---- inside the sublayers -------------------------------------------------------------------------------
  * What lies between the products: queries and keys on their way into attention, the activation of a feed-forward, and the
  * 8-bit matrices that the forward pass keeps for the backward pass.  As above: no atomics, sums in an order of the sizes alone, fp32
- * within, one rounding.
+ * within, one rounding.  Outputs lie apart from each other and from all inputs but those that they may take the place of.
  */
 
 /* Values [rows][heads][cols]: element (r, a, c) is number r * row + a * head + c behind p.  Heads may lie one after the other
@@ -592,7 +592,7 @@ typedef struct reft_eight {
  * Finite heads whose sum of squares reaches 2^128 (from 1.8e19 an element on) count as infinitely long, with results of zero.  With eps == 0 (eps
  * counts in fp32) squares below 2^-126 lose their last bits, and heads whose squares vanish have infinities and NaN, as heads of zeroes have NaN.
  * 1 / sqrt is the hardware's, to a step of fp32.
- * An output may be its input (with the same strides).  rows < 2^31, 1 to 65535 heads of each kind, 1 <= cols <= 512, 2 pairs <= cols.
+ * q_out may be q, k_out k (with the same strides).  rows < 2^31, 1 to 65535 heads of each kind, 1 <= cols <= 512, 2 pairs <= cols.
  */
 int reft_heads_forward(const reft_heads *q, uint64_t q_heads, const reft_heads *k, uint64_t k_heads, const void *q_weight,
                        const void *k_weight, const int64_t *positions, const float *freqs, uint64_t pairs, int adjacent,

@@ -364,7 +364,8 @@ __device__ __forceinline__ EightOut read(const __attribute__((address_space(4)))
 // is worked on once.  The rows' results leave while the columns' powers of two are settled, then the columns' (three tiles of fp32 in
 // registers) through LDS.  16384 x 11008 in bf16, silu, all five 8-bit results, 333 to 349 us, 4.7 to 4.9 TB/s: HBM's rate explains 70 % of the
 // time, the vector units' 31 instructions a value 50 %, and two blocks a compute unit (their registers allow no more) do not hide all of one
-// behind the other.  (160 registers, one block: 570 us; 128 with 55 spilled: 475; a block of 1024 that has its next tile on the way: 467.)  FULL: the tile lies within the matrix;
+// behind the other; the rows' results alone take 218 us (5.0 TB/s), the columns' alone 292 (4.3).  At the ends of a matrix each row's loads are behind branches
+// and waits of their own, one round trip to memory after the other: 1001 x 1728 14 us.  (160 registers, one block: 570 us; 128 with 55 spilled: 475; a block of 1024 that has its next tile on the way: 467.)  FULL: the tile lies within the matrix;
 // E4M3: so are all 8-bit matrices, and no conversion is chosen while it runs (4096 x 4096 32 -> 28 us).
 template <typename T, int ACT, bool FULL, bool E4M3, bool LINES, typename O> __device__ __forceinline__ void gate_tile(const Tile &t, Turn<3, O> &turn)
 {

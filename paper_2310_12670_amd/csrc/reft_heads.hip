@@ -214,7 +214,8 @@ struct Unit {
 // 64 + 8 heads of 128 in bf16 118 us, 5.1 TB/s (vector units busy 43 %; a lane a head's eight columns with its own sines 656 us, sines once
 // a row 122, no element-wise ends 117; results through the L2 122; loads past it no different); 1024 of them 8.3 us, one 3.2.  Four heads at once in more
 // registers, four waves a SIMD instead of five: 116, 10.5 and 3.3; three: 115, 9.9 and 3.3.  Five waves leave 96 registers, which all kernels keep to without a spill
-// but those of at most 64 columns, no multiple of 8, with halves as pairs: they take four (4000 rows of 24 heads of 60 in bf16 15.7 -> 14.9 us).
+// but those of at most 64 columns, no multiple of 8, with halves as pairs: they take four (4000 rows of 24 heads of 60 in bf16 15.7 -> 14.9 us,
+// 16384 of 40 in f16 66 -> 67).
 template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : MODE == kAny && !WHOLE && G == 8 ? 4 : 5) void k_heads_forward(HeadsArgs a)
 {
     typedef Wave<T, G, MODE, WHOLE> W;
@@ -284,7 +285,7 @@ template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(
 }
 
 // With u = dout turned back, xhat = x rho: dx = rho (u w - xhat mean(u w xhat)), dweight = sum of u xhat; both means of a head in one go over its lanes,
-// of x^2 and of u w x.  Bound by HBM: 16384 rows of 64 + 8 heads of 128 in bf16 182 us, 5.0 TB/s (queries' and keys' weights summed at once,
+// of x^2 and of u w x.  16384 rows of 64 + 8 heads of 128 in bf16 184 us, 4.9 TB/s, on two waves a SIMD (queries' and keys' weights summed at once,
 // which takes 16 registers more: 228; at 128 registers with four waves a SIMD: 411, spilled).
 // The gradients; a lane sums its heads' part of a weight's gradient, the block adds its groups' in their order.  Queries first, then keys.
 template <typename T, int G, int MODE, bool WHOLE> __global__ __launch_bounds__(256) void k_heads_backward(HeadsArgs a)
